@@ -1,0 +1,428 @@
+"""The operators that decode on a compacted cache, at the sizes they are called at: what is timed when they are timed.
+
+A cache holds, for every (sequence, KV head) segment, a room of rows in packed K and V arrays and the number of
+rows in use.  Four calls work on it:
+
+  fill    a prefill's kept rows enter the cache, narrowed to its type (4 bits: blocks of 32 E2M1 values that share a power of two)
+  append  the next tokens' rows enter behind them
+  attend  the attention of the next tokens' queries over the rows in use, and the weight each row got, added up
+  evict   the rows with the least added-up weight leave, the latest ones stay
+
+Rows that a call leaves in 8 or 4 bits are read back as 16-bit values (`Cache.rows`), as a program does that hands
+them to the selection by pooled importance.  Capacities differ between heads as an INF_sc map makes them differ: most
+heads small, a few large.  Values are synthetic: keys with channels of unequal size, queries that concentrate on some
+keys.  The lengths belong to the case, the values to the seed.
+"""
+
+import math
+import random
+
+import torch
+
+own = False
+
+QUERY = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "bf16_kv8": torch.bfloat16, "bf16_kv4": torch.bfloat16}
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+BLOCK = 32
+
+
+def _case(name, op, dtype, B, avg, **kw):
+    c = dict(name=name, op=op, dtype=dtype, B=B, Hq=32, Hkv=8, d=128, T=1, avg=avg, slack=128, skew=True, weights=True, keep=0, shape=1)
+    c.update(kw)
+    return c
+
+
+def listed():
+    return [
+        # the next token of one conversation whose cache holds 128 rows a head on average: latency
+        _case("attend_one_prompt", "attend", "bf16", 1, 128, slack=64),
+        # 16 conversations of 1024 rows a head: the ordinary serving step that feeds the eviction
+        _case("attend_batch", "attend", "bf16", 16, 1024),
+        # an uncompressed history of 32 K tokens, one sequence, nobody evicts
+        _case("attend_long_history", "attend", "bf16", 1, 32768, skew=False, weights=False),
+        # 8-bit cache, a larger batch
+        _case("attend_batch_kv8", "attend", "bf16_kv8", 32, 2048, shape=2),
+        # five drafted tokens checked at once, fp16, short head dimension, odd lengths
+        _case("attend_draft_f16", "attend", "f16", 6, 777, d=64, Hq=24, T=5, slack=77, shape=3),
+        # fp32, as many KV heads as query heads
+        _case("attend_f32", "attend", "f32", 2, 1000, Hq=4, Hkv=4, d=64, slack=24, skew=False),
+        # the 4-bit cache: a large batch of compacted conversations, and four long histories whose rows are all kept
+        _case("attend_batch_kv4", "attend", "bf16_kv4", 64, 1024, shape=4),
+        _case("attend_long_kv4", "attend", "bf16_kv4", 4, 79152, skew=False, shape=5, weights=False),
+        # the rows that a batch of prefills keeps enter the 4-bit cache; then one token of every conversation
+        _case("fill_kv4", "fill", "bf16_kv4", 16, 1024, shape=6),
+        _case("append_kv4", "append", "bf16_kv4", 64, 256, shape=7),
+        # eviction: a few rows too many after 128 tokens; a whole history down to its capacity in 4 bits
+        _case("evict_batch", "evict", "bf16", 16, 1024, keep=32, shape=8),
+        _case("evict_history_kv4", "evict", "bf16_kv4", 2, 1024, slack=30001, keep=64, shape=9),
+    ]
+
+
+MOST_BYTES = 240e6      # that a drawn case reads and writes
+
+
+def draw(rng):
+    def spread(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    op = rng.choice(["attend"] * 5 + ["fill", "append", "evict", "evict"])
+    dtype = rng.choice(["f32", "bf16", "bf16", "f16", "bf16_kv8", "bf16_kv4", "bf16_kv4"])
+    Hkv = rng.choice([1, 2, 4, 8])
+    G = rng.choice([1, 2, 3, 4, 4, 8])
+    B = spread(1, 64)
+    T = rng.choice([1, 1, 1, 2, 5, 8]) if op in ("attend", "append") else 1
+    c = dict(op=op, dtype=dtype, B=B, Hq=G * Hkv, Hkv=Hkv, d=rng.choice([64, 128, 128]), T=T, slack=spread(T, 300), skew=rng.random() < 0.7,
+             weights=rng.random() < 0.7, keep=rng.choice([0, 8, 32]) if op == "evict" else 0, shape=rng.randrange(1 << 30))
+    row = _row_bytes(c) + 30 if op in ("attend", "append") else 4 * (_row_bytes(c) + 30) + 8 * c["d"]
+    c["avg"] = spread(1, max(2, min(80000, int(MOST_BYTES / (row * B * Hkv)) - c["slack"])))
+    return c
+
+
+def _shape(c):
+    """(capacities per head, rows in use per segment, room per segment): of the case alone."""
+    r = random.Random(c["shape"])
+    B, Hkv, avg = c["B"], c["Hkv"], c["avg"]
+    if c["skew"]:
+        fixed = avg // 4
+        share = [r.betavariate(0.5, 5) + 1e-3 for _ in range(Hkv)]
+        caps = [max(1, fixed + int((avg - fixed) * Hkv * x / sum(share))) for x in share]
+    else:
+        caps = [avg] * Hkv
+    lens, rooms = [], []
+    for _ in range(B):
+        grown = r.randint(c["T"], c["slack"])
+        for h in range(Hkv):
+            lens.append(caps[h] if c["op"] == "fill" else caps[h] + grown)
+            rooms.append(caps[h] + c["slack"] + (c["T"] if c["op"] == "append" else 0))
+    return caps, lens, rooms
+
+
+def _offsets(counts):
+    out = [0]
+    for n in counts:
+        out.append(out[-1] + n)
+    return out
+
+
+def _row_bytes(c):
+    """K and V of one row of one head, in the cache."""
+    d = c["d"]
+    return 2 * {"f32": 4 * d, "bf16": 2 * d, "f16": 2 * d, "bf16_kv8": d, "bf16_kv4": d // 2 + d // BLOCK}[c["dtype"]]
+
+
+def work(c):
+    caps, lens, _ = _shape(c)
+    S, G, T, d, n = len(lens), c["Hq"] // c["Hkv"], c["T"], c["d"], sum(lens)
+    wide = 2 * d * (4 if c["dtype"] == "f32" else 2)          # K and V of one row, as values
+    row = _row_bytes(c)
+    narrow = c["dtype"] in ("bf16_kv8", "bf16_kv4")
+    if c["op"] == "attend":
+        out = S * G * T * (wide + 4) + (8 * n if c["weights"] else 0)      # q, out and lse; the weights read and written
+        return {"bytes": n * row + out, "flops": 4 * d * G * T * n}
+    if c["op"] in ("fill", "append"):
+        rows = n if c["op"] == "fill" else S * T
+        return {"bytes": rows * (2 * wide + 2 * row + 20), "flops": 2 * d * rows}   # read, written; read back, with positions, weights
+    kept = sum(min(m, max(caps[s % c["Hkv"]], c["keep"])) for s, m in enumerate(lens))
+    return {"bytes": 4 * n + kept * (2 * row + 20 + (row + wide if narrow else 0)), "flops": n}
+
+
+# ---------------------------------------------------------------- the 4-bit and 8-bit values
+
+def _to_fp4(x):
+    """[..., d] values -> (codes uint8 [..., d/2], two values a byte, the first in the low half; exponents uint8 [..., d/32]).
+    The exponent of a block is the smallest at which its largest magnitude is at most 7, half a step above the format's 6."""
+    x = x.float()
+    b = x.reshape(x.shape[:-1] + (x.shape[-1] // BLOCK, BLOCK))
+    top = b.abs().amax(-1)
+    m, e = torch.frexp(top)                                     # top = m 2^e, m in [0.5, 1): at most 7/8 of 2^e needs 2^(e-3)
+    e = torch.where(m <= 0.875, e - 3, e - 2).clamp(-127, 127)
+    e = torch.where(top > 0, e, torch.full_like(e, -127))
+    a = torch.ldexp(b.double(), -e[..., None]).abs()            # exact
+    # midpoints go to the even code: 0.25 -> 0, 0.75 -> 1, 1.25 -> 1, 1.75 -> 2, 2.5 -> 2, 3.5 -> 4, 5 -> 4
+    code = ((a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)).to(torch.uint8)
+    code = (code | (torch.signbit(b).to(torch.uint8) << 3)).reshape(x.shape)
+    return code[..., 0::2] | (code[..., 1::2] << 4), (e + 127).to(torch.uint8)
+
+
+def _from_fp4(codes, exps):
+    """The values as float32."""
+    table = torch.tensor(E2M1 + tuple(-v for v in E2M1), dtype=torch.float32, device=codes.device)
+    v = table[torch.stack((codes & 15, codes >> 4), -1).reshape(codes.shape[:-1] + (-1,)).long()]
+    b = v.reshape(v.shape[:-1] + (-1, BLOCK))
+    return torch.ldexp(b, (exps.int() - 127)[..., None]).reshape(v.shape)
+
+
+def _to_fp8(x):
+    return x.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def _narrow(c, x):
+    """Values -> (the cache's array, its exponents or None)."""
+    if c["dtype"] == "bf16_kv4":
+        return _to_fp4(x)
+    return (_to_fp8(x) if c["dtype"] == "bf16_kv8" else x), None
+
+
+def _wide(c, x, e):
+    """The cache's array -> float32 values."""
+    if c["dtype"] == "bf16_kv4":
+        return _from_fp4(x, e)
+    return x.view(torch.float8_e4m3fn).float() if c["dtype"] == "bf16_kv8" else x.float()
+
+
+# ---------------------------------------------------------------- what a program has in hand
+
+def _inputs(c, seed):
+    """Tensors of one case, from the seed."""
+    dev = "cuda" if torch.cuda.is_available() else "cpu"
+    g = torch.Generator(device=dev).manual_seed(seed)
+    B, Hq, Hkv, T, d = c["B"], c["Hq"], c["Hkv"], c["T"], c["d"]
+    caps, lens, rooms = _shape(c)
+    S, rows = len(lens), sum(rooms)
+    qt = QUERY[c["dtype"]]
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device=dev)
+
+    channel = torch.exp(0.5 * normal(d))          # keys have a few large channels; queries meet them the other way round
+    s = dict(case=c, offsets=_offsets(rooms), lens=lens, caps=caps, start=torch.tensor(_offsets(rooms)[:-1], device=dev),
+             lengths=torch.tensor(lens, dtype=torch.int32, device=dev))
+    s["pos"] = torch.arange(rows, dtype=torch.int32, device=dev) * 3 + 1
+    s["weight"] = torch.rand(rows, generator=g, device=dev).pow_(8) * 50       # few rows have got much of it
+    if c["op"] == "fill":
+        n = sum(lens)
+        s["src"] = _offsets(lens)
+        s["src_start"] = torch.tensor(s["src"][:-1], device=dev)
+        s["src_pos"] = torch.arange(n, dtype=torch.int32, device=dev) * 2
+        s["k_rows"], s["v_rows"] = (normal(n, d) * channel).to(qt), normal(n, d).to(qt)
+    else:
+        s["k"], s["k_scale"] = _narrow(c, (normal(rows, d) * channel).to(qt))
+        s["v"], s["v_scale"] = _narrow(c, normal(rows, d).to(qt))
+    if c["op"] == "attend":
+        s["q"] = (normal(B, Hq, T, d) * 2 / channel).to(qt)
+    if c["op"] == "append":
+        s["k_new"], s["v_new"] = (normal(B, Hkv, T, d) * channel).to(qt), normal(B, Hkv, T, d).to(qt)
+        s["pos_new"] = (torch.arange(T, device=dev, dtype=torch.int32)[None] + 100000).repeat(B, 1)
+        s["last"] = [i * T for i in range(S + 1)]
+    if c["op"] == "evict":
+        kept = [min(n, max(caps[i % Hkv], c["keep"])) for i, n in enumerate(lens)]
+        s["out_offsets"] = _offsets(kept)
+        s["out_start"] = torch.tensor(s["out_offsets"][:-1], device=dev)
+        s["cap"] = torch.tensor([max(caps[i % Hkv], c["keep"]) for i in range(S)], device=dev)
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    if own:
+        from paper_2508_15806_amd import api
+        c = s["case"]
+        shape = (c["dtype"], c["B"], c["Hq"], c["Hkv"], c["d"])
+        if c["op"] == "fill":
+            s["cache"] = api.Cache(*shape, s["offsets"])
+        else:
+            s["cache"] = api.Cache(*shape, s["offsets"], k=s["k"], v=s["v"], k_scale=s["k_scale"], v_scale=s["v_scale"],
+                                   lengths=s["lengths"].clone(), pos=s["pos"], weight=s["weight"])
+        if c["op"] == "evict":
+            s["kept"] = api.Cache(*shape, s["out_offsets"])
+            s["kept_idx"] = torch.empty(max(1, s["out_offsets"][-1]), dtype=torch.int32, device=s["lengths"].device)
+        if c["op"] == "attend":
+            s["sums"] = s["weight"].clone()
+    return s
+
+
+def run(s):
+    op = s["case"]["op"]
+    if op == "attend":
+        return _own_attend(s) if own else _attend(s)
+    if op == "fill":
+        return _own_fill(s) if own else _fill(s)
+    if op == "append":
+        return _own_append(s) if own else _append(s)
+    return _own_evict(s) if own else _evict(s)
+
+
+# ---------------------------------------------------------------- the framework's calls
+
+def _own_attend(s):
+    if s["case"]["weights"]:
+        out, lse = s["cache"].attend(s["q"], weight=s["sums"])
+        return {"out": out, "lse": lse, "weight": s["sums"]}
+    out, lse = s["cache"].attend(s["q"], weight=False)
+    return {"out": out, "lse": lse}
+
+
+def _own_fill(s):
+    s["cache"].fill(s["k_rows"], s["v_rows"], s["src"], s["src_pos"])
+    k, v, pos = s["cache"].rows(s["src"])
+    return {"k": k, "v": v, "pos": pos, "lengths": s["cache"].lengths}
+
+
+def _own_append(s):
+    s["cache"].append(s["k_new"], s["v_new"], s["pos_new"], at=s["lengths"])
+    k, v, pos = s["cache"].rows(s["last"])
+    return {"k": k, "v": v, "pos": pos, "lengths": s["cache"].lengths}
+
+
+def _own_evict(s):
+    kept = s["kept"]
+    s["cache"].evict(s["caps"], s["case"]["keep"], kept, s["kept_idx"])
+    k, v, pos = kept.rows(s["out_offsets"]) if s["case"]["dtype"] in ("bf16_kv8", "bf16_kv4") else (kept.k, kept.v, kept.pos)
+    return {"k": k, "v": v, "pos": pos, "weight": kept.weight, "idx": s["kept_idx"], "lengths": kept.lengths}
+
+
+# ---------------------------------------------------------------- the plain forms
+
+def _rows_of(start, count, most):
+    """Row numbers [S, most] of segments that begin at `start`, and which of them exist."""
+    j = torch.arange(most, device=start.device)
+    there = j[None] < count[:, None]
+    return torch.where(there, start[:, None] + j[None], 0), there
+
+
+def _attend(s):
+    c = s["case"]
+    B, Hq, Hkv, T, d = c["B"], c["Hq"], c["Hkv"], c["T"], c["d"]
+    S, R = B * Hkv, Hq // Hkv * T
+    at, there = _rows_of(s["start"], s["lengths"], max(s["lens"]))
+    take = [None if x is None else x[at] for x in (s["k"], s["k_scale"], s["v"], s["v_scale"])]
+    q = s["q"].float().reshape(S, R, d)
+    logit = torch.bmm(_wide(c, take[0], take[1]), q.transpose(1, 2).contiguous()) / math.sqrt(d)      # [S, rows, R]
+    # query t of the T latest sees the rows up to its own
+    t = torch.arange(R, device=q.device) % T
+    j = torch.arange(at.shape[1], device=q.device)
+    sees = j[None, :, None] < (s["lengths"][:, None, None] - (T - 1) + t[None, None])
+    logit = logit.masked_fill(~sees, -math.inf)
+    top = logit.amax(1, keepdim=True)
+    p = torch.exp(logit - torch.where(top == -math.inf, 0.0, top))
+    total = p.sum(1, keepdim=True)
+    lse = torch.where(total > 0, top + torch.log(total), -math.inf)
+    p = p / torch.where(total > 0, total, 1.0)
+    out = torch.bmm(p.transpose(1, 2).contiguous(), _wide(c, take[2], take[3]))
+    r = {"out": out.reshape(B, Hq, T, d).to(s["q"].dtype), "lse": lse.reshape(B, Hq, T)}
+    if c["weights"]:
+        r["weight"] = s["weight"].clone()
+        r["weight"][at[there]] += p.sum(2)[there]
+    return r
+
+
+def _fill(s):
+    c = s["case"]
+    return {"k": _wide(c, *_narrow(c, s["k_rows"])).to(s["k_rows"].dtype), "v": _wide(c, *_narrow(c, s["v_rows"])).to(s["k_rows"].dtype),
+            "pos": s["src_pos"].clone(), "lengths": s["lengths"].clone()}
+
+
+def _append(s):
+    c = s["case"]
+    T, d = c["T"], c["d"]
+    at = (s["start"] + s["lengths"])[:, None] + torch.arange(T, device=s["start"].device)
+    at = at.reshape(-1)
+    (k, ke), (v, ve) = _narrow(c, s["k_new"].reshape(-1, d)), _narrow(c, s["v_new"].reshape(-1, d))
+    s["k"][at], s["v"][at] = k, v
+    if ke is not None:
+        s["k_scale"][at], s["v_scale"][at] = ke, ve
+    s["pos"][at] = s["pos_new"].repeat_interleave(c["Hkv"], 0).reshape(-1)
+    s["weight"][at] = 0.0
+    read = [_wide(c, x[at], None if e is None else e[at]).to(s["k_new"].dtype) for x, e in ((s["k"], s["k_scale"]), (s["v"], s["v_scale"]))]
+    return {"k": read[0], "v": read[1], "pos": s["pos"][at], "lengths": s["lengths"] + T}
+
+
+def _evict(s):
+    c = s["case"]
+    keep = c["keep"]
+    at, there = _rows_of(s["start"], s["lengths"], max(s["lens"]))
+    n = s["lengths"].long()[:, None]
+    j = torch.arange(at.shape[1], device=at.device)[None]
+    ranked = there & (j < n - keep)
+    w = torch.where(ranked, s["weight"][at], -math.inf)
+    order = torch.sort(w, dim=1, descending=True, stable=True).indices       # equal weights: the lower row first
+    rank = torch.empty_like(order).scatter_(1, order, j.expand_as(order))
+    stays = there & ((j >= n - keep) | (rank < s["cap"][:, None] - keep) | (n <= s["cap"][:, None]))
+    lengths = stays.sum(1)
+    idx = j.expand_as(at)[stays]
+    row = at[stays]
+    k, v = ((x[row] if c["dtype"] in ("f32", "bf16", "f16") else _wide(c, x[row], None if e is None else e[row]).to(torch.bfloat16))
+            for x, e in ((s["k"], s["k_scale"]), (s["v"], s["v_scale"])))
+    return {"k": k, "v": v, "pos": s["pos"][row], "weight": s["weight"][row], "idx": idx.int(), "lengths": lengths.int()}
+
+
+# ---------------------------------------------------------------- from the definition, in 64 bits
+
+def _value4(codes, exps):
+    mag = codes & 7                                     # E2M1: 1 exponent-free step of 0.5, then (1 + m/2) 2^(e-1)
+    e, m = (mag >> 1).double(), (mag & 1).double()
+    v = torch.where(e > 0, (1 + m / 2) * 2.0 ** (e - 1), m / 2)
+    return torch.where(codes >= 8, -v, v) * 2.0 ** (exps.double() - 127)
+
+
+def _value64(c, x, e):
+    if c["dtype"] == "bf16_kv4":
+        codes = torch.stack((x % 16, x // 16), 2).flatten(1)
+        return _value4(codes, e.repeat_interleave(BLOCK, 1))
+    return (x.view(torch.float8_e4m3fn) if c["dtype"] == "bf16_kv8" else x).double()
+
+
+def _nearest64(c, x):
+    """Values as the cache holds them, from the nearest of all values that its type has (a block's exponent first)."""
+    x = x.double()
+    if c["dtype"] == "bf16_kv4":
+        b = x.reshape(-1, BLOCK)
+        top = b.abs().amax(1)
+        e = torch.full_like(top, -127.0)
+        for k in range(-126, 128):
+            e = torch.where(top > 7 * 2.0 ** (k - 1), float(k), e)
+        grid, scale = torch.tensor(E2M1, dtype=torch.float64, device=x.device), 2.0 ** e[:, None]
+    elif c["dtype"] == "bf16_kv8":
+        b, scale = x.reshape(-1, BLOCK), 1.0
+        grid = torch.arange(127, dtype=torch.uint8, device=x.device).view(torch.float8_e4m3fn).double()
+    else:
+        return x
+    a = (b.abs() / scale).clamp(max=float(grid[-1]))
+    hi = torch.searchsorted(grid, a.contiguous()).clamp(max=len(grid) - 1)
+    lo = (hi - 1).clamp(min=0)
+    up = (grid[hi] - a < a - grid[lo]) | ((grid[hi] - a == a - grid[lo]) & (hi % 2 == 0))
+    return (torch.where(up, grid[hi], grid[lo]) * scale * torch.where(b < 0, -1.0, 1.0)).reshape(x.shape)
+
+
+def exact(case, seed):
+    s = _inputs(case, seed)
+    c = s["case"]
+    B, Hq, Hkv, T, d = c["B"], c["Hq"], c["Hkv"], c["T"], c["d"]
+    G = Hq // Hkv
+    dev = s["lengths"].device
+    if c["op"] in ("fill", "append"):
+        k, v = (s["k_rows"], s["v_rows"]) if c["op"] == "fill" else (s["k_new"].reshape(-1, d), s["v_new"].reshape(-1, d))
+        return {"k": _nearest64(c, k), "v": _nearest64(c, v), "pos": None, "lengths": None}
+    if c["op"] == "evict":
+        rows = []
+        for i, n in enumerate(s["lens"]):
+            room = max(s["caps"][i % Hkv], c["keep"])
+            if n > room:
+                w = s["weight"][s["offsets"][i]:s["offsets"][i] + n - c["keep"]].double()
+                # as many as there are places, from the largest down, the lower row first among equal ones
+                first = (-w).argsort(stable=True)[:room - c["keep"]].sort().values
+                rows.append(torch.cat((first, torch.arange(n - c["keep"], n, device=dev))) + s["offsets"][i])
+            else:
+                rows.append(torch.arange(n, device=dev) + s["offsets"][i])
+        row = torch.cat(rows)
+        return {"k": _value64(c, s["k"][row], s["k_scale"][row] if s["k_scale"] is not None else None),
+                "v": _value64(c, s["v"][row], s["v_scale"][row] if s["v_scale"] is not None else None),
+                "pos": None, "weight": s["weight"][row].double(), "idx": None, "lengths": None}
+    out = torch.zeros(B, Hq, T, d, dtype=torch.float64, device=dev)
+    lse = torch.full((B, Hq, T), -math.inf, dtype=torch.float64, device=dev)
+    weight = s["weight"].double()
+    for i, n in enumerate(s["lens"]):
+        a = s["offsets"][i]
+        k = _value64(c, s["k"][a:a + n], s["k_scale"][a:a + n] if s["k_scale"] is not None else None)
+        v = _value64(c, s["v"][a:a + n], s["v_scale"][a:a + n] if s["v_scale"] is not None else None)
+        b, h = divmod(i, Hkv)
+        for t in range(T):
+            m = n - T + 1 + t                                   # rows that this query sees
+            if m <= 0:
+                continue
+            x = (s["q"][b, h * G:(h + 1) * G, t].double() @ k[:m].t()) / d ** 0.5
+            p = torch.softmax(x, 1)
+            out[b, h * G:(h + 1) * G, t] = p @ v[:m]
+            lse[b, h * G:(h + 1) * G, t] = torch.logsumexp(x, 1)
+            weight[a:a + m] += p.sum(0)
+    return {"out": out, "lse": lse, "weight": weight} if c["weights"] else {"out": out, "lse": lse}
