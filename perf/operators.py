@@ -17,6 +17,7 @@ keys.  The lengths belong to the case, the values to the seed.
 import math
 import random
 
+import numpy as np
 import torch
 
 own = False
@@ -98,10 +99,7 @@ def _shape(c):
 
 
 def _offsets(counts):
-    out = [0]
-    for n in counts:
-        out.append(out[-1] + n)
-    return out
+    return np.concatenate(([0], np.cumsum(counts))).astype(np.int64)
 
 
 def _row_bytes(c):
@@ -185,14 +183,13 @@ def _inputs(c, seed):
         return torch.randn(shape, generator=g, device=dev)
 
     channel = torch.exp(0.5 * normal(d))          # keys have a few large channels; queries meet them the other way round
-    s = dict(case=c, offsets=_offsets(rooms), lens=lens, caps=caps, start=torch.tensor(_offsets(rooms)[:-1], device=dev),
+    s = dict(case=c, offsets=_offsets(rooms), lens=lens, caps=np.array(caps, dtype=np.int32), start=torch.from_numpy(_offsets(rooms)[:-1]).to(dev),
              lengths=torch.tensor(lens, dtype=torch.int32, device=dev))
     s["pos"] = torch.arange(rows, dtype=torch.int32, device=dev) * 3 + 1
     s["weight"] = torch.rand(rows, generator=g, device=dev).pow_(8) * 50       # few rows have got much of it
     if c["op"] == "fill":
         n = sum(lens)
         s["src"] = _offsets(lens)
-        s["src_start"] = torch.tensor(s["src"][:-1], device=dev)
         s["src_pos"] = torch.arange(n, dtype=torch.int32, device=dev) * 2
         s["k_rows"], s["v_rows"] = (normal(n, d) * channel).to(qt), normal(n, d).to(qt)
     else:
@@ -203,11 +200,10 @@ def _inputs(c, seed):
     if c["op"] == "append":
         s["k_new"], s["v_new"] = (normal(B, Hkv, T, d) * channel).to(qt), normal(B, Hkv, T, d).to(qt)
         s["pos_new"] = (torch.arange(T, device=dev, dtype=torch.int32)[None] + 100000).repeat(B, 1)
-        s["last"] = [i * T for i in range(S + 1)]
+        s["last"] = _offsets([T] * S)
     if c["op"] == "evict":
         kept = [min(n, max(caps[i % Hkv], c["keep"])) for i, n in enumerate(lens)]
         s["out_offsets"] = _offsets(kept)
-        s["out_start"] = torch.tensor(s["out_offsets"][:-1], device=dev)
         s["cap"] = torch.tensor([max(caps[i % Hkv], c["keep"]) for i in range(S)], device=dev)
     return s
 
@@ -225,7 +221,7 @@ def prepare(case, seed):
                                    lengths=s["lengths"].clone(), pos=s["pos"], weight=s["weight"])
         if c["op"] == "evict":
             s["kept"] = api.Cache(*shape, s["out_offsets"])
-            s["kept_idx"] = torch.empty(max(1, s["out_offsets"][-1]), dtype=torch.int32, device=s["lengths"].device)
+            s["kept_idx"] = torch.empty(int(s["out_offsets"][-1]), dtype=torch.int32, device=s["lengths"].device)
         if c["op"] == "attend":
             s["sums"] = s["weight"].clone()
     return s
@@ -396,14 +392,15 @@ def exact(case, seed):
     if c["op"] == "evict":
         rows = []
         for i, n in enumerate(s["lens"]):
-            room = max(s["caps"][i % Hkv], c["keep"])
+            a = int(s["offsets"][i])
+            room = max(int(s["caps"][i % Hkv]), c["keep"])
             if n > room:
-                w = s["weight"][s["offsets"][i]:s["offsets"][i] + n - c["keep"]].double()
+                w = s["weight"][a:a + n - c["keep"]].double()
                 # as many as there are places, from the largest down, the lower row first among equal ones
                 first = (-w).argsort(stable=True)[:room - c["keep"]].sort().values
-                rows.append(torch.cat((first, torch.arange(n - c["keep"], n, device=dev))) + s["offsets"][i])
+                rows.append(torch.cat((first, torch.arange(n - c["keep"], n, device=dev))) + a)
             else:
-                rows.append(torch.arange(n, device=dev) + s["offsets"][i])
+                rows.append(torch.arange(n, device=dev) + a)
         row = torch.cat(rows)
         return {"k": _value64(c, s["k"][row], s["k_scale"][row] if s["k_scale"] is not None else None),
                 "v": _value64(c, s["v"][row], s["v_scale"][row] if s["v_scale"] is not None else None),
@@ -412,7 +409,7 @@ def exact(case, seed):
     lse = torch.full((B, Hq, T), -math.inf, dtype=torch.float64, device=dev)
     weight = s["weight"].double()
     for i, n in enumerate(s["lens"]):
-        a = s["offsets"][i]
+        a = int(s["offsets"][i])
         k = _value64(c, s["k"][a:a + n], s["k_scale"][a:a + n] if s["k_scale"] is not None else None)
         v = _value64(c, s["v"][a:a + n], s["v_scale"][a:a + n] if s["v_scale"] is not None else None)
         b, h = divmod(i, Hkv)
