@@ -13,6 +13,11 @@
  *     within the capacity plus the whole window                      -> slkv_compress_layer
  *     The same selection on a cache that is already compacted and has grown during generation
  *     (heads of different lengths)                                   -> slkv_recompress_layer
+ *   Decoding on the compacted cache (the paper's Section 3.4 generates on it; the operators are
+ *     standard ones): rows enter it, narrowed to 8 or 4 bits if asked for -> slkv_fill_cache,
+ *     slkv_append_cache; the next tokens attend to it                -> slkv_attend_cache
+ *     rows with the least accumulated attention weight leave it      -> slkv_evict_cache
+ *     rows come back as 16-bit values                                -> slkv_cache_rows
  *
  * Conventions
  *   - Pointers named d_* are DEVICE pointers, h_* are HOST pointers.  The caller owns every
@@ -50,8 +55,11 @@ typedef enum {
 
 /* Element type of Q, K and V.  SLKV_BF16_KV_FP8: queries bfloat16, keys and values 8-bit floating
  * point in the OCP E4M3 encoding (1 sign, 4 exponent bits with bias 7, 3 mantissa bits, subnormals,
- * no infinities, S.1111.111 = NaN), one byte per element; strides of d_k / d_v count bytes then. */
-typedef enum { SLKV_F32 = 0, SLKV_BF16 = 1, SLKV_F16 = 2, SLKV_BF16_KV_FP8 = 3 } slkv_dtype;
+ * no infinities, S.1111.111 = NaN), one byte per element; strides of d_k / d_v count bytes then.
+ * SLKV_BF16_KV_MXFP4 (the slkv_*_cache calls alone): queries bfloat16, keys and values 4-bit floating point in the OCP
+ * microscaling format: E2M1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the first in the low half;
+ * every 32 neighbouring elements of a row share a byte e that multiplies them by 2^(e - 127), 255 = NaN. */
+typedef enum { SLKV_F32 = 0, SLKV_BF16 = 1, SLKV_F16 = 2, SLKV_BF16_KV_FP8 = 3, SLKV_BF16_KV_MXFP4 = 4 } slkv_dtype;
 typedef enum { SLKV_POOL_NONE = 0, SLKV_POOL_MAX = 1, SLKV_POOL_AVG = 2 } slkv_pool;
 typedef enum { SLKV_BUDGET_EXACT = 0, SLKV_BUDGET_PAPER_LITERAL = 1, SLKV_BUDGET_EXACT_PER_QUERY_HEAD = 2 } slkv_budget_mode;
 
@@ -312,6 +320,95 @@ slkv_status slkv_recompress_layer(const slkv_ragged_desc* desc, const void* d_qw
                                   float* d_importance, float* d_pooled, int64_t out_capacity_rows,
                                   void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ------------------------------------------------------------------ decoding on a compacted cache
+ * A cache holds rows of K and V for S = B*Hkv segments s = b*Hkv + h (as slkv_compress_layer leaves them, with room to
+ * grow): segment s owns the rows h_offsets[s] .. h_offsets[s+1] of the packed arrays, its room, of which the first
+ * d_lengths[s] are in use, oldest first.  The lengths live on the device, so that a recorded HIP graph that appends,
+ * attends and evicts replays on a cache that has grown since; what a call reads of them is bounded by the room whatever they hold
+ * (below 0 counts as 0, above the room as the room).  Rows that are not in use are neither read as keys or values nor changed.
+ * The rooms may total 2^31 - 1 rows, one of them 2^30; addresses are 64-bit.
+ */
+typedef struct {
+  uint32_t struct_size;        /* sizeof(slkv_cache_desc) */
+  int32_t dtype;               /* slkv_dtype */
+  int32_t B, Hq, Hkv, d;       /* d in {64, 128}; Hq % Hkv == 0 */
+  int32_t reserved[2];         /* 0 */
+  const int64_t* h_offsets;    /* [B*Hkv+1] host: rooms, non-decreasing, >= 0, last < 2^31 */
+} slkv_cache_desc;
+
+typedef struct {
+  uint32_t struct_size;        /* sizeof(slkv_cache) */
+  uint32_t reserved;           /* 0 */
+  void *d_k, *d_v;             /* [rows][d] elements; MXFP4: [rows][d/2] bytes */
+  void *d_k_scale, *d_v_scale; /* MXFP4: [rows][d/32] bytes; NULL otherwise */
+  int32_t* d_lengths;          /* [B*Hkv] rows in use; NULL: every room is full (not where a call writes them) */
+  int32_t* d_pos;              /* [rows] original token positions, may be NULL */
+  float* d_weight;             /* [rows] attention weight accumulated by each row, may be NULL */
+} slkv_cache;
+
+/* The rows that a prefill kept become the cache: segment s gets the source rows h_src_offsets[s] .. h_src_offsets[s+1]
+ * (h_out_offsets of slkv_compress_layer) and that many in use; weights 0.
+ * d_k_rows, d_v_rows [rows][d] in the type of the queries: copied, or narrowed to
+ *   E4M3: to the nearest value, ties to the even code; finite values beyond 448 become 448, infinities and NaN become NaN;
+ *   MXFP4: the exponent of a block of 32 is the smallest, not below -127, at which its largest magnitude is at most 7 (half
+ *     a step above 6); elements go to the nearest value, ties to the even code, beyond 6 to 6; a block with an infinity or
+ *     NaN is a block of NaN.
+ * d_pos_rows [rows] int32 (d_kept_idx of slkv_compress_layer), may be NULL: the cache's positions stay as they are then.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED, CAPACITY (a segment's rows exceed its room), HIP. */
+slkv_status slkv_fill_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const int64_t* h_src_offsets,
+                            const void* d_k_rows, const void* d_v_rows, const int32_t* d_pos_rows, void* hip_stream);
+
+/* T rows of every segment enter behind those in use, converted as by slkv_fill_cache, with weight 0; d_lengths grows by T.
+ * Element (b, h, t, :) of d_k at b*k_stride[0] + h*k_stride[1] + t*k_stride[2], rows of d elements contiguous, strides
+ * multiples of 16 bytes, >= 0; the same for d_v.  d_pos [B][T] int32, may be NULL.  1 <= T <= 64.
+ * d_at [B*Hkv] int32, may be NULL (d_lengths): the rows enter behind the first d_at[s] instead, and the new length is d_at[s] + T.
+ * It may be d_lengths itself.  Rows that the room does not hold are left out, and the length is the room then.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED, HIP. */
+slkv_status slkv_append_cache(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, const void* d_k, const void* d_v,
+                              const int64_t k_stride[3], const int64_t v_stride[3], const int32_t* d_pos, const int32_t* d_at,
+                              void* hip_stream);
+
+/* The latest rows as values: segment s gives its latest c_s = h_out_offsets[s+1] - h_out_offsets[s] rows (all it has, if they
+ * are fewer) to the rows from h_out_offsets[s] on of d_k_rows, d_v_rows [..][d] in the type of the queries (E4M3 and MXFP4
+ * values are bfloat16 values; MXFP4 values of 2^128 and more become infinite) and d_pos_rows (NULL, or int32; needs cache->d_pos).  Output rows without a cache row are left as they were.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED, HIP. */
+slkv_status slkv_cache_rows(const slkv_cache_desc* desc, const slkv_cache* cache, const int64_t* h_out_offsets,
+                            void* d_k_rows, void* d_v_rows, int32_t* d_pos_rows, void* hip_stream);
+
+/* Attention of the T latest tokens' queries (their rows are in the cache already) over the rows in use.  Query t of query
+ * head hq sees the first n_s - T + 1 + t rows of segment (b, hq / (Hq/Hkv)); with x_j = q . k_j / sqrt(d) over these,
+ *   lse = ln sum_j exp(x_j),  out = sum_j exp(x_j - lse) v_j,
+ *   weight_out[j] = weight[j] + sum over the queries of the segment that see j of exp(x_j - lse)   for j < n_s.
+ * A query that sees no row: out 0, lse -infinity, nothing added.  Infinities and NaN in rows that a query does not see do not
+ * reach it.  Products are exact, sums, softmax and weights fp32; out is rounded once.  The result does not depend on
+ * what else runs, and has the same bits every time.
+ * d_q   [B][Hq][T][d] (device, read only); T >= 1, (Hq/Hkv)*T <= 64
+ * d_out [B][Hq][T][d] in the type of the queries;  d_lse [B][Hq][T] fp32, may be NULL
+ * d_weight_out [rows] fp32 or NULL; may be cache->d_weight itself.  cache->d_weight NULL: sums begin at 0.
+ * Workspace: slkv_attend_workspace_bytes (want_weights: d_weight_out is given), scratch alone: need not be cleared; two
+ * calls that may overlap in time need one each.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED ((Hq/Hkv)*T), WORKSPACE, HIP. */
+slkv_status slkv_attend_workspace_bytes(const slkv_cache_desc* desc, int32_t T, int32_t want_weights, size_t* bytes);
+slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, const void* d_q, void* d_out,
+                              float* d_lse, float* d_weight_out, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Eviction by accumulated attention weight.  Segment s with n_s rows in use and capacity C_h:
+ *   n_s <= max(C_h, w): every row stays;
+ *   otherwise the max(C_h, w) - w rows of the first n_s - w that have the largest weight (equal weights rank by lower row, a NaN
+ *   above all numbers), in ascending order, followed by the last w.
+ * Their K, V (bit for bit), scales, positions and weights go to the segment's first rows of another cache `out`, whose
+ * desc has the same dtype, B, Hq, Hkv, d and whose rooms hold min(room, max(C_h, w)) rows at least; out->d_lengths gets the counts.
+ * w         >= 0: latest rows that always stay;  h_budgets [Hkv] host: C_h >= 0
+ * out       out->d_lengths is required; d_pos and d_weight are carried where both caches have them.  No array of `out` may
+ *           overlap one of `cache` (d_lengths may be the same array).
+ * d_kept_idx [rows of out] int32, may be NULL: the kept rows' numbers inside their segment, at the places of the rows of `out`
+ * cache->d_weight is required.  Workspace: slkv_evict_workspace_bytes, scratch alone as above.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED, WORKSPACE, CAPACITY (a room of out), HIP. */
+slkv_status slkv_evict_workspace_bytes(const slkv_cache_desc* desc, const slkv_cache_desc* out_desc, int32_t w, const int32_t* h_budgets, size_t* bytes);
+slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const slkv_cache_desc* out_desc, const slkv_cache* out,
+                             int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx,
+                             void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ------------------------------------------------------------------ kernel timing -----
  * Optional instrumentation for benchmarks: between slkv_profile_begin and slkv_profile_end
  * every kernel the library launches is bracketed by a HIP event pair on the call's stream.
@@ -334,7 +431,12 @@ typedef enum {
   SLKV_K_ROW_CELLS = 5,     /* Stage 1: per-row weight cells */
   SLKV_K_HEAD_REDUCE = 6,   /* Stage 1: per-head sums and scores */
   SLKV_K_QK_CELLS = 7,      /* Stage 1 from queries and keys: logits, top-K and cells of every row */
-  SLKV_K_QK_FALLBACK = 8    /* the same for rows whose candidate list overflowed */
+  SLKV_K_QK_FALLBACK = 8,   /* the same for rows whose candidate list overflowed */
+  SLKV_K_CACHE_STORE = 9,   /* rows into a cache: fill and append */
+  SLKV_K_CACHE_ROWS = 10,   /* rows out of a cache */
+  SLKV_K_ATTEND = 11,       /* attention over a cache */
+  SLKV_K_ATTEND_JOIN = 12,  /* the parts of split segments joined; weights */
+  SLKV_K_EVICT = 13         /* eviction: selection and copy */
 } slkv_kernel_id;
 typedef struct {
   int32_t kernel; /* slkv_kernel_id */

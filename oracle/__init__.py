@@ -12,6 +12,8 @@ Modules
   budgets   - Stage 2a: per-head capacities (Eq. 6, Algorithm 2).
   behavior  - Stage 1: WO / WD / WS counting and SF / LG / INF scores
               (Algorithm 1).
+  decode    - decoding on the compacted cache: 8- and 4-bit values, attention,
+              eviction by accumulated weight.
 
 Every function here is pinned by tests that do not call back into it (closed
 forms, brute force on tiny inputs, library routines, hand-worked examples from

@@ -1,6 +1,8 @@
 """Convenience layer over binding.py: uploads host arrays, allocates outputs and
 workspace with torch, calls the library.  No arithmetic of the method lives here."""
 
+import contextlib
+
 import numpy as np
 import torch
 
@@ -11,6 +13,8 @@ from . import binding as B
 DTYPES = {"f32": (B.SLKV_F32, torch.float32, torch.float32), "bf16": (B.SLKV_BF16, torch.bfloat16, torch.bfloat16),
           "f16": (B.SLKV_F16, torch.float16, torch.float16),
           "bf16_kv8": (B.SLKV_BF16_KV_FP8, torch.bfloat16, torch.uint8)}   # E4M3 bytes travel as uint8
+# types of a cache (Cache): these, and 4 bits, whose bytes hold two E2M1 values each, with an exponent byte for every 32 of them
+CACHE_DTYPES = dict(DTYPES, bf16_kv4=(B.SLKV_BF16_KV_MXFP4, torch.bfloat16, torch.uint8))
 
 
 def to_device(arr, dtype, device="cuda"):
@@ -149,3 +153,139 @@ def score_heads_qk(q, k, needle_start, needle_len, topk, acc=None, stream=None):
     ws = torch.empty((B.slkv_score_heads_qk_workspace_bytes(L, Hq, T, n),), dtype=torch.uint8, device=q.device)
     B.slkv_score_heads_qk(q, k, needle_start, needle_len, topk, acc, scores, ws, stream, first)
     return acc, scores
+
+
+class Cache:
+    """One layer's cache for decoding: packed K and V rows in a room per segment (sequence b, KV head h: b * Hkv + h), of which the first
+    lengths[s] are in use.
+
+    `offsets` [B * Hkv + 1]: the rooms.  The arrays are allocated unless they are given (k, v [rows, d], "bf16_kv4": [rows, d / 2] uint8 and
+    k_scale, v_scale [rows, d / 32] uint8; lengths [B * Hkv], pos [rows] int32; weight [rows] fp32); given keys without lengths fill their
+    rooms.  positions, weights = False: a cache without these arrays.  Calls of one object share its workspace, as do replays of graphs
+    that captured them: each waits for the one before it, on whatever stream that was.  Make the first call of a kind outside a capture: it allocates the workspace."""
+
+    def __init__(self, dtype, B_, Hq, Hkv, d, offsets, k=None, v=None, k_scale=None, v_scale=None, lengths=None, pos=None, weight=None,
+                 device="cuda", positions=True, weights=True):
+        code, self.query_dtype, self.row_dtype = CACHE_DTYPES[dtype]
+        self.dtype, self.B, self.Hq, self.Hkv, self.d = dtype, B_, Hq, Hkv, d
+        self.layout = B.CacheLayout(code, B_, Hq, Hkv, d, offsets)
+        offsets = self.layout.offsets
+        rows, S = int(offsets[-1]), B_ * Hkv
+        four = dtype == "bf16_kv4"
+        if (k is None) != (v is None) or (k is not None and four and (k_scale is None or v_scale is None)):
+            raise ValueError("keys, values and their scales are given together")
+        if k is not None:
+            device = k.device
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        if lengths is None:
+            lengths = torch.zeros((S,), dtype=torch.int32, device=self.device) if k is None else torch.from_numpy(np.diff(offsets).astype(np.int32)).to(self.device)
+        width = d // 2 if four else d
+
+        def array(t, shape, tdt, name, make):
+            if t is None:
+                return make(shape, dtype=tdt, device=self.device)
+            return self._tensor(t, shape, tdt, name)
+
+        self.k = array(k, (rows, width), self.row_dtype, "k", torch.empty)
+        self.v = array(v, (rows, width), self.row_dtype, "v", torch.empty)
+        self.k_scale = array(k_scale, (rows, d // 32), torch.uint8, "k_scale", torch.empty) if four else None
+        self.v_scale = array(v_scale, (rows, d // 32), torch.uint8, "v_scale", torch.empty) if four else None
+        self.lengths = self._tensor(lengths, (S,), torch.int32, "lengths")
+        self.pos = array(pos, (rows,), torch.int32, "pos", torch.zeros) if positions or pos is not None else None
+        self.weight = array(weight, (rows,), torch.float32, "weight", torch.zeros) if weights or weight is not None else None
+        self.rows_in_all = rows
+        self._arrays = B.CacheTensors(self.k, self.v, self.k_scale, self.v_scale, self.lengths, self.pos, self.weight)
+        self._workspaces = {}
+
+    def _tensor(self, t, shape, tdt, name, contiguous=True):
+        if t.dtype != tdt or tuple(t.shape) != shape:
+            raise ValueError("%s: %s of shape %s wanted, got %s of shape %s" % (name, tdt, shape, t.dtype, tuple(t.shape)))
+        if t.device != self.device:
+            raise ValueError("%s is on %s, the cache on %s" % (name, t.device, self.device))
+        if contiguous and not t.is_contiguous():
+            raise ValueError("%s is not contiguous" % name)
+        return t
+
+    def _on_device(self):
+        """The cache's device as the current one, where it is not."""
+        return contextlib.nullcontext() if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
+
+    def _workspace(self, key, nbytes):
+        ws = self._workspaces.get(key)
+        if ws is None or ws.numel() < nbytes:
+            ws = self._workspaces[key] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        return ws
+
+    def fill(self, k_rows, v_rows, src_offsets, pos=None, stream=None):
+        """The rows that a prefill kept (LayerCall's k_out, v_out, offsets, kept_idx) become the cache."""
+        rows = int(src_offsets[-1])
+        for t, name in ((k_rows, "k_rows"), (v_rows, "v_rows")):
+            if t.dim() != 2 or t.shape[0] < rows:
+                raise ValueError("%s: at least %d rows wanted, got shape %s" % (name, rows, tuple(t.shape)))
+            self._tensor(t, (t.shape[0], self.d), self.query_dtype, name)
+        if pos is not None:
+            self._tensor(pos, (max(pos.shape[0], rows),), torch.int32, "pos")
+        with self._on_device():
+            B.slkv_fill_cache(self.layout, self._arrays, src_offsets, k_rows, v_rows, pos, stream)
+
+    def append(self, k, v, pos=None, at=None, stream=None):
+        """k, v [B, Hkv, T, d] (any strides, rows contiguous), pos [B, T]: the next T tokens enter behind the rows in use, or behind the first at[s]
+        of them (drafted tokens that were not accepted are overwritten this way)."""
+        shape = (self.B, self.Hkv, k.shape[2] if k.dim() == 4 else 0, self.d)
+        for t, name in ((k, "k"), (v, "v")):
+            if self._tensor(t, shape, self.query_dtype, name, contiguous=False).stride(3) != 1:
+                raise ValueError("%s: rows are not contiguous" % name)
+        if pos is not None:
+            self._tensor(pos, (self.B, shape[2]), torch.int32, "pos")
+        if at is not None:
+            self._tensor(at, (self.B * self.Hkv,), torch.int32, "at")
+        with self._on_device():
+            B.slkv_append_cache(self.layout, self._arrays, k, v, pos, at, stream)
+
+    def attend(self, q, out=None, lse=None, weight=None, stream=None):
+        """q [B, Hq, T, d]: the queries of the T latest tokens, whose rows are in the cache.  Returns (out [B, Hq, T, d], lse [B, Hq, T] fp32).
+        weight: where the cache's weights plus this call's go; None: the cache's own array, if it has one; False: nowhere."""
+        if q.dim() != 4:
+            raise ValueError("q: four dimensions wanted, got shape %s" % (tuple(q.shape),))
+        T = q.shape[2]
+        shape = (self.B, self.Hq, T, self.d)
+        self._tensor(q, shape, self.query_dtype, "q")
+        out = torch.empty(shape, dtype=self.query_dtype, device=self.device) if out is None else self._tensor(out, shape, self.query_dtype, "out")
+        lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
+        if weight is None:
+            weight = self.weight
+        elif weight is False:
+            weight = None
+        else:
+            self._tensor(weight, (self.rows_in_all,), torch.float32, "weight")
+        key = (T, weight is not None)
+        ws = self._workspaces.get(key)
+        with self._on_device():
+            if ws is None:
+                ws = self._workspace(key, B.slkv_attend_workspace_bytes(self.layout, T, weight is not None))
+            B.slkv_attend_cache(self.layout, self._arrays, q, out, ws, lse, weight, stream)
+        return out, lse
+
+    def rows(self, out_offsets, stream=None):
+        """Every segment's latest out_offsets[s + 1] - out_offsets[s] rows as values: (k, v [rows, d], pos [rows] or None).  Output rows that have no
+        row in the cache hold nothing in particular."""
+        rows = int(out_offsets[-1])
+        k = torch.empty((rows, self.d), dtype=self.query_dtype, device=self.device)
+        v = torch.empty((rows, self.d), dtype=self.query_dtype, device=self.device)
+        pos = torch.empty((rows,), dtype=torch.int32, device=self.device) if self.pos is not None else None
+        with self._on_device():
+            B.slkv_cache_rows(self.layout, self._arrays, out_offsets, k, v, pos, stream)
+        return k, v, pos
+
+    def evict(self, budgets, keep_last, out, kept_idx=None, stream=None):
+        """The rows that stay within the capacities `budgets` [Hkv], by accumulated weight and the latest keep_last always, go to the Cache `out`.
+        kept_idx [rows of out] int32, may be None: their numbers inside their segments."""
+        if kept_idx is not None:
+            self._tensor(kept_idx, (out.rows_in_all,), torch.int32, "kept_idx")
+        if out.device != self.device:
+            raise ValueError("out is on %s, the cache on %s" % (out.device, self.device))
+        with self._on_device():
+            ws = self._workspace("evict", B.slkv_evict_workspace_bytes(self.layout, out.layout, keep_last, budgets))
+            B.slkv_evict_cache(self.layout, self._arrays, out.layout, out._arrays, keep_last, budgets, ws, kept_idx, stream)

@@ -14,7 +14,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libslkv.so")
 
-SLKV_F32, SLKV_BF16, SLKV_F16, SLKV_BF16_KV_FP8 = 0, 1, 2, 3
+SLKV_F32, SLKV_BF16, SLKV_F16, SLKV_BF16_KV_FP8, SLKV_BF16_KV_MXFP4 = 0, 1, 2, 3, 4
 SLKV_POOL_NONE, SLKV_POOL_MAX, SLKV_POOL_AVG = 0, 1, 2
 SLKV_BUDGET_EXACT, SLKV_BUDGET_PAPER_LITERAL, SLKV_BUDGET_EXACT_PER_QUERY_HEAD = 0, 1, 2
 SLKV_AGG_MICRO, SLKV_AGG_MACRO = 0, 1
@@ -28,13 +28,15 @@ EXPORTS = ["slkv_status_str", "slkv_last_error", "slkv_version", "slkv_init", "s
            "slkv_score_heads_workspace_bytes", "slkv_allocate_budgets", "slkv_fixed_from_beta",
            "slkv_compacted_sizes", "slkv_workspace_bytes", "slkv_compress_layer", "slkv_compress_layer_static",
            "slkv_recompress_sizes", "slkv_recompress_workspace_bytes", "slkv_recompress_layer",
+           "slkv_fill_cache", "slkv_append_cache", "slkv_cache_rows", "slkv_attend_workspace_bytes", "slkv_attend_cache",
+           "slkv_evict_workspace_bytes", "slkv_evict_cache",
            "slkv_profile_begin", "slkv_profile_end"]
 
 SLKV_ERR_HIP = 7
 SLKV_WORKSPACE_HEADER_BYTES = 65536
 
 KERNEL_NAMES = ["score_stats", "combine", "score_accum", "select", "gather", "row_cells", "head_reduce", "qk_cells",
-                "qk_fallback"]
+                "qk_fallback", "cache_store", "cache_rows", "attend", "attend_join", "evict"]
 
 
 class SlkvError(RuntimeError):
@@ -68,6 +70,18 @@ class RaggedDesc(C.Structure):
                 ("pool_kernel", C.c_int32), ("pool", C.c_int32), ("reserved", C.c_int32),
                 ("h_in_offsets", C.POINTER(C.c_int64)),
                 ("h_budgets", C.POINTER(C.c_int32))]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32),
+                ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("reserved", C.c_int32 * 2),
+                ("h_offsets", C.c_void_p)]
+
+
+class CacheArrays(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("reserved", C.c_uint32),
+                ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
+                ("d_lengths", C.c_void_p), ("d_pos", C.c_void_p), ("d_weight", C.c_void_p)]
 
 
 _lib = None
@@ -127,6 +141,21 @@ def lib():
         L.slkv_score_heads_first.argtypes = L.slkv_score_heads_ex.argtypes
         L.slkv_score_heads_qk_first.restype = C.c_int
         L.slkv_score_heads_qk_first.argtypes = L.slkv_score_heads_qk.argtypes
+        vp, cd, ca = C.c_void_p, C.c_void_p, C.c_void_p      # descriptors by address: of objects that outlive the call
+        L.slkv_fill_cache.restype = C.c_int
+        L.slkv_fill_cache.argtypes = [cd, ca, vp, vp, vp, vp, vp]
+        L.slkv_append_cache.restype = C.c_int
+        L.slkv_append_cache.argtypes = [cd, ca, C.c_int32, vp, vp, vp, vp, vp, vp, vp]
+        L.slkv_cache_rows.restype = C.c_int
+        L.slkv_cache_rows.argtypes = [cd, ca, vp, vp, vp, vp, vp]
+        L.slkv_attend_workspace_bytes.restype = C.c_int
+        L.slkv_attend_workspace_bytes.argtypes = [cd, C.c_int32, C.c_int32, vp]
+        L.slkv_attend_cache.restype = C.c_int
+        L.slkv_attend_cache.argtypes = [cd, ca, C.c_int32, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.slkv_evict_workspace_bytes.restype = C.c_int
+        L.slkv_evict_workspace_bytes.argtypes = [cd, cd, C.c_int32, vp, vp]
+        L.slkv_evict_cache.restype = C.c_int
+        L.slkv_evict_cache.argtypes = [cd, ca, cd, ca, C.c_int32, vp, vp, vp, C.c_size_t, vp]
         L.slkv_profile_begin.restype = C.c_int
         L.slkv_profile_begin.argtypes = [C.c_int32]
         L.slkv_profile_end.restype = C.c_int
@@ -294,6 +323,87 @@ def slkv_score_heads_qk(q, k, needle_start, needle_len, topk, acc, scores, works
     call = lib().slkv_score_heads_qk_first if first else lib().slkv_score_heads_qk
     _check(call(_ptr(q), _ptr(k), L, Hq, Hkv, T, n, d, int(needle_start), int(needle_len), int(topk), _ptr(acc), _ptr(scores),
                 _ptr(workspace), int(workspace.numel() * workspace.element_size()), _stream(stream)))
+
+
+class CacheLayout:
+    """Host-side descriptor of a cache's rooms; keeps the numpy array it points to alive."""
+
+    def __init__(self, dtype, B, Hq, Hkv, d, offsets):
+        self.offsets = np.array(offsets, dtype=np.int64)           # a copy: the rooms stay what they are
+        if self.offsets.shape != (B * Hkv + 1,):
+            raise ValueError("offsets: %d entries wanted, got shape %s" % (B * Hkv + 1, self.offsets.shape))
+        self.desc = CacheDesc(C.sizeof(CacheDesc), int(dtype), B, Hq, Hkv, d, (C.c_int32 * 2)(0, 0), self.offsets.ctypes.data)
+        self.address = C.addressof(self.desc)
+        self.B, self.Hq, self.Hkv, self.d = B, Hq, Hkv, d
+
+
+class CacheTensors:
+    """The device arrays of a cache; keeps the tensors alive."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, lengths=None, pos=None, weight=None):
+        self.tensors = (k, v, k_scale, v_scale, lengths, pos, weight)
+        self.arrays = CacheArrays(C.sizeof(CacheArrays), 0, *(_ptr(t) for t in self.tensors))
+        self.address = C.addressof(self.arrays)
+
+
+def _offsets_of(layout, offsets):
+    offsets = np.ascontiguousarray(offsets, dtype=np.int64)
+    if offsets.shape != layout.offsets.shape:
+        raise ValueError("offsets: %d entries wanted, got shape %s" % (layout.offsets.size, offsets.shape))
+    return offsets
+
+
+def _budgets_of(layout, budgets):
+    budgets = np.ascontiguousarray(budgets, dtype=np.int32)
+    if budgets.shape != (layout.Hkv,):
+        raise ValueError("budgets: %d entries wanted, got shape %s" % (layout.Hkv, budgets.shape))
+    return budgets
+
+
+def slkv_fill_cache(layout, cache, src_offsets, k_rows, v_rows, pos_rows=None, stream=None):
+    """Enqueues the copy of packed rows [rows, d] into the cache's rooms on `stream` (torch stream; default: current)."""
+    offs = _offsets_of(layout, src_offsets)
+    _check(lib().slkv_fill_cache(layout.address, cache.address, offs.ctypes.data, _ptr(k_rows), _ptr(v_rows), _ptr(pos_rows), _stream(stream)))
+
+
+def slkv_append_cache(layout, cache, k, v, pos=None, at=None, stream=None):
+    """k, v: [B, Hkv, T, d] of any strides with contiguous rows; pos [B, T] int32, at [B * Hkv] int32 device tensors or None."""
+    strides = (C.c_int64 * 6)(*k.stride()[:3], *v.stride()[:3])
+    base = C.addressof(strides)
+    _check(lib().slkv_append_cache(layout.address, cache.address, k.shape[2], _ptr(k), _ptr(v), base, base + 24, _ptr(pos), _ptr(at),
+                                   _stream(stream)))
+
+
+def slkv_cache_rows(layout, cache, out_offsets, k_rows, v_rows, pos_rows=None, stream=None):
+    """Enqueues the copy of every segment's latest rows, as values, to k_rows / v_rows [rows, d]."""
+    offs = _offsets_of(layout, out_offsets)
+    _check(lib().slkv_cache_rows(layout.address, cache.address, offs.ctypes.data, _ptr(k_rows), _ptr(v_rows), _ptr(pos_rows), _stream(stream)))
+
+
+def slkv_attend_workspace_bytes(layout, T, want_weights):
+    n = C.c_size_t(0)
+    _check(lib().slkv_attend_workspace_bytes(layout.address, T, int(want_weights), C.addressof(n)))
+    return int(n.value)
+
+
+def slkv_attend_cache(layout, cache, q, out, workspace, lse=None, weight_out=None, stream=None):
+    """q, out: [B, Hq, T, d]; lse [B, Hq, T] fp32; weight_out [rows] fp32."""
+    _check(lib().slkv_attend_cache(layout.address, cache.address, q.shape[2], _ptr(q), _ptr(out), _ptr(lse), _ptr(weight_out), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def slkv_evict_workspace_bytes(layout, out_layout, w, budgets):
+    n = C.c_size_t(0)
+    budgets = _budgets_of(layout, budgets)
+    _check(lib().slkv_evict_workspace_bytes(layout.address, out_layout.address, int(w), budgets.ctypes.data, C.addressof(n)))
+    return int(n.value)
+
+
+def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, workspace, kept_idx=None, stream=None):
+    """Enqueues the copy of the rows that stay to another cache."""
+    budgets = _budgets_of(layout, budgets)
+    _check(lib().slkv_evict_cache(layout.address, cache.address, out_layout.address, out.address, int(w), budgets.ctypes.data, _ptr(kept_idx),
+                                  _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def slkv_profile_begin(max_records):

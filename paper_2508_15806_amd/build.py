@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libslkv.so")
 
 ROCM_INCLUDE = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 
-HIP_SOURCES = ["compress.hip", "stage1.hip"]
+HIP_SOURCES = ["compress.hip", "stage1.hip", "cache.hip", "attend.hip"]
 HOST_SOURCES = ["slkv_host.cpp", "timing.cpp"]
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC]

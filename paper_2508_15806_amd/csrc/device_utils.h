@@ -150,6 +150,23 @@ __device__ __forceinline__ void select_bin(const uint32_t* hist, uint32_t k, uin
   __syncthreads();
 }
 
+// Segment of a block / row: the largest s with prefix(s) <= x (prefix non-decreasing, prefix(nseg) > x), for an x that is
+// the same in all 64 lanes of a wave (all of them active).  64 prefixes are compared at a time, so that a table of up to 64 segments costs one memory round trip and one of up to 4096 two, not one per
+// halving: these lookups come before a workgroup's first key.
+template <class F>
+__device__ __forceinline__ int find_segment_wave(int nseg, int x, F prefix) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, span = nseg;                             // the segment is one of lo .. lo + span - 1
+  while (span > 1) {
+    const int step = (span + 63) >> 6;
+    const bool below = lane * step < span && prefix(min(lo + lane * step, nseg - 1)) <= x;
+    const int last = max(__popcll(__ballot(below)) - 1, 0);
+    lo += last * step;
+    span = min(step, span - last * step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
 // Order-preserving map from fp32 bit patterns to unsigned integers (larger float -> larger key).
 __device__ __forceinline__ uint32_t float_key(float f) {
   uint32_t u = f == 0.f ? 0u : __float_as_uint(f);   // -0 and +0 rank as equal

@@ -93,6 +93,48 @@ slkv_status validate_ragged_desc(const slkv_ragged_desc* d) {
   return SLKV_OK;
 }
 
+slkv_status validate_offsets(const int64_t* h, int64_t S, const char* name) {
+  if (!h) return fail(SLKV_ERR_NULL, "%s is NULL", name);
+  if (h[0] < 0) return fail(SLKV_ERR_BAD_ARG, "%s[0] < 0", name);
+  for (int64_t s = 0; s < S; ++s)
+    if (h[s + 1] < h[s]) return fail(SLKV_ERR_BAD_ARG, "%s not monotone at %lld", name, (long long)s);
+  if (h[S] >= (int64_t(1) << 31)) return fail(SLKV_ERR_BAD_ARG, "%s[B*Hkv] >= 2^31", name);
+  return SLKV_OK;
+}
+
+slkv_status validate_cache_desc(const slkv_cache_desc* d, const char* name) {
+  if (!d) return fail(SLKV_ERR_NULL, "%s is NULL", name);
+  if (d->struct_size != sizeof(slkv_cache_desc))
+    return fail(SLKV_ERR_BAD_ARG, "%s.struct_size %u != %zu", name, d->struct_size, sizeof(slkv_cache_desc));
+  if (d->dtype < SLKV_F32 || d->dtype > SLKV_BF16_KV_MXFP4) return fail(SLKV_ERR_BAD_ARG, "%s: unknown dtype %d", name, d->dtype);
+  if (d->B < 1 || d->Hq < 1 || d->Hkv < 1) return fail(SLKV_ERR_BAD_ARG, "%s: B, Hq, Hkv must be >= 1", name);
+  if (d->B > (1 << 20) || d->Hkv > (1 << 16) || d->Hq > (1 << 16) || (int64_t)d->B * d->Hkv > (1 << 24))
+    return fail(SLKV_ERR_BAD_ARG, "%s: B, Hq or Hkv too large", name);
+  if (d->Hq % d->Hkv) return fail(SLKV_ERR_BAD_ARG, "%s: Hq %% Hkv != 0", name);
+  if (d->d != 64 && d->d != 128) return fail(SLKV_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", d->d);
+  if (d->reserved[0] || d->reserved[1]) return fail(SLKV_ERR_BAD_ARG, "%s.reserved must be 0", name);
+  const int64_t S = (int64_t)d->B * d->Hkv;
+  slkv_status st = validate_offsets(d->h_offsets, S, "h_offsets");
+  for (int64_t s = 0; st == SLKV_OK && s < S; ++s)     // the kernels round a segment's rows up in 32-bit numbers
+    if (d->h_offsets[s + 1] - d->h_offsets[s] > (int64_t(1) << 30)) st = fail(SLKV_ERR_UNSUPPORTED, "segment %lld: a room of more than 2^30 rows", (long long)s);
+  return st;
+}
+
+slkv_status validate_cache(const slkv_cache_desc* d, const slkv_cache* c, const char* name) {
+  if (!c) return fail(SLKV_ERR_NULL, "%s is NULL", name);
+  if (c->struct_size != sizeof(slkv_cache))
+    return fail(SLKV_ERR_BAD_ARG, "%s.struct_size %u != %zu", name, c->struct_size, sizeof(slkv_cache));
+  if (c->reserved) return fail(SLKV_ERR_BAD_ARG, "%s.reserved must be 0", name);
+  const bool scaled = d->dtype == SLKV_BF16_KV_MXFP4;
+  if (d->h_offsets[(int64_t)d->B * d->Hkv] > 0 && (!c->d_k || !c->d_v || (scaled && (!c->d_k_scale || !c->d_v_scale))))
+    return fail(SLKV_ERR_NULL, "%s: an array of keys, values or scales is NULL", name);
+  if (!scaled && (c->d_k_scale || c->d_v_scale)) return fail(SLKV_ERR_BAD_ARG, "%s: scales belong to MXFP4 alone", name);
+  const void* ptrs[] = {c->d_k, c->d_v, c->d_k_scale, c->d_v_scale, c->d_lengths, c->d_pos, c->d_weight};
+  for (const void* ptr : ptrs)
+    if (reinterpret_cast<uintptr_t>(ptr) % 16) return fail(SLKV_ERR_BAD_ARG, "%s: device pointer %p not 16-byte aligned", name, ptr);
+  return SLKV_OK;
+}
+
 }  // namespace slkv
 
 using namespace slkv;

@@ -22,6 +22,11 @@ int64_t kept_rows(int64_t n, int64_t w, int64_t cap);
 // Checks everything in the descriptor that can be checked on the host.
 slkv_status validate_desc(const slkv_layer_desc* d);
 slkv_status validate_ragged_desc(const slkv_ragged_desc* d);
+slkv_status validate_cache_desc(const slkv_cache_desc* d, const char* name = "desc");
+// The cache's arrays: there where rows > 0 (scales: exactly for MXFP4), 16-byte aligned.
+slkv_status validate_cache(const slkv_cache_desc* d, const slkv_cache* c, const char* name = "cache");
+// Source or target rows of a call, [B*Hkv+1] offsets.
+slkv_status validate_offsets(const int64_t* h, int64_t S, const char* name);
 
 // Kernel timing (slkv_profile_begin / _end).  A ScopedKernelTimer names the kernel that the
 // launches inside its scope belong to; while profiling is on, profile_events() hands such a

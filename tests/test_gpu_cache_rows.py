@@ -1,0 +1,247 @@
+"""slkv_fill_cache, slkv_append_cache and slkv_cache_rows: conversions bit for bit against the formats' definitions, places, lengths, what stays untouched."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode
+from paper_2508_15806_amd import api
+from paper_2508_15806_amd import binding as B
+from decode_parity import DTYPES, f64, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def narrowed(vals, dtype):
+    """(rows as the cache holds them, exponents or None) of float64 values [.., d], as numpy."""
+    if dtype == "bf16_kv4":
+        return decode.to_mxfp4(vals)
+    return (decode.to_e4m3(vals), None) if dtype == "bf16_kv8" else (vals, None)
+
+
+def stored(cache, x, e, rows):
+    got = x[rows]
+    return (got.cpu().numpy() if cache.dtype in ("bf16_kv4", "bf16_kv8") else f64(got)), None if e is None else e[rows].cpu().numpy()
+
+
+def mark(cache):
+    """A pattern in every array, to see what is written."""
+    for t in (cache.k, cache.v, cache.k_scale, cache.v_scale):
+        if t is not None:
+            t.view(torch.uint8).fill_(0x5A)
+    cache.pos.fill_(-9)
+    cache.weight.fill_(9.5)
+
+
+def check_rows(cache, k_want, v_want, rows):
+    for x, e, vals in ((cache.k, cache.k_scale, k_want), (cache.v, cache.v_scale, v_want)):
+        got, exps = stored(cache, x, e, rows)
+        want, wexps = narrowed(vals, cache.dtype)
+        if wexps is not None:
+            assert np.array_equal(exps, wexps)
+            bad = np.repeat(wexps == 255, 16, -1)         # codes of a block of NaN say nothing
+            assert np.array_equal(got[~bad], want[~bad])
+        elif cache.dtype == "bf16_kv8":
+            nan = (want & 0x7F) == 0x7F
+            assert np.array_equal((got & 0x7F) == 0x7F, nan) and np.array_equal(got[~nan], want[~nan])
+        else:
+            assert np.array_equal(got, want, equal_nan=True)
+
+
+def check_untouched(cache, rows):
+    """Rows other than these still hold the pattern."""
+    other = torch.ones(cache.rows_in_all, dtype=torch.bool, device="cuda")
+    other[rows] = False
+    for t in (cache.k, cache.v, cache.k_scale, cache.v_scale):
+        if t is not None:
+            assert bool((t.view(torch.uint8).reshape(cache.rows_in_all, -1)[other] == 0x5A).all())
+    assert bool((cache.pos[other] == -9).all()) and bool((cache.weight[other] == 9.5).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B_", [1, 40, 200])
+def test_fill(dtype, d, B_):
+    rng = np.random.default_rng([d, B_, DTYPES.index(dtype)])
+    Hkv = 3
+    counts = rng.integers(0, 100, B_ * Hkv)
+    counts[:3] = [0, 1, 33]
+    rooms = counts + rng.integers(0, 20, B_ * Hkv)
+    src = np.concatenate([[0], np.cumsum(counts)]) + 5               # the first source row is not 0
+    offsets = np.concatenate([[0], np.cumsum(rooms)]) + 2
+    cache = api.Cache(dtype, B_, Hkv * 2, Hkv, d, offsets)
+    mark(cache)
+    k, v = normal(rng, (int(src[-1]), d), dtype), normal(rng, (int(src[-1]), d), dtype)
+    pos = torch.arange(int(src[-1]), dtype=torch.int32, device="cuda") + 1000
+    cache.fill(k, v, src, pos)
+    at = np.concatenate([offsets[s] + np.arange(c) for s, c in enumerate(counts)]).astype(np.int64)
+    rows = torch.from_numpy(at).cuda()
+    assert cache.lengths.cpu().tolist() == counts.tolist()
+    check_rows(cache, f64(k)[5:], f64(v)[5:], rows)
+    check_untouched(cache, rows)
+    assert torch.equal(cache.pos[rows], pos[5:]) and bool((cache.weight[rows] == 0).all())
+    # and back: all rows, then the latest 20 of each
+    back = cache.rows(np.concatenate([[0], np.cumsum(counts)]))
+    for got, (x, e) in zip(back, ((cache.k, cache.k_scale), (cache.v, cache.v_scale))):
+        codes, exps = stored(cache, x, e, rows)
+        want = decode.from_mxfp4(codes, exps) if dtype == "bf16_kv4" else decode.from_e4m3(codes) if dtype == "bf16_kv8" else codes
+        assert np.array_equal(f64(got), want)
+    assert torch.equal(back[2], pos[5:])
+    few = np.arange(B_ * Hkv + 1) * 20
+    last = [torch.full((int(few[-1]), d), 77.0, dtype=cache.query_dtype, device="cuda") for _ in range(2)]
+    last_pos = torch.full((int(few[-1]),), -4, dtype=torch.int32, device="cuda")
+    B.slkv_cache_rows(cache.layout, cache._arrays, few, last[0], last[1], last_pos)
+    for s in range(0, B_ * Hkv, 7):
+        c = int(counts[s])
+        m = min(c, 20)
+        a = int(src[s]) - 5 + c - m
+        assert torch.equal(last[0][s * 20:s * 20 + m], back[0][a:a + m]) and torch.equal(last[1][s * 20:s * 20 + m], back[1][a:a + m])
+        assert torch.equal(last_pos[s * 20:s * 20 + m], back[2][a:a + m])
+        assert bool((last[0][s * 20 + m:(s + 1) * 20] == 77).all()) and bool((last_pos[s * 20 + m:(s + 1) * 20] == -4).all())
+
+
+def as_bf16(values):
+    """MXFP4 values as bfloat16: 4 * 2^126 = 2^128 (to which magnitudes above 3.5 * 2^126 go) and what is above it exceed the largest
+    bfloat16, (2 - 2^-7) * 2^127 < 2^128, and are infinite."""
+    return np.where(np.abs(values) >= 2.0 ** 128, np.copysign(np.inf, values), values)
+
+
+@pytest.mark.parametrize("dtype", ["bf16_kv8", "bf16_kv4"])
+def test_every_bf16_value(dtype):
+    """All 65536 codes: as they are (E4M3), and in blocks of like magnitude and against a larger neighbour (MXFP4)."""
+    bits = np.arange(65536, dtype=np.uint16)
+    rows = [bits.reshape(-1, 64)]
+    if dtype == "bf16_kv4":
+        other = bits.reshape(-1, 64).copy()
+        rng = np.random.default_rng(3)
+        # a block's largest element up to 2^6 times the others, at a place of its own
+        big = (other[:, ::32].astype(np.int64) & 0x7FFF) + (rng.integers(0, 7, other[:, ::32].shape) << 7) + rng.integers(0, 128, other[:, ::32].shape)
+        other[:, ::32] = np.minimum(big, 0x7F7F)
+        rows += [other, rng.permutation(bits).reshape(-1, 64)]
+    x = np.concatenate(rows)
+    x = np.concatenate([x, np.zeros_like(x[:1]), np.full_like(x[:1], 0x8000)])         # blocks of zeros
+    t = torch.from_numpy(x.view(np.int16)).cuda().view(torch.bfloat16)
+    n = len(x)
+    cache = api.Cache(dtype, 1, 1, 1, 64, [0, n])
+    cache.fill(t, t.flip(0), [0, n])
+    check_rows(cache, f64(t), f64(t)[::-1], slice(0, n))
+    back = cache.rows([0, n])
+    codes, exps = stored(cache, cache.k, cache.k_scale, slice(0, n))
+    want = as_bf16(decode.from_mxfp4(codes, exps)) if dtype == "bf16_kv4" else decode.from_e4m3(codes)
+    assert np.array_equal(f64(back[0]), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("exp", [0, 1, 2, 126, 127, 128, 253, 254, 255])
+def test_every_mxfp4_code(exp):
+    codes = torch.arange(256, dtype=torch.uint8).reshape(8, 32).cuda()
+    scale = torch.full((8, 2), exp, dtype=torch.uint8, device="cuda")
+    cache = api.Cache("bf16_kv4", 1, 1, 1, 64, [0, 8], k=codes, v=codes.flip(0).contiguous(), k_scale=scale, v_scale=scale)
+    k, v, _ = cache.rows([0, 8])
+    with np.errstate(over="ignore"):
+        want = decode.from_mxfp4(codes.cpu().numpy(), scale.cpu().numpy())
+    want = as_bf16(want)
+    assert np.array_equal(f64(k), want, equal_nan=True) and np.array_equal(f64(v), want[::-1], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [1, 2, 5, 17, 64])
+@pytest.mark.parametrize("layout", ["head", "token"])
+def test_append(dtype, d, T, layout):
+    rng = np.random.default_rng([d, T, DTYPES.index(dtype)])
+    B_, Hkv = 3, 2
+    rooms = [70, 130, 64, 200, 10, 100]
+    lens = [0, 3, 64, 130, 9, 99]                     # an empty segment, full ones, and ones that take some of the rows
+    offsets = np.concatenate([[0], np.cumsum(rooms)]) + 1
+    cache = api.Cache(dtype, B_, Hkv * 4, Hkv, d, offsets)
+    mark(cache)
+    cache.lengths.copy_(torch.tensor(lens, dtype=torch.int32))
+    k, v = normal(rng, (B_, Hkv, T, d), dtype), normal(rng, (B_, Hkv, T, d), dtype)
+    if layout == "token":
+        k, v = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+    pos = torch.from_numpy(rng.integers(0, 1 << 30, (B_, T)).astype(np.int32)).cuda()
+    cache.append(k, v, pos)
+    fit = [min(T, r - n) for r, n in zip(rooms, lens)]
+    assert cache.lengths.cpu().tolist() == [n + f for n, f in zip(lens, fit)]
+    rows = torch.from_numpy(np.concatenate([offsets[s] + lens[s] + np.arange(f) for s, f in enumerate(fit)]).astype(np.int64)).cuda()
+    pick = [(s // Hkv, s % Hkv, t) for s, f in enumerate(fit) for t in range(f)]
+    b, h, t = (torch.tensor(x, device="cuda") for x in zip(*pick))
+    check_rows(cache, f64(k[b, h, t]), f64(v[b, h, t]), rows)
+    check_untouched(cache, rows)
+    assert torch.equal(cache.pos[rows], pos[b, t]) and bool((cache.weight[rows] == 0).all())
+    # again behind fewer rows: what was there is overwritten, the lengths follow
+    at = torch.tensor([0, 1, 2, 3, 4, 5], dtype=torch.int32, device="cuda")
+    cache.append(k, v, None, at=at)
+    assert cache.lengths.cpu().tolist() == [min(T, r - i) + i for i, r in enumerate(rooms)]
+    assert at.cpu().tolist() == list(range(6))
+
+
+def test_append_to_many_segments_and_broadcast_rows():
+    rng = np.random.default_rng(4)
+    S, d = 1800, 64
+    cache = api.Cache("bf16", S, 1, 1, d, np.arange(S + 1) * 3)
+    k = normal(rng, (S, 1, 1, d), "bf16")
+    v = normal(rng, (1, 1, 1, d), "bf16").expand(S, 1, 2, d)         # stride 0: one row for all
+    cache.append(k, v[:, :, :1])
+    cache.append(k.expand(S, 1, 2, d), v)
+    assert cache.lengths.cpu().tolist() == [3] * S
+    got = cache.k.reshape(S, 3, d)
+    assert all(torch.equal(got[:, i], k[:, 0, 0]) for i in range(3)) and bool((cache.v == v[0, 0, 0]).all())
+
+
+def test_append_lengths_out_of_range():
+    rng = np.random.default_rng(5)
+    cache = api.Cache("bf16_kv4", 1, 3, 3, 64, [0, 8, 16, 24])
+    mark(cache)
+    cache.lengths.copy_(torch.tensor([-7, 1000, (1 << 31) - 1], dtype=torch.int32))
+    k = normal(rng, (1, 3, 2, 64), "bf16_kv4")
+    cache.append(k, k)
+    assert cache.lengths.cpu().tolist() == [2, 8, 8]
+    check_untouched(cache, torch.tensor([0, 1], device="cuda"))
+
+
+def test_captured_appends():
+    rng = np.random.default_rng(6)
+    cache = api.Cache("bf16_kv8", 2, 2, 2, 128, [0, 9, 18, 27, 36])
+    k, v = normal(rng, (2, 2, 1, 128), "bf16_kv8"), normal(rng, (2, 2, 1, 128), "bf16_kv8")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        cache.append(k, v)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        cache.append(k, v)
+    cache.lengths.fill_(3)
+    for i in range(8):
+        k.copy_(normal(rng, k.shape, "bf16_kv8"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        n = min(4 + i, 9)
+        assert cache.lengths.cpu().tolist() == [n] * 4
+        if 3 + i < 9:
+            at = torch.tensor([0, 9, 18, 27], device="cuda") + 3 + i
+            assert np.array_equal(cache.k[at].cpu().numpy(), decode.to_e4m3(f64(k)[:, :, 0].reshape(4, 128)))
+
+
+def test_refusals_of_tensors():
+    cache = api.Cache("bf16_kv4", 2, 4, 2, 64, [0, 8, 16, 24, 32])
+    k = torch.zeros((2, 2, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (k.float(), k[:1], k[..., ::2], k.transpose(2, 3), k.cpu()):
+        with pytest.raises(ValueError):
+            cache.append(bad, k)
+    with pytest.raises(ValueError):
+        cache.append(k, k, pos=torch.zeros((2, 2), dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        cache.append(k, k, at=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    rows = torch.zeros((10, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        cache.fill(rows, rows, [0, 1, 2, 3, 11])
+    with pytest.raises(ValueError):
+        cache.fill(rows, rows, [0, 1, 2, 3])
+    with pytest.raises(B.SlkvError) as e:
+        cache.fill(rows, rows, [0, 9, 9, 9, 9])
+    assert e.value.status == 6
+    with pytest.raises(ValueError):
+        api.Cache("bf16_kv4", 1, 1, 1, 64, [0, 4], k=torch.zeros((4, 32), dtype=torch.uint8, device="cuda"), v=torch.zeros((4, 32), dtype=torch.uint8, device="cuda"))

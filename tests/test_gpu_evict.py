@@ -1,0 +1,171 @@
+"""slkv_evict_cache against the oracle's full sort: sets, order, bytes, lengths, ties, weights that are no ordinary numbers."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode
+from paper_2508_15806_amd import api
+from paper_2508_15806_amd import binding as B
+from decode_parity import DTYPES, random_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def check(cache, budgets, w, slack=0, positions=True, weights=True, before=0):
+    S, Hkv = cache.B * cache.Hkv, cache.Hkv
+    off = cache.layout.offsets
+    lens = [min(max(n, 0), int(off[s + 1] - off[s])) for s, n in enumerate(cache.lengths.cpu().tolist())]
+    most = [min(int(off[s + 1] - off[s]), max(budgets[s % Hkv], w)) for s in range(S)]
+    out_off = np.concatenate([[0], np.cumsum([m + slack for m in most])]) + before
+    out = api.Cache(cache.dtype, cache.B, cache.Hq, Hkv, cache.d, out_off, positions=positions, weights=weights)
+    rows_out = int(out_off[-1])
+    for t in (out.k, out.v, out.k_scale, out.v_scale):
+        if t is not None:
+            t.view(torch.uint8).fill_(0x5A)
+    if out.pos is not None:
+        out.pos.fill_(-9)
+    if out.weight is not None:
+        out.weight.fill_(9.5)
+    kept_idx = torch.full((rows_out,), -3, dtype=torch.int32, device="cuda")
+    cache.evict(budgets, w, out, kept_idx)
+    torch.cuda.synchronize()
+    weight = cache.weight.cpu().numpy()
+    want = [decode.evict_segment(weight[off[s]:off[s] + lens[s]], w, budgets[s % Hkv]) for s in range(S)]
+    assert out.lengths.cpu().tolist() == [len(x) for x in want]
+    src = torch.from_numpy(np.concatenate([x + off[s] for s, x in enumerate(want)]).astype(np.int64)).cuda()
+    dst = torch.from_numpy(np.concatenate([np.arange(len(x)) + out_off[s] for s, x in enumerate(want)]).astype(np.int64)).cuda()
+    assert np.array_equal(kept_idx[dst].cpu().numpy(), np.concatenate(want))
+    other = torch.ones(rows_out, dtype=torch.bool, device="cuda")
+    other[dst] = False
+    assert bool((kept_idx[other] == -3).all())
+
+    def same(a, b, rest):
+        if a is None or b is None:
+            return
+        a, b = (x.view(torch.uint8).reshape(x.shape[0], -1) for x in (a, b))
+        assert torch.equal(a[src], b[dst])
+        assert bool((b[other] == rest).all()) if rest is not None else True
+    same(cache.k, out.k, 0x5A), same(cache.v, out.v, 0x5A)
+    same(cache.k_scale, out.k_scale, 0x5A), same(cache.v_scale, out.v_scale, 0x5A)
+    same(cache.pos, out.pos, None), same(cache.weight, out.weight, None)
+    if out.pos is not None:
+        assert bool((out.pos[other] == -9).all())
+    if out.weight is not None:
+        assert bool((out.weight[other] == 9.5).all())
+    return out
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("w", [0, 1, 32])
+def test_types_lengths_windows(dtype, d, w):
+    rng = np.random.default_rng([d, w, DTYPES.index(dtype)])
+    lens = [0, 1, 31, 32, 33, 64, 65, 100, 1000, 1023, 1024, 1025, 4096, 4097, 5000, 12]
+    cache = random_cache(rng, dtype, 4, 4, 2, d, lens, rooms=[n + 17 for n in lens], before=5)
+    check(cache, [0, 31, 64, 700], w, slack=3, before=2)
+
+
+@pytest.mark.parametrize("n", [8192, 32768, 70001])
+@pytest.mark.parametrize("share", [0.01, 0.5, 0.999])
+def test_long_histories(n, share):
+    rng = np.random.default_rng(n)
+    cache = random_cache(rng, "bf16_kv4", 1, 2, 4, 64, [n, n - 5])
+    cache.weight.copy_(torch.from_numpy((rng.random(2 * n - 5) ** 12).astype(np.float32)))
+    check(cache, [int(n * share), 40], 8)
+
+
+@pytest.mark.parametrize("n", [50, 3000, 20000])
+def test_equal_weights(n):
+    rng = np.random.default_rng(n)
+    cache = random_cache(rng, "bf16", 1, 4, 1, 64, [n] * 4)
+    w = cache.weight.reshape(4, n)
+    w[0] = 0.25                                            # all equal
+    w[1] = torch.from_numpy(rng.integers(0, 3, n).astype(np.float32))
+    w[2] = 0.0
+    w[2, ::7] = -0.0                                       # ranks as 0
+    w[3] = torch.from_numpy(rng.choice([1.0, np.nextafter(np.float32(1), np.float32(2)), 2.0], n).astype(np.float32))
+    check(cache, [n // 3, n // 2, n // 5, n - 7], 5)
+
+
+def test_weights_that_are_no_ordinary_numbers():
+    n = 2000
+    rng = np.random.default_rng(1)
+    cache = random_cache(rng, "f16", 1, 3, 1, 64, [n] * 3)
+    w = cache.weight.reshape(3, n)
+    w[0, ::50] = float("nan")
+    w[0, 1::60] = float("inf")
+    w[0, 2::70] = -float("nan")
+    w[1] = -w[1]
+    w[1, ::9] = float("-inf")
+    w[2] = w[2] * 1e-42                                    # subnormal
+    check(cache, [60, 300, 1000], 0)
+
+
+def test_lengths_out_of_range_and_in_place():
+    rng = np.random.default_rng(2)
+    cache = random_cache(rng, "bf16", 1, 4, 1, 64, [100, 100, 100, 100])
+    cache.lengths.copy_(torch.tensor([-1, 1 << 30, 60, 100], dtype=torch.int32))
+    want = check(cache, [50, 50, 70, 0], 10)
+    # the lengths may be the same array
+    out = api.Cache("bf16", 1, 4, 4, 64, want.layout.offsets, lengths=cache.lengths)
+    cache.evict([50, 50, 70, 0], 10, out)
+    assert torch.equal(out.lengths, want.lengths) and cache.lengths.cpu().tolist() == [0, 50, 60, 10]
+
+
+@pytest.mark.parametrize("S", [64, 65, 290, 291, 900])
+def test_segment_tables(S):
+    rng = np.random.default_rng(S)
+    lens = rng.integers(0, 60, S).tolist()
+    cache = random_cache(rng, "bf16_kv4", S, 1, 1, 64, lens, rooms=[n + 4 for n in lens])
+    check(cache, [25], 3, slack=1)
+
+
+def test_without_positions_or_weights():
+    rng = np.random.default_rng(3)
+    cache = random_cache(rng, "f32", 1, 2, 1, 128, [90, 40])
+    check(cache, [30, 30], 2, positions=False, weights=False)
+
+
+def test_captured_eviction_follows_lengths_and_weights():
+    rng = np.random.default_rng(4)
+    cache = random_cache(rng, "bf16", 2, 2, 2, 64, [3000, 400, 90, 5])
+    budgets, w = [300, 50], 16
+    offs = np.concatenate([[0], np.cumsum([300, 50, 90, 16])])
+    out, ref = api.Cache("bf16", 2, 4, 2, 64, offs), api.Cache("bf16", 2, 4, 2, 64, offs)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        cache.evict(budgets, w, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        cache.evict(budgets, w, out)
+    for lens in ([3000, 400, 90, 5], [10, 400, 17, 0], [299, 51, 90, 5], [3000, 49, 0, 1]):
+        cache.lengths.copy_(torch.tensor(lens, dtype=torch.int32))
+        cache.weight.copy_(torch.from_numpy(rng.random(cache.rows_in_all, dtype=np.float32)))
+        out.k.zero_(), ref.k.zero_(), out.weight.zero_(), ref.weight.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        cache.evict(budgets, w, ref)
+        torch.cuda.synchronize()
+        assert torch.equal(out.k, ref.k) and torch.equal(out.weight, ref.weight) and torch.equal(out.lengths, ref.lengths)
+
+
+def test_refusals():
+    cache = api.Cache("bf16", 1, 2, 2, 64, [0, 50, 100])
+    for offs, status in (([0, 19, 40], 6), ([0, 20, 39], 6)):
+        with pytest.raises(B.SlkvError) as e:
+            cache.evict([20, 20], 4, api.Cache("bf16", 1, 2, 2, 64, offs))
+        assert e.value.status == status
+    with pytest.raises(B.SlkvError) as e:
+        cache.evict([20, 20], 4, cache)                    # onto itself
+    assert e.value.status == 2
+    with pytest.raises(B.SlkvError) as e:
+        cache.evict([20, 20], 4, api.Cache("f16", 1, 2, 2, 64, [0, 50, 100]))
+    assert e.value.status == 2
+    with pytest.raises(ValueError):
+        cache.evict([20], 4, api.Cache("bf16", 1, 2, 2, 64, [0, 50, 100]))
+    with pytest.raises(ValueError):
+        cache.evict([20, 20], 4, api.Cache("bf16", 1, 2, 2, 64, [0, 50, 100]), kept_idx=torch.zeros(9, dtype=torch.int32, device="cuda"))

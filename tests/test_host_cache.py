@@ -1,0 +1,162 @@
+"""CPU-only tests of the calls on a cache: descriptors, refusals before any GPU call, workspace sizes."""
+
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from paper_2508_15806_amd import binding as B
+
+FAKE, ODD, NULL = 4096, 4100, None
+BIG = 1 << 40
+
+
+def layout(**over):
+    p = dict(dtype=B.SLKV_BF16, B=2, Hq=8, Hkv=2, d=128, offsets=[0, 100, 130, 130, 190])
+    p.update(over)
+    return B.CacheLayout(**p)
+
+
+def arrays(scaled=False, **over):
+    p = dict(d_k=FAKE, d_v=FAKE, d_k_scale=FAKE if scaled else NULL, d_v_scale=FAKE if scaled else NULL, d_lengths=FAKE, d_pos=FAKE, d_weight=FAKE)
+    size, reserved = over.pop("struct_size", C.sizeof(B.CacheArrays)), over.pop("reserved", 0)
+    p.update(over)
+    return B.CacheArrays(size, reserved, *(p[k] for k in ("d_k", "d_v", "d_k_scale", "d_v_scale", "d_lengths", "d_pos", "d_weight")))
+
+
+def attend(lay=None, arr=None, T=1, q=FAKE, out=FAKE, lse=NULL, weight=NULL, ws=FAKE, nbytes=BIG):
+    lay, arr = lay or layout(), arrays() if arr is None else arr
+    return B.lib().slkv_attend_cache(lay.address, C.addressof(arr), T, q, out, lse, weight, ws, nbytes, None)
+
+
+def test_struct_sizes_match_the_header():
+    assert C.sizeof(B.CacheDesc) == 6 * 4 + 8 + 8 and C.sizeof(B.CacheArrays) == 8 + 7 * 8
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(d=96), 4), (dict(Hq=7), 2), (dict(dtype=5), 2), (dict(dtype=-1), 2), (dict(B=0, offsets=[0]), 2),
+    (dict(offsets=[0, 100, 90, 130, 190]), 2), (dict(offsets=[-1, 100, 130, 130, 190]), 2), (dict(offsets=[0, 100, 130, 130, 2 ** 31]), 2),
+    (dict(Hkv=0, Hq=0, offsets=[0]), 2), (dict(offsets=[0, 0, 2 ** 30 + 1, 2 ** 30 + 1, 2 ** 30 + 1]), 4),
+])
+def test_descriptors(over, status):
+    lay = layout(**over)
+    with pytest.raises(B.SlkvError) as e:
+        B.slkv_attend_workspace_bytes(lay, 1, True)
+    assert e.value.status == status and B.lib().slkv_last_error() != b""
+
+
+def test_descriptor_struct():
+    L, n = B.lib(), C.c_size_t(0)
+    lay = layout()
+    lay.desc.struct_size = 8
+    assert L.slkv_attend_workspace_bytes(lay.address, 1, 0, C.addressof(n)) == 2
+    lay = layout()
+    lay.desc.reserved[1] = 1
+    assert L.slkv_attend_workspace_bytes(lay.address, 1, 0, C.addressof(n)) == 2
+    lay = layout()
+    lay.desc.h_offsets = None
+    assert L.slkv_attend_workspace_bytes(lay.address, 1, 0, C.addressof(n)) == 1
+    assert L.slkv_attend_workspace_bytes(None, 1, 0, C.addressof(n)) == 1
+    lay = layout()
+    assert L.slkv_attend_workspace_bytes(lay.address, 1, 0, None) == 1
+    with pytest.raises(ValueError):
+        layout(offsets=[0, 1])
+
+
+def test_layout_keeps_a_copy_of_the_offsets():
+    offs = np.array([0, 100, 130, 130, 190], dtype=np.int64)
+    lay = layout(offsets=offs)
+    before = B.slkv_attend_workspace_bytes(lay, 1, True)
+    offs[:] = 5
+    assert B.slkv_attend_workspace_bytes(lay, 1, True) == before
+
+
+def test_attend_refuses_before_touching_the_gpu():
+    assert attend(q=NULL) == 1 and attend(out=NULL) == 1 and attend(ws=NULL) == 1
+    assert attend(T=0) == 2 and attend(T=17) == 4 and attend(T=1 << 30) == 4          # 4 * 17 queries a segment
+    assert attend(lay=layout(Hq=130), T=1) == 4
+    for bad in ("q", "out", "lse", "weight", "ws"):
+        assert attend(**{bad: ODD}) == 2
+    assert attend(nbytes=0) == 5
+    need = B.slkv_attend_workspace_bytes(layout(), 1, True)
+    assert attend(weight=FAKE, nbytes=need - 1) == 5
+    assert B.slkv_attend_workspace_bytes(layout(), 1, False) < need
+    for key in ("d_k", "d_v"):
+        assert attend(arr=arrays(**{key: NULL})) == 1
+        assert attend(arr=arrays(**{key: ODD})) == 2
+    assert attend(arr=arrays(d_lengths=ODD)) == 2 and attend(arr=arrays(struct_size=8)) == 2 and attend(arr=arrays(reserved=1)) == 2
+    assert attend(arr=arrays(scaled=True)) == 2                                       # scales without MXFP4
+    four = layout(dtype=B.SLKV_BF16_KV_MXFP4)
+    assert attend(lay=four) == 1 and attend(lay=four, arr=arrays(scaled=True, d_v_scale=NULL)) == 1
+    lay = layout()
+    assert B.lib().slkv_attend_cache(lay.address, None, 1, FAKE, FAKE, None, None, FAKE, BIG, None) == 1
+
+
+def test_the_other_calls_refuse_mxfp4():
+    lay = B.Layer(B.SLKV_BF16_KV_MXFP4, 1, 8, 2, 128, 16, [0, 100], [40, 40], (128, 12800), (128, 12800))
+    with pytest.raises(B.SlkvError) as e:
+        B.slkv_compacted_sizes(lay)
+    assert e.value.status == 2
+
+
+def fill(lay=None, arr=None, src=(0, 100, 130, 130, 190), k=FAKE, v=FAKE, pos=FAKE):
+    lay, arr = lay or layout(), arrays() if arr is None else arr
+    src = None if src is None else np.array(src, dtype=np.int64)
+    return B.lib().slkv_fill_cache(lay.address, C.addressof(arr), None if src is None else src.ctypes.data, k, v, pos, None)
+
+
+def test_fill_refuses_before_touching_the_gpu():
+    assert fill(src=None) == 1 and fill(k=NULL) == 1 and fill(v=NULL) == 1 and fill(arr=arrays(d_lengths=NULL)) == 1
+    assert fill(src=[0, 101, 131, 131, 191]) == 6                                     # one row too many
+    assert fill(src=[0, 10, 5, 30, 60]) == 2 and fill(src=[-1, 10, 15, 30, 60]) == 2
+    assert fill(src=[2 ** 31 - 61, 2 ** 31 - 1, 2 ** 31, 2 ** 31, 2 ** 31]) == 2
+    assert fill(k=ODD) == 2 and fill(pos=ODD) == 2
+
+
+def append(arr=None, T=1, k=FAKE, v=FAKE, ks=(256, 128, 128), vs=(256, 128, 128), pos=NULL, at=NULL, **over):
+    lay = layout(**over)
+    arr = arrays() if arr is None else arr
+    ks, vs = (None if x is None else (C.c_int64 * 3)(*x) for x in (ks, vs))
+    return B.lib().slkv_append_cache(lay.address, C.addressof(arr), T, k, v, None if ks is None else C.addressof(ks), None if vs is None else C.addressof(vs),
+                                     pos, at, None)
+
+
+def test_append_refuses_before_touching_the_gpu():
+    assert append(k=NULL) == 1 and append(v=NULL) == 1 and append(ks=None) == 1 and append(arr=arrays(d_lengths=NULL)) == 1
+    assert append(T=0) == 2 and append(T=65) == 4
+    assert append(ks=(256, 128, 4)) == 2 and append(vs=(-256, 128, 128)) == 2         # 8 bytes; negative
+    assert append(k=ODD) == 2 and append(pos=ODD) == 2 and append(at=ODD) == 2
+
+
+def test_rows_refuses_before_touching_the_gpu():
+    def rows(out=(0, 5, 10, 15, 20), k=FAKE, v=FAKE, pos=NULL, arr=None):
+        lay, arr = layout(), arrays() if arr is None else arr
+        out = None if out is None else np.array(out, dtype=np.int64)
+        return B.lib().slkv_cache_rows(lay.address, C.addressof(arr), None if out is None else out.ctypes.data, k, v, pos, None)
+    assert rows(out=None) == 1 and rows(k=NULL) == 1 and rows(v=NULL) == 1 and rows(pos=FAKE, arr=arrays(d_pos=NULL)) == 1
+    assert rows(out=[0, 5, 4, 5, 6]) == 2 and rows(k=ODD) == 2
+
+
+def test_evict_refuses_before_touching_the_gpu():
+    far = 1 << 30
+
+    def evict(lay=None, arr=None, out_lay=None, out=None, w=4, budgets=(40, 20), idx=NULL, ws=FAKE, nbytes=BIG):
+        lay = lay or layout()
+        out_lay = out_lay or layout(offsets=[0, 40, 60, 100, 120])
+        arr = arr or arrays()
+        out = out or arrays(**{f: far + i * (1 << 22) for i, f in enumerate(["d_k", "d_v", "d_lengths", "d_pos", "d_weight"])})
+        bud = None if budgets is None else np.array(budgets, dtype=np.int32)
+        return B.lib().slkv_evict_cache(lay.address, C.addressof(arr), out_lay.address, C.addressof(out), w, None if bud is None else bud.ctypes.data, idx,
+                                        ws, nbytes, None)
+    assert evict(w=-1) == 2 and evict(budgets=None) == 1 and evict(budgets=(-1, 3)) == 2
+    assert evict(arr=arrays(d_weight=NULL)) == 1 and evict(ws=NULL) == 1
+    assert evict(ws=ODD) == 2 and evict(idx=ODD) == 2
+    assert evict(out_lay=layout(offsets=[0, 39, 60, 100, 120])) == 6
+    assert evict(w=50) == 6                                                            # the latest 50 rows do not fit
+    assert evict(out_lay=layout(dtype=B.SLKV_F16, offsets=[0, 40, 60, 100, 120])) == 2
+    assert evict(out_lay=layout(Hq=4, offsets=[0, 40, 60, 100, 120])) == 2
+    assert evict(nbytes=0) == 5
+    assert evict(out=arrays()) == 2                                                    # the same arrays
+    one = dict(d_k=far, d_v=far + (1 << 22), d_lengths=far + (2 << 22), d_pos=far + (3 << 22), d_weight=far + (4 << 22))
+    assert evict(out=arrays(**dict(one, d_v=FAKE + 190 * 256 - 16))) == 2              # overlaps by 16 bytes
+    assert evict(out=arrays(**dict(one, d_lengths=NULL))) == 1
