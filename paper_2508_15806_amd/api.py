@@ -213,8 +213,9 @@ class Cache:
         return contextlib.nullcontext() if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
 
     def _workspace(self, key, nbytes):
+        """A workspace for calls of one kind and size: never replaced, since a captured graph may hold it."""
         ws = self._workspaces.get(key)
-        if ws is None or ws.numel() < nbytes:
+        if ws is None:
             ws = self._workspaces[key] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
         return ws
 
@@ -287,5 +288,6 @@ class Cache:
         if out.device != self.device:
             raise ValueError("out is on %s, the cache on %s" % (out.device, self.device))
         with self._on_device():
-            ws = self._workspace("evict", B.slkv_evict_workspace_bytes(self.layout, out.layout, keep_last, budgets))
+            nbytes = B.slkv_evict_workspace_bytes(self.layout, out.layout, keep_last, budgets)
+            ws = self._workspace(("evict", nbytes), nbytes)
             B.slkv_evict_cache(self.layout, self._arrays, out.layout, out._arrays, keep_last, budgets, ws, kept_idx, stream)

@@ -13,14 +13,29 @@
 #include "device_utils.h"
 #include "launch.h"
 
+#include <cmath>
+
 namespace slkv {
 
-constexpr int kAttendWaves = 4, kAttendThreads = kAttendWaves * kWave;
+constexpr int kAttendThreads = 256;  // of the joining kernel
 constexpr int kTileRows = 32;        // rows of a tile of stored logits, and what parts of a segment are a multiple of
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+constexpr int kJoinPairs = 2048;     // (part, query) pairs of a segment whose references a workgroup holds in LDS
+
+// Segments of a launch: first row of their rooms.  A table of more than 64 says in which order the segments' parts are launched, and how many parts come before every
+// 16th segment of that order.
 template <int N>
-using AttendTab = SegWords<N, 2>;    // w[0] room of the segment (first row), w[1] parts before it (of the call)
+struct AttendTab {
+  static constexpr int kSegs = N;
+  static constexpr int kGroup = 16;
+  static constexpr bool kOrdered = N > 64;
+  int32_t nseg, seg0, ordered;       // ordered 0: as they stand
+  int32_t start[N + 1];
+  int32_t before[kOrdered ? (N + kGroup - 1) / kGroup : 1];
+  uint16_t order[kOrdered ? N : 1];
+};
+constexpr int kAttendSegs = 600;
 
 struct AttendArgs {
   const unsigned char *k, *v, *k_scale, *v_scale, *q;
@@ -30,11 +45,13 @@ struct AttendArgs {
   const float* w_in;
   float* w_out;
   float* part_o;                     // [part][R][D] sums of a part, relative to its reference
-  float* part_ml;                    // [part][2][R] reference (log2), sum
+  float* part_ml;                    // [part][R][2] reference (log2), sum
   float* logits;                     // x in log2 units: tiles of [R][32 rows]
   int32_t T, R;
+  int32_t tiles_each;                // room of a part in tiles of 32 rows
   int32_t row0;                      // first row of the call's rooms; logits of segment s, row j: tile (start - row0) / 32 + s + j / 32
   float c_log2;                      // log2(e) / sqrt(d)
+  double per_tiles_each;             // 1 / tiles_each
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -61,6 +78,43 @@ struct Attend {
   struct KRegs { uint32_t w[kTiles][kKWords]; uint32_t s[kTiles]; };
   struct VRegs { uint32_t w[kEach][kVWords]; uint32_t s[kEach]; };
 
+  // The rows of a part as buffers: what is beyond their end reads as 0, whatever is there.  The lane's place moves by whole steps; tiles and rows of a step are
+  // constant offsets of the loads.
+  struct Rows { __amdgpu_buffer_rsrc_t k, v, ks, vs; };
+  struct Place { uint32_t k, v, ks, vs; };
+
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const unsigned char* p, int64_t first, int rows, int row_bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(p + first * row_bytes), 0, rows * row_bytes, 0x00027000);
+  }
+  static __device__ __forceinline__ Rows rows_of(const AttendArgs& a, int64_t first, int rows) {
+    Rows r;
+    r.k = buffer(a.k, first, rows, kRowBytes);
+    r.v = buffer(a.v, first, rows, kRowBytes);
+    if constexpr (KIND == SLKV_BF16_KV_MXFP4) {
+      r.ks = buffer(a.k_scale, first, rows, kScales);
+      r.vs = buffer(a.v_scale, first, rows, kScales);
+    }
+    return r;
+  }
+  static __device__ __forceinline__ Place place_of(int step, int lane) {
+    const int c = lane & 15, g = lane >> 4;
+    const uint32_t krow = step * kStep + c / 4 * kEach + c % 4, vrow = step * kStep + g * kEach;
+    Place p;
+    p.k = krow * kRowBytes + g * (KIND == SLKV_BF16_KV_MXFP4 ? kRowBytes / 4 : 16);
+    p.v = vrow * kRowBytes + c * (kRowBytes / 16);
+    p.ks = krow * kScales + g * kScales / 4;
+    p.vs = vrow * kScales + c * kVD / kScaleBlock;
+    return p;
+  }
+  static __device__ __forceinline__ void advance(Place& p, int steps) {
+    p.k += steps * kStep * kRowBytes;
+    p.v += steps * kStep * kRowBytes;
+    if constexpr (KIND == SLKV_BF16_KV_MXFP4) {
+      p.ks += steps * kStep * kScales;
+      p.vs += steps * kStep * kScales;
+    }
+  }
+
   // dims that lane group g multiplies in product p (of 8 dims; fp32: one dim each)
   static __device__ __forceinline__ int dim_of(int p, int g) {
     if constexpr (kF32) return p / 4 * 16 + g * 4 + p % 4;
@@ -69,40 +123,36 @@ struct Attend {
     else return p * 32 + g * 8;
   }
 
-  static __device__ __forceinline__ void load_k(KRegs& r, const AttendArgs& a, int64_t base, int key0, int last, int lane) {
-    const int rho = lane & 15, g = lane >> 4;
+  static __device__ __forceinline__ void load_k(KRegs& r, const Rows& rows, const Place& p) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const int64_t row = base + min(key0 + rho / 4 * kEach + t * 4 + rho % 4, last);
-      const unsigned char* p = a.k + row * kRowBytes;
       if constexpr (KIND == SLKV_BF16_KV_MXFP4) {
-        if constexpr (kKWords == 4) *(u32x4*)r.w[t] = *(const u32x4*)(p + g * 16);
-        else *(u32x2*)r.w[t] = *(const u32x2*)(p + g * 8);
-        r.s[t] = a.k_scale[row * kScales + g * kScales / 4];
+        if constexpr (kKWords == 4) *(u32x4*)r.w[t] = __builtin_amdgcn_raw_buffer_load_b128(rows.k, p.k + t * 4 * kRowBytes, 0, 0);
+        else *(u32x2*)r.w[t] = __builtin_amdgcn_raw_buffer_load_b64(rows.k, p.k + t * 4 * kRowBytes, 0, 0);
+        r.s[t] = __builtin_amdgcn_raw_buffer_load_b8(rows.ks, p.ks + t * 4 * kScales, 0, 0);
       } else {
 #pragma unroll
-        for (int i = 0; i < kKWords / 4; ++i) *(u32x4*)(r.w[t] + i * 4) = *(const u32x4*)(p + i * 64 + g * 16);
+        for (int i = 0; i < kKWords / 4; ++i)
+          *(u32x4*)(r.w[t] + i * 4) = __builtin_amdgcn_raw_buffer_load_b128(rows.k, p.k + t * 4 * kRowBytes + i * 64, 0, 0);
       }
     }
   }
 
-  static __device__ __forceinline__ void load_v(VRegs& r, const AttendArgs& a, int64_t base, int key0, int last, int lane) {
-    const int c = lane & 15, g = lane >> 4;
+  static __device__ __forceinline__ void load_v(VRegs& r, const Rows& rows, const Place& p) {
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-      const int64_t row = base + min(key0 + g * kEach + j, last);
-      const unsigned char* p = a.v + row * kRowBytes + c * (kRowBytes / 16);
+      const uint32_t at = p.v + j * kRowBytes;
       if constexpr (kRowBytes / 16 == 2) {
-        r.w[j][0] = *(const uint16_t*)p;
+        r.w[j][0] = __builtin_amdgcn_raw_buffer_load_b16(rows.v, at, 0, 0);
       } else if constexpr (kVWords == 1) {
-        r.w[j][0] = *(const uint32_t*)p;
+        r.w[j][0] = __builtin_amdgcn_raw_buffer_load_b32(rows.v, at, 0, 0);
       } else if constexpr (kVWords == 2) {
-        *(u32x2*)r.w[j] = *(const u32x2*)p;
+        *(u32x2*)r.w[j] = __builtin_amdgcn_raw_buffer_load_b64(rows.v, at, 0, 0);
       } else {
 #pragma unroll
-        for (int i = 0; i < kVWords / 4; ++i) *(u32x4*)(r.w[j] + i * 4) = *(const u32x4*)(p + i * 16);
+        for (int i = 0; i < kVWords / 4; ++i) *(u32x4*)(r.w[j] + i * 4) = __builtin_amdgcn_raw_buffer_load_b128(rows.v, at + i * 16, 0, 0);
       }
-      if constexpr (KIND == SLKV_BF16_KV_MXFP4) r.s[j] = a.v_scale[row * kScales + c * kVD / kScaleBlock];
+      if constexpr (KIND == SLKV_BF16_KV_MXFP4) r.s[j] = __builtin_amdgcn_raw_buffer_load_b8(rows.vs, p.vs + j * kScales, 0, 0);
     }
   }
 
@@ -137,26 +187,12 @@ struct Attend {
     }
   }
 
-  // Row j of the lane's block of V as kVD / 2 pairs of wide elements.
-  static __device__ __forceinline__ void v_pairs(const VRegs& r, int j, uint32_t (&o)[kVD / 2]) {
-    if constexpr (KIND == SLKV_BF16_KV_MXFP4) {
-      const float s = scale_of(r.s[j]);
-      o[0] = fp4_pair<0>(r.w[j][0], s);
-      o[1] = fp4_pair<1>(r.w[j][0], s);
-      if constexpr (kVD == 8) {
-        o[2] = fp4_pair<2>(r.w[j][0], s);
-        o[3] = fp4_pair<3>(r.w[j][0], s);
-      }
-    } else if constexpr (KIND == SLKV_BF16_KV_FP8) {
-#pragma unroll
-      for (int i = 0; i < kVD / 4; ++i) {
-        o[i * 2] = fp8_pair<false>(r.w[j][i]);
-        o[i * 2 + 1] = fp8_pair<true>(r.w[j][i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVD / 2; ++i) o[i] = r.w[j][i];
-    }
+  // Pair U of row j of the lane's block of V: wide elements of dims c kVD + 2 U and the next.
+  template <int U>
+  static __device__ __forceinline__ uint32_t v_pair(const VRegs& r, int j) {
+    if constexpr (KIND == SLKV_BF16_KV_MXFP4) return fp4_pair<U>(r.w[j][0], scale_of(r.s[j]));
+    else if constexpr (KIND == SLKV_BF16_KV_FP8) return fp8_pair<U % 2 == 1>(r.w[j][U / 2]);
+    else return r.w[j][U];
   }
 
   // Pairs of wide elements with 0 in the place of infinities and NaN.
@@ -184,24 +220,141 @@ struct Attend {
   }
 };
 
+template <int KIND>
+__device__ __forceinline__ void store_out(unsigned char* dst, f32x4 o) {   // four neighbouring outputs
+  if constexpr (KIND == SLKV_F32) {
+    *(f32x4*)dst = o;
+  } else if constexpr (KIND == SLKV_F16) {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    *(f16x4*)dst = __builtin_convertvector(o, f16x4);
+  } else {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *(bf16x4*)dst = __builtin_convertvector(o, bf16x4);
+  }
+}
+
+// A query's log-sum-exp in log2 units, +infinity where it sees no row (its weights come out 0), and what the caller gets.
+__device__ __forceinline__ float lse_of(float top, float total, bool none) { return none ? INFINITY : total > 0.f ? top + __builtin_amdgcn_logf(total) : NAN; }
+__device__ __forceinline__ float lse_out(float lse2, bool none) { return none ? -INFINITY : lse2 * kLn2; }
+__device__ __forceinline__ f32x4 output_of(f32x4 o, float total, bool none) {
+  const float inv = 1.f / total;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = none ? 0.f : total > 0.f ? o[e] * inv : NAN;
+  return o;
+}
+
+// Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread; lse: of its R queries, in LDS.  The first rows' numbers can
+// be asked for before the log-sum-exp is known.
+constexpr int kAheadQueries = 4;
+struct WeightsAhead { f32x4 x[kAheadQueries], w; };
+__device__ __forceinline__ const float* logits_of(const AttendArgs& a, int tile, int j) {
+  return a.logits + (int64_t)(tile + j / kTileRows) * a.R * kTileRows + j % kTileRows;
+}
+__device__ __forceinline__ void load_weights(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j, int j1) {
+  if (j >= j1) return;
+  const float* l = logits_of(a, tile, j);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h.w[e] = a.w_in && j + e < j1 ? a.w_in[start + j + e] : 0.f;
+#pragma unroll
+  for (int r = 0; r < kAheadQueries; ++r)
+    if (r < a.R) h.x[r] = *(const f32x4*)(l + r * kTileRows);
+}
+template <int NT>
+__device__ __forceinline__ void add_weights(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j0, int j1, const float* lse) {
+  for (int j = j0 + 4 * (int)threadIdx.x; j < j1; j += 4 * NT) {
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](f32x4 x, float l) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += exp2_fast(x[e] - l);
+    };
+#pragma unroll
+    for (int r = 0; r < kAheadQueries; ++r)
+      if (r < a.R) add(h.x[r], lse[r]);
+    const float* l = logits_of(a, tile, j);
+#pragma unroll 4
+    for (int r = kAheadQueries; r < a.R; ++r) add(*(const f32x4*)(l + r * kTileRows), lse[r]);
+    s += h.w;
+    load_weights(h, a, start, tile, j + 4 * NT, j1);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < j1) a.w_out[start + j + e] = s[e];
+  }
+}
+
+// The segment of a workgroup, which is a part of one: segments have max(1, ceil(room / rows_each)) parts.  One wave looks it up and reads the length for all: the
+// table is read from the kernel's arguments, where a workgroup that goes through 3 KB of it with every wave waits up to 20 us behind the others (768 workgroups; this way 1 to 2).
+struct Where { int seg, start, part, parts, first, n, tile; };
+template <class TAB>
+__device__ __forceinline__ Where find_part(const AttendArgs& a, const TAB& tab, Where& shared) {
+  if (threadIdx.x < kWave) {
+    const int lane = threadIdx.x, part_id = blockIdx.x;
+    int s = lane, first0 = 0;
+    bool in = lane < tab.nseg;
+    if constexpr (TAB::kOrdered) {
+      const int groups = (tab.nseg + TAB::kGroup - 1) / TAB::kGroup;
+      const int b = tab.before[min(lane, groups - 1)];
+      const int g = __popcll(__ballot(lane < groups && b <= part_id)) - 1;
+      first0 = __builtin_amdgcn_readlane(b, g);
+      in = lane < TAB::kGroup && g * TAB::kGroup + lane < tab.nseg;
+      s = min(g * TAB::kGroup + lane, tab.nseg - 1);
+      if (tab.ordered) s = tab.order[s];
+    }
+    s = min(s, tab.nseg - 1);
+    const int in_use = a.lengths ? a.lengths[tab.seg0 + s] : 0, at = tab.start[s], room = tab.start[s + 1] - at;
+    // tiles of 32 rows: below 2^26, and 2^15 a part at most, so a double's quotient of (numerator + 1/2) is never on the wrong side of a whole number
+    const int tiles = (room + kTileRows - 1) / kTileRows;
+    const int parts = in ? max(1, (int)((tiles + a.tiles_each - 1 + 0.5) * a.per_tiles_each)) : 0;
+    const int first = first0 + (int)wave_incl_scan((uint32_t)parts) - parts;
+    if (parts && first <= part_id && part_id < first + parts) {
+      Where w;
+      w.seg = tab.seg0 + s;
+      w.start = at;
+      w.part = part_id - first;
+      w.parts = parts;
+      w.first = first;
+      w.n = a.lengths ? min(max(in_use, 0), room) : room;
+      w.tile = (at - a.row0) / kTileRows + w.seg;
+      shared = w;
+    }
+  }
+  __syncthreads();
+  Where w;
+  w.seg = __builtin_amdgcn_readfirstlane(shared.seg);
+  w.start = __builtin_amdgcn_readfirstlane(shared.start);
+  w.part = __builtin_amdgcn_readfirstlane(shared.part);
+  w.parts = __builtin_amdgcn_readfirstlane(shared.parts);
+  w.first = __builtin_amdgcn_readfirstlane(shared.first);
+  w.n = __builtin_amdgcn_readfirstlane(shared.n);
+  w.tile = __builtin_amdgcn_readfirstlane(shared.tile);
+  return w;
+}
+
 // RT: tiles of 16 queries.
-template <int KIND, int D, int RT, class TAB>
-__global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel(const AttendArgs a, const TAB tab) {
+constexpr int attend_waves_per_cu(int rt) { return rt == 4 ? 4 : 8; }
+template <int KIND, int D, int RT, int W, class TAB>
+__global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend_kernel(const AttendArgs a, const TAB tab) {
   using A = Attend<KIND, D>;
   constexpr int kProducts = A::kF32 ? D / 4 : D / 32, kVD = A::kVD, kEach = A::kEach;
-  __shared__ float sh_o[kAttendWaves][16][D + 4];
-  __shared__ float sh_m[kAttendWaves][16 * RT], sh_l[kAttendWaves][16 * RT], sh_lse[16 * RT];
-  const int part_id = (int)blockIdx.x + tab.w[1][0];
-  const int i = find_segment_wave(tab.nseg, part_id, [&](int s) { return tab.w[1][s]; });
-  const int seg = tab.seg0 + i, parts = tab.w[1][i + 1] - tab.w[1][i], part = part_id - tab.w[1][i];
-  const int start = tab.w[0][i];
-  const int n = rows_in_use(a.lengths, seg, tab.w[0][i + 1] - start);
-  const int each = part_rows(n, parts);
+  constexpr bool kAhead = RT * D <= 128;               // the next step's rows are on their way during a step (more tiles of queries leave no registers for them)
+  __shared__ __align__(16) float sh_o[W][16][D + 4];
+  __shared__ float sh_m[W][16 * RT], sh_l[W][16 * RT];
+  __shared__ float sh_lse[16 * RT], sh_total[16 * RT];
+  __shared__ Where sh_at;
+  const Where at = find_part(a, tab, sh_at);
+  const int seg = at.seg, start = at.start, part = at.part, n = at.n;
+  const int each = part_rows(n, at.parts);
   const int begin = part * each, end = min(n, begin + each);
   if (begin >= end && part > 0) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = threadIdx.x % kWave;
   const int rq = lane & 15, g = lane >> 4, R = a.R, T = a.T;
   const int64_t base = start;
+
+  const typename A::Rows rows = A::rows_of(a, base + begin, end - begin);
+  typename A::KRegs kr0, kr1;
+  typename A::VRegs vr0, vr1;
+  typename A::Place place = A::place_of(wave, lane);
+  A::load_k(kr0, rows, place);
+  A::load_v(vr0, rows, place);
 
   u32x4 q[RT][A::kF32 ? 1 : kProducts];
   float qf[RT][A::kF32 ? kProducts : 1];
@@ -219,7 +372,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel
       for (int u = 0; u < kProducts; ++u) q[rt][u] = *(const u32x4*)(p + A::dim_of(u, g) * 2);
     }
   }
-  const int64_t tile_seg = (int64_t)(start - a.row0) / kTileRows + seg;
+  const int64_t tile_seg = at.tile;
 
   float ref[RT], sum[RT];
   f32x4 acc[RT][kVD];
@@ -227,8 +380,135 @@ __global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel
   // the rounding of the output).  An infinite value would make NaN of the second one's zero, and values of rows that a query does not see would reach it through
   // a weight of zero: sums that come out not finite are taken again, with such values kept out of the second number's products and, where not every query
   // sees the row, out of both.
-  bool careful = false;
-  for (;;) {
+  auto step = [&](auto careful_c, const typename A::KRegs& kr, const typename A::VRegs& vr, const int key0) __attribute__((always_inline)) {
+    constexpr bool careful = decltype(careful_c)::value;
+    f32x4 x[RT][A::kTiles];
+#pragma unroll
+    for (int t = 0; t < A::kTiles; ++t) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) x[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < kProducts; ++u) {
+        if constexpr (A::kF32) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr.w[t][u]), qf[rt][u], x[rt][t], 0, 0, 0);
+        } else {
+          const u32x4 ko = A::k_operand(kr, t, u);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) x[rt][t] = A::mfma(ko, q[rt][u], x[rt][t]);
+        }
+      }
+    }
+    const int mine = key0 + g * kEach;                 // the lane's rows: mine .. mine + kEach - 1
+    const bool tail = key0 + A::kStep > min(end, n - T + 1);
+    float p[RT][kEach];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) p[rt][j] = x[rt][j / 4][j % 4] * a.c_log2;
+      if (tail) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+          if (mine + j >= sees[rt]) p[rt][j] = -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) top = fmaxf(top, p[rt][j]);
+      if (a.logits && rt * 16 + rq < R) {
+        float* l = a.logits + ((tile_seg + key0 / kTileRows) * R + rt * 16 + rq) * kTileRows + mine % kTileRows;
+#pragma unroll
+        for (int j = 0; j < kEach; j += 4) *(f32x4*)(l + j) = f32x4{p[rt][j], p[rt][j + 1], p[rt][j + 2], p[rt][j + 3]};
+      }
+      if (__ballot(top > ref[rt] + A::kAbove)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(ref[rt], top - A::kBelow);
+        const float f = ref[rt] == -INFINITY ? 0.f : exp2_fast(ref[rt] - now);
+        // (sums of a NaN stay one)
+        sum[rt] *= f;
+#pragma unroll
+        for (int m = 0; m < kVD; ++m) acc[rt][m] *= f;
+        ref[rt] = now;
+      }
+      const float from = ref[rt] == -INFINITY ? 0.f : ref[rt];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        p[rt][j] = exp2_fast(p[rt][j] - from);
+        sum[rt] += p[rt][j];
+      }
+    }
+    uint32_t hold = ~0u;                               // bit j: the lane's row j takes part in the products
+    if (careful && tail) {
+      // rows that not every query sees: one at a time, to the queries that see it
+      const int from = max(key0, n - T + 1), to = min(key0 + A::kStep, end);
+      for (int key = from; key < to; ++key) {
+        const int holder = (key - key0) / kEach, which = (key - key0) % kEach;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float w = 0.f;
+#pragma unroll
+          for (int j = 0; j < kEach; ++j)
+            if (j == which) w = p[rt][j];
+          w = __shfl(w, holder * 16 + rq);
+          if (key < sees[rt]) {
+#pragma unroll
+            for (int m = 0; m < kVD; ++m)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[rt][m][e] += w * A::value(a, base + key, (g * 4 + e) * kVD + m);
+          }
+        }
+      }
+      hold = mine >= from ? 0u : mine + kEach <= from ? ~0u : (1u << (from - mine)) - 1u;
+    }
+    if constexpr (A::kF32) {
+#pragma unroll
+      for (int m = 0; m < kVD; ++m)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          const float v = !careful || hold >> j & 1 ? __uint_as_float(vr.w[j][m]) : 0.f;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[rt][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rt][j], acc[rt][m], 0, 0, 0);
+        }
+    } else {
+      u32x4 hi[RT], lo[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t h, l;
+          A::split(p[rt][2 * j], p[rt][2 * j + 1], h, l);
+          hi[rt][j] = h;
+          lo[rt][j] = l;
+        }
+      auto product = [&](auto u_c) __attribute__((always_inline)) {
+        constexpr int u = decltype(u_c)::value;
+        uint32_t pair[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          pair[j] = A::template v_pair<u>(vr, j);
+          if constexpr (careful) pair[j] = hold >> j & 1 ? pair[j] : 0u;
+        }
+#pragma unroll
+        for (int m = 2 * u; m < 2 * u + 2; ++m) {
+          u32x4 vo;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) vo[j] = __builtin_amdgcn_perm(pair[2 * j + 1], pair[2 * j], m % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[rt][m] = A::mfma(vo, hi[rt], acc[rt][m]);
+          if constexpr (careful) vo = A::finite(vo);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[rt][m] = A::mfma(vo, lo[rt], acc[rt][m]);
+        }
+      };
+      product(std::integral_constant<int, 0>{});
+      product(std::integral_constant<int, 1>{});
+      if constexpr (kVD == 8) {
+        product(std::integral_constant<int, 2>{});
+        product(std::integral_constant<int, 3>{});
+      }
+    }
+  };
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       ref[rt] = -INFINITY;
@@ -236,147 +516,47 @@ __global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel
 #pragma unroll
       for (int m = 0; m < kVD; ++m) acc[rt][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int key0 = begin + wave * A::kStep; key0 < end; key0 += kAttendWaves * A::kStep) {
-      typename A::KRegs kr;
-      typename A::VRegs vr;
-      A::load_k(kr, a, base, key0, end - 1, lane);
-      A::load_v(vr, a, base, key0, end - 1, lane);
-      f32x4 x[RT][A::kTiles];
-#pragma unroll
-      for (int t = 0; t < A::kTiles; ++t) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) x[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < kProducts; ++u) {
-          if constexpr (A::kF32) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr.w[t][u]), qf[rt][u], x[rt][t], 0, 0, 0);
-          } else {
-            const u32x4 ko = A::k_operand(kr, t, u);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) x[rt][t] = A::mfma(ko, q[rt][u], x[rt][t]);
-          }
-        }
-      }
-      const int mine = key0 + g * kEach;               // the lane's rows: mine .. mine + kEach - 1
-      const bool tail = key0 + A::kStep > min(end, n - T + 1);
-      float p[RT][kEach];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          p[rt][j] = x[rt][j / 4][j % 4] * a.c_log2;
-          if (tail && mine + j >= sees[rt]) p[rt][j] = -INFINITY;
-          top = fmaxf(top, p[rt][j]);
-        }
-        if (a.logits && rt * 16 + rq < R) {
-          float* l = a.logits + ((tile_seg + key0 / kTileRows) * R + rt * 16 + rq) * kTileRows + mine % kTileRows;
-#pragma unroll
-          for (int j = 0; j < kEach; j += 4) *(f32x4*)(l + j) = f32x4{p[rt][j], p[rt][j + 1], p[rt][j + 2], p[rt][j + 3]};
-        }
-        if (__ballot(top > ref[rt] + A::kAbove)) {
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float now = fmaxf(ref[rt], top - A::kBelow);
-          const float f = ref[rt] == -INFINITY ? 0.f : exp2_fast(ref[rt] - now);
-          // (sums of a NaN stay one)
-          sum[rt] *= f;
-#pragma unroll
-          for (int m = 0; m < kVD; ++m) acc[rt][m] *= f;
-          ref[rt] = now;
-        }
-        const float at = ref[rt] == -INFINITY ? 0.f : ref[rt];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          p[rt][j] = exp2_fast(p[rt][j] - at);
-          sum[rt] += p[rt][j];
-        }
-      }
-      // rows beyond the end were loaded from the last one
-      if (key0 + A::kStep > end) {
-#pragma unroll
-        for (int j = 0; j < kEach; ++j)
-          if (mine + j >= end) {
-#pragma unroll
-            for (int u = 0; u < A::kVWords; ++u) vr.w[j][u] = 0;
-            if constexpr (KIND == SLKV_BF16_KV_MXFP4) vr.s[j] = 127;
-          }
-      }
-      if (careful && tail) {
-        // rows that not every query sees: one at a time, to the queries that see it
-        const int from = max(key0, n - T + 1), to = min(key0 + A::kStep, end);
-        for (int key = from; key < to; ++key) {
-          const int holder = (key - key0) / kEach, which = (key - key0) % kEach;
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            float w = 0.f;
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-              if (j == which) w = p[rt][j];
-            w = __shfl(w, holder * 16 + rq);
-            if (key < sees[rt]) {
-#pragma unroll
-              for (int m = 0; m < kVD; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[rt][m][e] += w * A::value(a, base + key, (g * 4 + e) * kVD + m);
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < kEach; ++j)
-          if (mine + j >= from) {
-#pragma unroll
-            for (int u = 0; u < A::kVWords; ++u) vr.w[j][u] = 0;
-            if constexpr (KIND == SLKV_BF16_KV_MXFP4) vr.s[j] = 127;
-          }
-      }
-      if constexpr (A::kF32) {
-#pragma unroll
-        for (int m = 0; m < kVD; ++m)
-#pragma unroll
-          for (int j = 0; j < kEach; ++j)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-              acc[rt][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr.w[j][m]), p[rt][j], acc[rt][m], 0, 0, 0);
-      } else {
-        uint32_t pair[kEach][kVD / 2];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) A::v_pairs(vr, j, pair[j]);
-        u32x4 hi[RT], lo[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t h, l;
-            A::split(p[rt][2 * j], p[rt][2 * j + 1], h, l);
-            hi[rt][j] = h;
-            lo[rt][j] = l;
-          }
-#pragma unroll
-        for (int m = 0; m < kVD; ++m) {
-          u32x4 vo;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            vo[j] = __builtin_amdgcn_perm(pair[2 * j + 1][m / 2], pair[2 * j][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][m] = A::mfma(vo, hi[rt], acc[rt][m]);
-          if (careful) vo = A::finite(vo);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][m] = A::mfma(vo, lo[rt], acc[rt][m]);
-        }
-      }
+  };
+  using std::integral_constant;
+  constexpr int kStride = W * A::kStep;
+  clear();
+  if constexpr (kAhead) {
+    for (int key0 = begin + wave * A::kStep; key0 < end; key0 += kStride) {
+      A::advance(place, W);                 // (beyond the end nothing is fetched)
+      A::load_k(kr1, rows, place);
+      A::load_v(vr1, rows, place);
+      step(integral_constant<bool, false>{}, kr0, vr0, key0);
+      key0 += kStride;
+      if (key0 >= end) break;
+      A::advance(place, W);
+      A::load_k(kr0, rows, place);
+      A::load_v(vr0, rows, place);
+      step(integral_constant<bool, false>{}, kr1, vr1, key0);
     }
-    if (careful) break;
-    bool finite = true;
+  } else {
+    for (int key0 = begin + wave * A::kStep; key0 < end; key0 += kStride) {
+      step(integral_constant<bool, false>{}, kr0, vr0, key0);
+      A::advance(place, W);
+      A::load_k(kr0, rows, place);
+      A::load_v(vr0, rows, place);
+    }
+  }
+  bool finite = true;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+  for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int m = 0; m < kVD; ++m)
+    for (int m = 0; m < kVD; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) finite = finite && fabsf(acc[rt][m][e]) < INFINITY;
-    if (!__ballot(!finite)) break;
-    careful = true;
+      for (int e = 0; e < 4; ++e) finite = finite && fabsf(acc[rt][m][e]) < INFINITY;
+  if (__ballot(!finite)) {
+    clear();
+    place = A::place_of(wave, lane);
+    for (int key0 = begin + wave * A::kStep; key0 < end; key0 += kStride) {
+      A::load_k(kr0, rows, place);
+      A::load_v(vr0, rows, place);
+      step(integral_constant<bool, true>{}, kr0, vr0, key0);
+      A::advance(place, W);
+    }
   }
 
   // the waves' references and sums
@@ -391,16 +571,16 @@ __global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel
     }
   }
   __syncthreads();
-  const int rows_each = max(each, 1), active = (n + rows_each - 1) / rows_each;
+  const int active = each ? (n + each - 1) / each : 0;
   const bool whole = active <= 1;
+  float* const ml = a.part_ml + (int64_t)blockIdx.x * 2 * R;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float top = -INFINITY, total = 0.f;
+    float top = -INFINITY, total = 0.f, mine = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, sh_m[w][rt * 16 + rq]);
-    float mine = 0.f;
+    for (int w = 0; w < W; ++w) top = fmaxf(top, sh_m[w][rt * 16 + rq]);
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float m = sh_m[w][rt * 16 + rq], l = sh_l[w][rt * 16 + rq];
       // (a wave that saw nothing has a sum of 0, or NaN where a product was NaN)
       const float f = m == -INFINITY ? 1.f : exp2_fast(m - top);
@@ -408,48 +588,33 @@ __global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel
       if (w == wave) mine = f;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int m = 0; m < kVD; ++m) sh_o[wave][rq][(g * 4 + e) * kVD + m] = acc[rt][m][e] * mine;
-    }
+      for (int m = 0; m < kVD; m += 4)
+        *(f32x4*)&sh_o[wave][rq][(g * 4 + e) * kVD + m] = f32x4{acc[rt][m][e], acc[rt][m + 1][e], acc[rt][m + 2][e], acc[rt][m + 3][e]} * mine;
     const int r = rt * 16 + rq;
     if (wave == 0 && g == 0 && r < R) {
+      const bool none = n - T + 1 + r % T <= 0;
+      sh_total[r] = total;
       if (whole) {
-        const float lse2 = total > 0.f ? top + __builtin_amdgcn_logf(total) : (n - T + 1 + r % T > 0 ? NAN : INFINITY);
+        const float lse2 = lse_of(top, total, none);
         sh_lse[r] = lse2;
-        if (a.lse) a.lse[(int64_t)seg * R + r] = lse2 == INFINITY && !(total > 0.f) ? -INFINITY : lse2 * kLn2;
+        if (a.lse) a.lse[(int64_t)seg * R + r] = lse_out(lse2, none);
       } else {
-        float* ml = a.part_ml + (int64_t)part_id * 2 * R;
-        ml[r] = top;
-        ml[R + r] = total;
+        *(f32x2*)(ml + 2 * r) = f32x2{top, total};
       }
-      sh_l[0][r] = total;
     }
     __syncthreads();
-    for (int idx = threadIdx.x; idx < 16 * D / 4; idx += kAttendThreads) {
+    for (int idx = threadIdx.x; idx < 16 * D / 4; idx += (W * kWave)) {
       const int r16 = idx / (D / 4), d0 = idx % (D / 4) * 4, row = rt * 16 + r16;
       if (row >= R) continue;
       f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kAttendWaves; ++w) o += *(const f32x4*)&sh_o[w][r16][d0];
-      if (!whole) {
-        *(f32x4*)(a.part_o + ((int64_t)part_id * R + row) * D + d0) = o;
-        continue;
-      }
-      const float l = sh_l[0][row];
-      const bool none = n - T + 1 + row % T <= 0;
-      const float inv = 1.f / l;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = none ? 0.f : l > 0.f ? o[e] * inv : NAN;
-      unsigned char* dst = a.out + ((int64_t)seg * R + row) * (D * (int)sizeof(typename A::wide));
-      if constexpr (A::kF32) {
-        *(f32x4*)(dst + d0 * 4) = o;
-      } else if constexpr (KIND == SLKV_F16) {
-        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-        *(f16x4*)(dst + d0 * 2) = __builtin_convertvector(o, f16x4);
+      for (int w = 0; w < W; ++w) o += *(const f32x4*)&sh_o[w][r16][d0];
+      if (whole) {
+        store_out<KIND>(a.out + (((int64_t)seg * R + row) * D + d0) * (int)sizeof(typename A::wide), output_of(o, sh_total[row], n - T + 1 + row % T <= 0));
       } else {
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        *(bf16x4*)(dst + d0 * 2) = __builtin_convertvector(o, bf16x4);
+        *(f32x4*)(a.part_o + ((int64_t)blockIdx.x * R + row) * D + d0) = o;
       }
     }
     __syncthreads();
@@ -457,107 +622,166 @@ __global__ __launch_bounds__(kAttendThreads, RT == 4 ? 1 : 2) void attend_kernel
   if (!whole || !a.w_out) return;
   __threadfence_block();
   __syncthreads();
-  for (int j = threadIdx.x; j < n; j += kAttendThreads) {
-    float w = a.w_in ? a.w_in[base + j] : 0.f;
-    const float* l = a.logits + (tile_seg + j / kTileRows) * R * kTileRows + j % kTileRows;
-    float s = 0.f;
-    for (int r = 0; r < R; ++r) s += exp2_fast(l[r * kTileRows] - sh_lse[r]);
-    a.w_out[base + j] = w + s;
-  }
+  WeightsAhead h;
+  load_weights(h, a, base, at.tile, 4 * (int)threadIdx.x, n);
+  add_weights<W * kWave>(h, a, base, at.tile, 0, n, sh_lse);
 }
 
-// Segments of more than one part: the parts put together, in their order, and the weights.  Part p of a segment finishes the queries p, p + active, .. and
-// the weights of its own rows; every workgroup adds up the references and sums of all parts, R pairs each.
+// Over `share` neighbouring lanes, 4 to 64, in every lane.
+template <class OP>
+__device__ __forceinline__ float reduce_lanes(float v, int share, OP op) {
+  auto move = [&](auto ctrl) __attribute__((always_inline)) { return __uint_as_float(dpp_move<decltype(ctrl)::value>(0u, __float_as_uint(v))); };
+  using std::integral_constant;
+  v = op(v, move(integral_constant<int, 0xb1>{}));     // quad_perm 1, 0, 3, 2
+  v = op(v, move(integral_constant<int, 0x4e>{}));     // quad_perm 2, 3, 0, 1
+  if (share >= 8) v = op(v, move(integral_constant<int, 0x141>{}));    // row_half_mirror
+  if (share >= 16) v = op(v, move(integral_constant<int, 0x140>{}));   // row_mirror
+  if (share >= 32) v = op(v, __shfl_xor(v, 16));
+  if (share >= 64) v = op(v, __shfl_xor(v, 32));
+  return v;
+}
+
+// Segments of more than one part: the parts put together, in their order.  The workgroup of part p of a segment adds up the references and sums of its R queries over
+// all parts, 256 / R lanes a query, 4 to 64, and finishes a slice of the outputs and the weights of the part's rows.  What it reads is asked for at once: behind the table
+// and the length there is one round trip.  (Two other ways were measured.  The workgroups of a segment waiting for each other in the launch above: 40 us instead of 34 for
+// one long history, whose memory traffic their meeting competes with, nothing gained elsewhere; the last one to arrive joining the segment alone: 25 to 40 % slower.)
+constexpr int kJoinFirst = 4;          // parts of an output that a thread asks for at once
 template <int KIND, int D, class TAB>
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a, const TAB tab) {
-  using A = Attend<KIND, D>;
-  __shared__ float sh_m[64], sh_l[64], sh_lse[64];
-  __shared__ float sh_o[kAttendThreads / (D / 4)][D];
-  const int part_id = (int)blockIdx.x + tab.w[1][0];
-  const int i = find_segment_wave(tab.nseg, part_id, [&](int s) { return tab.w[1][s]; });
-  const int seg = tab.seg0 + i, first = tab.w[1][i], parts = tab.w[1][i + 1] - first, part = part_id - first;
-  const int start = tab.w[0][i];
-  const int n = rows_in_use(a.lengths, seg, tab.w[0][i + 1] - start);
-  const int each = part_rows(n, parts);
-  const int active = each ? (n + each - 1) / each : 0;
+  __shared__ Where sh_at;
+  __shared__ float sh_lse[64], sh_top[64], sh_total[64], sh_factor[kJoinPairs];   // [part][query], where all fit
+  __shared__ f32x4 sh_o[kAttendThreads];
+  const Where w = find_part(a, tab, sh_at);
+  const int n = w.n, part = w.part, each = part_rows(n, w.parts), active = each ? (n + each - 1) / each : 0;
   if (active <= 1 || part >= active) return;
-  const int R = a.R, T = a.T, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const float* ml = a.part_ml + (int64_t)first * 2 * R;
-  for (int r = wave; r < R; r += kAttendWaves) {
-    float top = -INFINITY, l = 0.f;
-    for (int p = lane; p < active; p += kWave) top = fmaxf(top, ml[p * 2 * R + r]);
+  const int R = a.R, T = a.T, tid = threadIdx.x;
+  const float* ml = a.part_ml + (int64_t)w.first * 2 * R;
+  const float* po = a.part_o + (int64_t)w.first * R * D;
+  const bool fit = R * active <= kJoinPairs;
+  // the queries: `share` lanes each, a lane per part
+  const int share = R <= 4 ? 64 : R <= 8 ? 32 : R <= 16 ? 16 : R <= 32 ? 8 : 4;
+  const int r = tid / share, lane = tid % share;
+  f32x2 pair = f32x2{-INFINITY, 0.f};
+  if (r < R && lane < active) pair = *(const f32x2*)(ml + 2 * (lane * R + r));
+  // a slice of the outputs, four at a time: a thread per kJoinFirst parts of an output, as far as there are threads
+  const int all = R * (D / 4);
+  const int f0 = (int)((uint32_t)(all * part) / (uint32_t)active), f1 = (int)((uint32_t)(all * (part + 1)) / (uint32_t)active), mine = f1 - f0;
+  const int nf = max(min(mine, kAttendThreads), 1);
+  const int groups = min(kAttendThreads / nf, (active + kJoinFirst - 1) / kJoinFirst);
+  const int grp = tid / nf, fi = tid - grp * nf;
+  f32x4 x[kJoinFirst];
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    for (int p = lane; p < active; p += kWave) {
-      const float m = ml[p * 2 * R + r];
-      l += ml[p * 2 * R + R + r] * (m == -INFINITY ? 1.f : exp2_fast(m - top));
+  for (int k = 0; k < kJoinFirst; ++k) {
+    const int p = grp + k * groups;
+    if (grp < groups && fi < mine && p < active) x[k] = *(const f32x4*)(po + (int64_t)p * R * D + (f0 + fi) * 4);
+  }
+  WeightsAhead h;
+  const int end = min(n, (part + 1) * each);
+  if (a.w_out) load_weights(h, a, w.start, w.tile, part * each + 4 * tid, end);
+
+  auto factor_of = [](float m, float top) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : exp2_fast(m - top); };
+  float top = pair[0];
+  if (r < R)
+    for (int p = lane + share; p < active; p += share) top = fmaxf(top, ml[2 * (p * R + r)]);
+  top = reduce_lanes(top, share, [](float u, float v) { return fmaxf(u, v); });
+  float f = factor_of(pair[0], top), total = pair[1] * f;
+  if (r < R) {
+    if (fit && lane < active) sh_factor[lane * R + r] = f;
+    for (int p = lane + share; p < active; p += share) {
+      f = factor_of(ml[2 * (p * R + r)], top);
+      total += ml[2 * (p * R + r) + 1] * f;
+      if (fit) sh_factor[p * R + r] = f;
     }
-    l = wave_sum(l);
-    if (lane == 0) {
-      const bool none = n - T + 1 + r % T <= 0;
-      const float lse2 = l > 0.f ? top + __builtin_amdgcn_logf(l) : none ? INFINITY : NAN;
-      sh_m[r] = top;
-      sh_l[r] = l;
-      sh_lse[r] = lse2;
-      if (part == 0 && a.lse) a.lse[(int64_t)seg * R + r] = none ? -INFINITY : lse2 * kLn2;
-    }
+  }
+  total = reduce_lanes(total, share, [](float u, float v) { return u + v; });
+  if (r < R && lane == 0) {
+    const bool none = n - T + 1 + r % T <= 0;
+    const float lse2 = lse_of(top, total, none);
+    sh_top[r] = top;
+    sh_total[r] = total;
+    sh_lse[r] = lse2;
+    if (part == 0 && a.lse) a.lse[(int64_t)w.seg * R + r] = lse_out(lse2, none);
   }
   __syncthreads();
-  constexpr int kLanes = D / 4, kGroups = kAttendThreads / kLanes;
-  const int d0 = threadIdx.x % kLanes * 4, grp = threadIdx.x / kLanes;
-  for (int r = part; r < R; r += active) {
+  for (int f4 = f0; f4 < f1; f4 += kAttendThreads) {
+    const int at = f4 + fi, row = min(at / (D / 4), R - 1);
+    auto factor = [&](int p) __attribute__((always_inline)) { return fit ? sh_factor[p * R + row] : factor_of(ml[2 * (p * R + row)], sh_top[row]); };
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int p = grp; p < active; p += kGroups) {
-      const float m = ml[p * 2 * R + r];
-      const float f = m == -INFINITY ? 1.f : exp2_fast(m - sh_m[r]);
-      o += *(const f32x4*)(a.part_o + ((int64_t)(first + p) * R + r) * D + d0) * f;
-    }
-    *(f32x4*)&sh_o[grp][d0] = o;
-    __syncthreads();
-    if ((int)threadIdx.x < D) {
-      float s = 0.f;
+    if (grp < groups && at < f1) {
+      int p = grp;
+      if (f4 == f0) {
 #pragma unroll
-      for (int w = 0; w < kGroups; ++w) s += sh_o[w][threadIdx.x];
-      const float l = sh_l[r];
-      s = n - T + 1 + r % T <= 0 ? 0.f : l > 0.f ? s / l : NAN;
-      ((typename A::wide*)a.out)[((int64_t)seg * R + r) * D + threadIdx.x] = (typename A::wide)s;
+        for (int k = 0; k < kJoinFirst; ++k, p += groups)
+          if (p < active) o += x[k] * factor(p);
+      }
+#pragma unroll 4
+      for (; p < active; p += groups) o += *(const f32x4*)(po + (int64_t)p * R * D + at * 4) * factor(p);
     }
-    __syncthreads();
+    if (groups > 1) {                                  // (then this is the only round)
+      sh_o[tid] = o;
+      __syncthreads();
+      if (grp == 0)
+        for (int u = 1; u < groups; ++u) o += sh_o[u * nf + fi];
+    }
+    if (grp == 0 && at < f1)
+      store_out<KIND>(a.out + ((int64_t)w.seg * R * D + at * 4) * (int)sizeof(typename Kind<KIND>::wide),
+                      output_of(o, sh_total[row], n - T + 1 + row % T <= 0));
   }
-  if (!a.w_out) return;
-  const int64_t tile_seg = (int64_t)(start - a.row0) / kTileRows + seg;
-  const int end = min(n, (part + 1) * each);
-  for (int j = part * each + (int)threadIdx.x; j < end; j += kAttendThreads) {
-    const float w = a.w_in ? a.w_in[(int64_t)start + j] : 0.f;
-    const float* l = a.logits + (tile_seg + j / kTileRows) * R * kTileRows + j % kTileRows;
-    float s = 0.f;
-    for (int r = 0; r < R; ++r) s += exp2_fast(l[r * kTileRows] - sh_lse[r]);
-    a.w_out[(int64_t)start + j] = w + s;
-  }
+  if (a.w_out) add_weights<kAttendThreads>(h, a, w.start, w.tile, part * each, end, sh_lse);
 }
 
 // ------------------------------------------------------------------ host
 
 struct AttendPlan {
-  int64_t rows_each;                 // room rows of a part, about
-  int64_t parts;                     // of the whole call
-  bool split;                        // some segment has more than one
+  int64_t rows_each;                 // room rows of a part, at most: a multiple of 32
+  int64_t parts;                     // of a launch, the most
+  bool split;                        // some segment has more than one part
+  int waves;                         // of a workgroup
   size_t off_ml, off_o, off_logits, bytes;
 };
 
 static int64_t parts_of(const slkv_cache_desc* d, int64_t s, int64_t rows_each) {
-  return std::max<int64_t>(1, (d->h_offsets[s + 1] - d->h_offsets[s] + rows_each - 1) / rows_each);
+  const uint32_t room = (uint32_t)(d->h_offsets[s + 1] - d->h_offsets[s]);
+  return std::max<uint32_t>(1u, (room + (uint32_t)rows_each - 1) / (uint32_t)rows_each);
 }
 
 static AttendPlan plan_attend(const slkv_cache_desc* d, int T, bool weights) {
   AttendPlan p;
   const int64_t S = (int64_t)d->B * d->Hkv, rows = d->h_offsets[S] - d->h_offsets[0];
   const int64_t R = (int64_t)(d->Hq / d->Hkv) * T;
-  constexpr int64_t kPlaces = 2 * 256, kLeast = kAttendWaves * 32;
-  p.rows_each = std::max(kLeast, ((rows + kPlaces - 1) / kPlaces + kTileRows - 1) / kTileRows * kTileRows);
+  constexpr int64_t kMost = 1 << 20;                   // a part's bytes are a 32-bit number
+  auto round = [](int64_t n) { return (n + kTileRows - 1) / kTileRows * kTileRows; };
+  const double row_bytes = d->d * kind_bits(d->dtype) / 4;
+  const int rt = R <= 16 ? 1 : R <= 32 ? 2 : 4;
+  int64_t most = 0;
+  for (int64_t s = 0; s < S; ++s) most = std::max(most, d->h_offsets[s + 1] - d->h_offsets[s]);
+  // Eight waves a workgroup where segments are few and long: half as many parts to join (8 segments of 4224 rows 14.3 us, of 32 K 32.2; four waves 15.4, 32.3).  Four
+  // otherwise: two workgroups on a CU fill each other's beginnings and ends (128 segments of 270 to 3012 rows 22.9 us, 256 of E4M3 43.8; eight waves 23.5, 50.6).
+  p.waves = rt == 1 && S <= 64 && rows >= 32768 ? 8 : 4;
+  const int64_t places = 256 * attend_waves_per_cu(rt) / p.waves;
+  // Whole segments while the longest takes one workgroup no longer than all rows take the chip and a second launch that joins parts.  One workgroup: 10.2 ns a row of 512
+  // bytes, 4.9 of 136; the chip: 5 TB/s; the launch: 5 to 8 us.  (8 segments of 96 to 440 rows: whole 10.2 us, in parts 12.8; 8 of 1016 rows of 512 bytes: 15.3 and 12.5;
+  // 512 of 280 to 2189 rows of 136 bytes: 24.2 and 33.2.)
+  const double whole_us = most * (0.0035 * rt + row_bytes / 75e3), split_us = rows * row_bytes / 5e6 + 5;
+  if (most <= kMost && whole_us <= split_us) {
+    p.rows_each = std::max<int64_t>(kTileRows, round(most));
+  } else {
+    // The workgroups that are on the chip at once share the rows.  Segments end inside a part, so a part is made larger until all are on the chip.
+    p.rows_each = std::min(kMost, std::max<int64_t>(p.waves * 32, round((rows + places - 1) / places)));
+    for (int tries = 0; tries < 4 && S <= places / 4 * 3 && p.rows_each < kMost; ++tries) {
+      int64_t parts = 0;
+      for (int64_t s = 0; s < S; ++s) parts += parts_of(d, s, p.rows_each);
+      if (parts <= places) break;
+      p.rows_each = std::min(kMost, std::max(p.rows_each + kTileRows, round(p.rows_each * parts / (places + S / 4))));
+    }
+  }
   p.parts = 0;
-  for (int64_t s = 0; s < S; ++s) p.parts += parts_of(d, s, p.rows_each);
-  p.split = p.parts > S;
+  p.split = most > p.rows_each;
+  for (int64_t s0 = 0; s0 < S; s0 += kAttendSegs) {
+    int64_t here = 0;
+    for (int64_t s = s0; s < std::min<int64_t>(S, s0 + kAttendSegs); ++s) here += parts_of(d, s, p.rows_each);
+    p.parts = std::max(p.parts, here);
+  }
   size_t at = 0;
   auto take = [&](int64_t floats) {
     const size_t off = at;
@@ -569,6 +793,21 @@ static AttendPlan plan_attend(const slkv_cache_desc* d, int T, bool weights) {
   p.off_logits = take(weights ? (rows / kTileRows + S + 1) * kTileRows * R : 0);
   p.bytes = std::max<size_t>(at, 16);
   return p;
+}
+
+// The order in which a launch's whole segments begin: the longest first, by sixteenths of the longest.  Heads of unequal capacity come at the same places in every
+// sequence, so that in their own order long ones meet on a CU: 64 sequences of 8 heads with 270 to 2061 rows 31.0 us, sorted 25.0; 128 of shorter ones 130 and 87.
+template <class TAB>
+static void order_segments(TAB& tab, const AttendPlan& p) {
+  constexpr int kSteps = 16;
+  int from[kSteps + 1] = {};
+  uint8_t key[TAB::kSegs];
+  for (int i = 0; i < tab.nseg; ++i) {
+    key[i] = (uint8_t)(kSteps - 1 - (tab.start[i + 1] - tab.start[i]) * (int64_t)(kSteps - 1) / p.rows_each);
+    ++from[key[i] + 1];
+  }
+  for (int k = 0; k < kSteps; ++k) from[k + 1] += from[k];
+  for (int i = 0; i < tab.nseg; ++i) tab.order[from[key[i]]++] = (uint16_t)i;
 }
 
 static slkv_status attend_checks(const slkv_cache_desc* desc, int32_t T) {
@@ -603,7 +842,6 @@ extern "C" slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv
   for (const void* ptr : ptrs)
     if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);
   const AttendPlan p = plan_attend(desc, T, d_weight_out != nullptr);
-  if (p.parts >= (int64_t(1) << 31)) return fail(SLKV_ERR_BAD_ARG, "too many parts");
   if (workspace_bytes < p.bytes) return fail(SLKV_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, p.bytes);
   unsigned char* ws = (unsigned char*)d_workspace;
   const int64_t S = (int64_t)desc->B * desc->Hkv;
@@ -627,35 +865,38 @@ extern "C" slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv
   a.c_log2 = kLog2e / std::sqrt((float)desc->d);
   hipStream_t const stream = (hipStream_t)hip_stream;
 
-  int64_t before = 0;                                  // parts of the segments of earlier tables
+  a.tiles_each = (int32_t)(p.rows_each / kTileRows);
+  a.per_tiles_each = 1.0 / a.tiles_each;
   auto launch = [&](auto tab, int64_t s0, int64_t ns) {
     using TAB = decltype(tab);
     tab.nseg = (int32_t)ns;
     tab.seg0 = (int32_t)s0;
-    int64_t at = before;
-    bool split = false;
-    for (int64_t i = 0; i <= ns; ++i) {
-      tab.w[0][i] = (int32_t)desc->h_offsets[s0 + i];
-      tab.w[1][i] = (int32_t)at;
-      if (i == ns) break;
-      const int64_t parts = parts_of(desc, s0 + i, p.rows_each);
-      split = split || parts > 1;
-      at += parts;
+    for (int64_t i = 0; i <= ns; ++i) tab.start[i] = (int32_t)desc->h_offsets[s0 + i];
+    int64_t parts = 0;
+    if constexpr (TAB::kOrdered) {
+      tab.ordered = !p.split;
+      if (tab.ordered) order_segments(tab, p);
+      for (int64_t i = 0; i < ns; ++i) {
+        if (i % TAB::kGroup == 0) tab.before[i / TAB::kGroup] = (int32_t)parts;
+        parts += p.split ? parts_of(desc, s0 + i, p.rows_each) : 1;
+      }
+    } else {
+      for (int64_t i = 0; i < ns; ++i) parts += parts_of(desc, s0 + i, p.rows_each);
     }
-    const dim3 grid((unsigned)(at - before)), block(kAttendThreads);
-    before = at;
+    const dim3 grid((unsigned)parts);
     with_kind(desc->dtype, [&](auto kind) {
       auto with_dim = [&](auto dim) {
         constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
         {
           ScopedKernelTimer timer(SLKV_K_ATTEND);
-          if (a.R <= 16) SLKV_LAUNCH((attend_kernel<kKind, kDim, 1, TAB>), grid, block, 0, stream, a, tab);
-          else if (a.R <= 32) SLKV_LAUNCH((attend_kernel<kKind, kDim, 2, TAB>), grid, block, 0, stream, a, tab);
-          else SLKV_LAUNCH((attend_kernel<kKind, kDim, 4, TAB>), grid, block, 0, stream, a, tab);
+          if (a.R <= 16 && p.waves == 8) SLKV_LAUNCH((attend_kernel<kKind, kDim, 1, 8, TAB>), grid, dim3(8 * kWave), 0, stream, a, tab);
+          else if (a.R <= 16) SLKV_LAUNCH((attend_kernel<kKind, kDim, 1, 4, TAB>), grid, dim3(4 * kWave), 0, stream, a, tab);
+          else if (a.R <= 32) SLKV_LAUNCH((attend_kernel<kKind, kDim, 2, 4, TAB>), grid, dim3(4 * kWave), 0, stream, a, tab);
+          else SLKV_LAUNCH((attend_kernel<kKind, kDim, 4, 4, TAB>), grid, dim3(4 * kWave), 0, stream, a, tab);
         }
-        if (split) {
+        if (p.split) {
           ScopedKernelTimer timer(SLKV_K_ATTEND_JOIN);
-          SLKV_LAUNCH((attend_join_kernel<kKind, kDim, TAB>), grid, block, 0, stream, a, tab);
+          SLKV_LAUNCH((attend_join_kernel<kKind, kDim, TAB>), grid, dim3(kAttendThreads), 0, stream, a, tab);
         }
       };
       if (desc->d == 64) with_dim(std::integral_constant<int, 64>{});
@@ -664,6 +905,6 @@ extern "C" slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv
   };
   if (S <= kFewSegs) launch(AttendTab<kFewSegs>{}, 0, S);
   else
-    for (int64_t s0 = 0; s0 < S; s0 += kManySegs2) launch(AttendTab<kManySegs2>{}, s0, std::min<int64_t>(kManySegs2, S - s0));
+    for (int64_t s0 = 0; s0 < S; s0 += kAttendSegs) launch(AttendTab<kAttendSegs>{}, s0, std::min<int64_t>(kAttendSegs, S - s0));
   return launch_status("attend");
 }

@@ -30,7 +30,7 @@ struct SegWords {
   int32_t nseg, seg0;
   int32_t w[WORDS][N + 1];
 };
-constexpr int kFewSegs = 64, kManySegs2 = 440, kManySegs3 = 290;
+constexpr int kFewSegs = 64, kManySegs3 = 290;
 
 __device__ __forceinline__ int rows_in_use(const int32_t* lengths, int seg, int room) {
   return lengths ? min(max(lengths[seg], 0), room) : room;

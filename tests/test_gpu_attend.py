@@ -79,7 +79,7 @@ def test_no_lengths_is_full_rooms():
     assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
-@pytest.mark.parametrize("S", [63, 64, 65, 440, 441, 1000])
+@pytest.mark.parametrize("S", [63, 64, 65, 899, 900, 901, 2000])
 def test_segment_tables(S):
     rng = np.random.default_rng(S)
     lens = rng.integers(0, 40, S).tolist()
@@ -182,6 +182,24 @@ def test_same_bits_every_time_and_in_place(dtype):
     B.slkv_attend_cache(cache.layout, bare, q, o3, ws, l3, fresh)
     want = np.where(used.cpu().numpy(), f64(after) - f64(before), 0)
     close(f64(fresh), want, 2.0 ** -22 * (1 + f64(before)), "fresh weights")
+
+
+def test_three_streams_at_once():
+    """Calls that hold the chip together, a workspace each."""
+    rng = np.random.default_rng(14)
+    caches = [random_cache(rng, t, 1, 8, 4, 128, [3000 + 100 * i] * 8) for i, t in enumerate(("bf16", "bf16_kv8", "bf16_kv4"))]
+    qs = [normal(rng, (1, 32, 1, 128), "bf16") for _ in caches]
+    want = [run(c, q)[1:] for c, q in zip(caches, qs)]
+    streams = [torch.cuda.Stream() for _ in caches]
+    got = [[] for _ in caches]
+    for _ in range(20):
+        for c, q, s, g in zip(caches, qs, streams, got):
+            with torch.cuda.stream(s):
+                w = torch.full_like(c.weight, -1.0)
+                g.append((w,) + c.attend(q, weight=w))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(a, b) for one in g for a, b in zip(w, one))
 
 
 def test_other_stream():
