@@ -399,15 +399,12 @@ slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv_cache* cac
  * Their K, V (bit for bit), scales, positions and weights go to the segment's first rows of another cache `out`, whose
  * desc has the same dtype, B, Hq, Hkv, d and whose rooms hold min(room, max(C_h, w)) rows at least; out->d_lengths gets the counts.
  * w         >= 0: latest rows that always stay;  h_budgets [Hkv] host: C_h >= 0
- * out       out->d_lengths is required; d_pos and d_weight are carried where both caches have them.  No array of `out` may
- *           overlap one of `cache` (d_lengths may be the same array).
+ * out       out->d_lengths is required; d_pos and d_weight are carried where both caches have them.  No array of `out`, nor d_kept_idx, may
+ *           overlap one of `cache`.
  * d_kept_idx [rows of out] int32, may be NULL: the kept rows' numbers inside their segment, at the places of the rows of `out`
- * cache->d_weight is required.  Workspace: slkv_evict_workspace_bytes, scratch alone as above.
- * Errors: NULL, BAD_ARG, UNSUPPORTED, WORKSPACE, CAPACITY (a room of out), HIP. */
-slkv_status slkv_evict_workspace_bytes(const slkv_cache_desc* desc, const slkv_cache_desc* out_desc, int32_t w, const int32_t* h_budgets, size_t* bytes);
+ * cache->d_weight is required.  Errors: NULL, BAD_ARG, UNSUPPORTED, CAPACITY (a room of out), HIP. */
 slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const slkv_cache_desc* out_desc, const slkv_cache* out,
-                             int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx,
-                             void* d_workspace, size_t workspace_bytes, void* hip_stream);
+                             int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx, void* hip_stream);
 
 /* ------------------------------------------------------------------ kernel timing -----
  * Optional instrumentation for benchmarks: between slkv_profile_begin and slkv_profile_end

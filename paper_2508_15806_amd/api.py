@@ -161,8 +161,9 @@ class Cache:
 
     `offsets` [B * Hkv + 1]: the rooms.  The arrays are allocated unless they are given (k, v [rows, d], "bf16_kv4": [rows, d / 2] uint8 and
     k_scale, v_scale [rows, d / 32] uint8; lengths [B * Hkv], pos [rows] int32; weight [rows] fp32); given keys without lengths fill their
-    rooms.  positions, weights = False: a cache without these arrays.  Calls of one object share its workspace, as do replays of graphs
-    that captured them: each waits for the one before it, on whatever stream that was.  Make the first call of a kind outside a capture: it allocates the workspace."""
+    rooms.  positions, weights = False: a cache without these arrays.  Calls run on `stream`, or the current stream of the cache's device.  Those of one object share
+    its workspace, as do replays of graphs that captured them: each waits for the one before it, on whatever stream that was, and the object outlives them.
+    Make the first attend() of a kind outside a capture: it allocates the workspace."""
 
     def __init__(self, dtype, B_, Hq, Hkv, d, offsets, k=None, v=None, k_scale=None, v_scale=None, lengths=None, pos=None, weight=None,
                  device="cuda", positions=True, weights=True):
@@ -179,6 +180,7 @@ class Cache:
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._here = contextlib.nullcontext()
         if lengths is None:
             lengths = torch.zeros((S,), dtype=torch.int32, device=self.device) if k is None else torch.from_numpy(np.diff(offsets).astype(np.int32)).to(self.device)
         width = d // 2 if four else d
@@ -208,16 +210,20 @@ class Cache:
             raise ValueError("%s is not contiguous" % name)
         return t
 
-    def _on_device(self):
-        """The cache's device as the current one, where it is not."""
-        return contextlib.nullcontext() if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
+    def _on(self, stream):
+        """The call's stream as the current one, so that what it allocates belongs to it; without one, the cache's device, where it is not current."""
+        if stream is not None:
+            return torch.cuda.stream(stream)
+        return self._here if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
 
-    def _workspace(self, key, nbytes):
-        """A workspace for calls of one kind and size: never replaced, since a captured graph may hold it."""
-        ws = self._workspaces.get(key)
-        if ws is None:
-            ws = self._workspaces[key] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
-        return ws
+    def _attend_buffers(self, T, weights):
+        """Workspace of calls of one kind, and a tensor in the shape of their lse.  Never replaced: a captured graph may hold it."""
+        found = self._workspaces.get((T, weights))
+        if found is None:
+            nbytes = B.slkv_attend_workspace_bytes(self.layout, T, weights)
+            found = (torch.empty((nbytes,), dtype=torch.uint8, device=self.device), torch.empty((self.B, self.Hq, T), dtype=torch.float32, device=self.device))
+            self._workspaces[T, weights] = found
+        return found
 
     def fill(self, k_rows, v_rows, src_offsets, pos=None, stream=None):
         """The rows that a prefill kept (LayerCall's k_out, v_out, offsets, kept_idx) become the cache."""
@@ -228,8 +234,8 @@ class Cache:
             self._tensor(t, (t.shape[0], self.d), self.query_dtype, name)
         if pos is not None:
             self._tensor(pos, (max(pos.shape[0], rows),), torch.int32, "pos")
-        with self._on_device():
-            B.slkv_fill_cache(self.layout, self._arrays, src_offsets, k_rows, v_rows, pos, stream)
+        with self._on(stream):
+            B.slkv_fill_cache(self.layout, self._arrays, src_offsets, k_rows, v_rows, pos)
 
     def append(self, k, v, pos=None, at=None, stream=None):
         """k, v [B, Hkv, T, d] (any strides, rows contiguous), pos [B, T]: the next T tokens enter behind the rows in use, or behind the first at[s]
@@ -242,8 +248,8 @@ class Cache:
             self._tensor(pos, (self.B, shape[2]), torch.int32, "pos")
         if at is not None:
             self._tensor(at, (self.B * self.Hkv,), torch.int32, "at")
-        with self._on_device():
-            B.slkv_append_cache(self.layout, self._arrays, k, v, pos, at, stream)
+        with self._on(stream):
+            B.slkv_append_cache(self.layout, self._arrays, k, v, pos, at)
 
     def attend(self, q, out=None, lse=None, weight=None, stream=None):
         """q [B, Hq, T, d]: the queries of the T latest tokens, whose rows are in the cache.  Returns (out [B, Hq, T, d], lse [B, Hq, T] fp32).
@@ -253,31 +259,27 @@ class Cache:
         T = q.shape[2]
         shape = (self.B, self.Hq, T, self.d)
         self._tensor(q, shape, self.query_dtype, "q")
-        out = torch.empty(shape, dtype=self.query_dtype, device=self.device) if out is None else self._tensor(out, shape, self.query_dtype, "out")
-        lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
         if weight is None:
             weight = self.weight
         elif weight is False:
             weight = None
         else:
             self._tensor(weight, (self.rows_in_all,), torch.float32, "weight")
-        key = (T, weight is not None)
-        ws = self._workspaces.get(key)
-        with self._on_device():
-            if ws is None:
-                ws = self._workspace(key, B.slkv_attend_workspace_bytes(self.layout, T, weight is not None))
-            B.slkv_attend_cache(self.layout, self._arrays, q, out, ws, lse, weight, stream)
+        with self._on(stream):
+            ws, lse_like = self._attend_buffers(T, weight is not None)
+            out = torch.empty_like(q) if out is None else self._tensor(out, shape, self.query_dtype, "out")
+            lse = torch.empty_like(lse_like) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
+            B.slkv_attend_cache(self.layout, self._arrays, q, out, ws, lse, weight)
         return out, lse
 
     def rows(self, out_offsets, stream=None):
         """Every segment's latest out_offsets[s + 1] - out_offsets[s] rows as values: (k, v [rows, d], pos [rows] or None).  Output rows that have no
         row in the cache hold nothing in particular."""
         rows = int(out_offsets[-1])
-        k = torch.empty((rows, self.d), dtype=self.query_dtype, device=self.device)
-        v = torch.empty((rows, self.d), dtype=self.query_dtype, device=self.device)
-        pos = torch.empty((rows,), dtype=torch.int32, device=self.device) if self.pos is not None else None
-        with self._on_device():
-            B.slkv_cache_rows(self.layout, self._arrays, out_offsets, k, v, pos, stream)
+        with self._on(stream):
+            k, v = torch.empty((2, rows, self.d), dtype=self.query_dtype, device=self.device).unbind(0)
+            pos = torch.empty((rows,), dtype=torch.int32, device=self.device) if self.pos is not None else None
+            B.slkv_cache_rows(self.layout, self._arrays, out_offsets, k, v, pos)
         return k, v, pos
 
     def evict(self, budgets, keep_last, out, kept_idx=None, stream=None):
@@ -287,7 +289,5 @@ class Cache:
             self._tensor(kept_idx, (out.rows_in_all,), torch.int32, "kept_idx")
         if out.device != self.device:
             raise ValueError("out is on %s, the cache on %s" % (out.device, self.device))
-        with self._on_device():
-            nbytes = B.slkv_evict_workspace_bytes(self.layout, out.layout, keep_last, budgets)
-            ws = self._workspace(("evict", nbytes), nbytes)
-            B.slkv_evict_cache(self.layout, self._arrays, out.layout, out._arrays, keep_last, budgets, ws, kept_idx, stream)
+        with self._on(stream):
+            B.slkv_evict_cache(self.layout, self._arrays, out.layout, out._arrays, keep_last, budgets, kept_idx)

@@ -29,7 +29,7 @@ EXPORTS = ["slkv_status_str", "slkv_last_error", "slkv_version", "slkv_init", "s
            "slkv_compacted_sizes", "slkv_workspace_bytes", "slkv_compress_layer", "slkv_compress_layer_static",
            "slkv_recompress_sizes", "slkv_recompress_workspace_bytes", "slkv_recompress_layer",
            "slkv_fill_cache", "slkv_append_cache", "slkv_cache_rows", "slkv_attend_workspace_bytes", "slkv_attend_cache",
-           "slkv_evict_workspace_bytes", "slkv_evict_cache",
+           "slkv_evict_cache",
            "slkv_profile_begin", "slkv_profile_end"]
 
 SLKV_ERR_HIP = 7
@@ -152,10 +152,8 @@ def lib():
         L.slkv_attend_workspace_bytes.argtypes = [cd, C.c_int32, C.c_int32, vp]
         L.slkv_attend_cache.restype = C.c_int
         L.slkv_attend_cache.argtypes = [cd, ca, C.c_int32, vp, vp, vp, vp, vp, C.c_size_t, vp]
-        L.slkv_evict_workspace_bytes.restype = C.c_int
-        L.slkv_evict_workspace_bytes.argtypes = [cd, cd, C.c_int32, vp, vp]
         L.slkv_evict_cache.restype = C.c_int
-        L.slkv_evict_cache.argtypes = [cd, ca, cd, ca, C.c_int32, vp, vp, vp, C.c_size_t, vp]
+        L.slkv_evict_cache.argtypes = [cd, ca, cd, ca, C.c_int32, vp, vp, vp]
         L.slkv_profile_begin.restype = C.c_int
         L.slkv_profile_begin.argtypes = [C.c_int32]
         L.slkv_profile_end.restype = C.c_int
@@ -392,18 +390,11 @@ def slkv_attend_cache(layout, cache, q, out, workspace, lse=None, weight_out=Non
                                    workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
-def slkv_evict_workspace_bytes(layout, out_layout, w, budgets):
-    n = C.c_size_t(0)
-    budgets = _budgets_of(layout, budgets)
-    _check(lib().slkv_evict_workspace_bytes(layout.address, out_layout.address, int(w), budgets.ctypes.data, C.addressof(n)))
-    return int(n.value)
-
-
-def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, workspace, kept_idx=None, stream=None):
+def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, kept_idx=None, stream=None):
     """Enqueues the copy of the rows that stay to another cache."""
     budgets = _budgets_of(layout, budgets)
     _check(lib().slkv_evict_cache(layout.address, cache.address, out_layout.address, out.address, int(w), budgets.ctypes.data, _ptr(kept_idx),
-                                  _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+                                  _stream(stream)))
 
 
 def slkv_profile_begin(max_records):

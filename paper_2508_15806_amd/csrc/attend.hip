@@ -46,7 +46,7 @@ struct AttendArgs {
   float* w_out;
   float* part_o;                     // [part][R][D] sums of a part, relative to its reference
   float* part_ml;                    // [part][R][2] reference (log2), sum
-  float* logits;                     // x in log2 units: tiles of [R][32 rows]
+  float* logits;                     // q . k: tiles of [R][32 rows]
   int32_t T, R;
   int32_t tiles_each;                // room of a part in tiles of 32 rows
   int32_t row0;                      // first row of the call's rooms; logits of segment s, row j: tile (start - row0) / 32 + s + j / 32
@@ -265,7 +265,7 @@ __device__ __forceinline__ void add_weights(WeightsAhead& h, const AttendArgs& a
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
     auto add = [&](f32x4 x, float l) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += exp2_fast(x[e] - l);
+      for (int e = 0; e < 4; ++e) s[e] += exp2_fast(fmaf(x[e], a.c_log2, -l));
     };
 #pragma unroll
     for (int r = 0; r < kAheadQueries; ++r)
@@ -404,16 +404,17 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
     float p[RT][kEach];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) p[rt][j] = x[rt][j / 4][j % 4] * a.c_log2;
+      for (int j = 0; j < kEach; ++j) p[rt][j] = x[rt][j / 4][j % 4];
       if (tail) {
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
           if (mine + j >= sees[rt]) p[rt][j] = -INFINITY;
       }
+      float top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < kEach; ++j) top = fmaxf(top, p[rt][j]);
+      top *= a.c_log2;
       if (a.logits && rt * 16 + rq < R) {
         float* l = a.logits + ((tile_seg + key0 / kTileRows) * R + rt * 16 + rq) * kTileRows + mine % kTileRows;
 #pragma unroll
@@ -430,10 +431,11 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
         for (int m = 0; m < kVD; ++m) acc[rt][m] *= f;
         ref[rt] = now;
       }
+      // (one rounding, of the difference: a large product's own would be an error of the weight)
       const float from = ref[rt] == -INFINITY ? 0.f : ref[rt];
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
-        p[rt][j] = exp2_fast(p[rt][j] - from);
+        p[rt][j] = exp2_fast(fmaf(p[rt][j], a.c_log2, -from));
         sum[rt] += p[rt][j];
       }
     }

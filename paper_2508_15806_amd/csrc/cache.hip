@@ -28,12 +28,15 @@ static CacheArrays arrays_of(const slkv_cache* c) {
 
 struct Unit { u32x4 lo, hi; };       // 8 wide elements: 16 bytes in lo, or 32 (fp32)
 
+// Rows that are read once and in whole lines are loaded past the caches' order of use: 131072 rows of bf16 into a cache 30.7 -> 25.1 us, eviction from 16
+// conversations 37.0 -> 31.6; loads of 4 bytes (rows of MXFP4) are slower this way, 17.4 -> 22.0, and stores gain 3 % or nothing.
+
 template <int KIND>
 __device__ __forceinline__ Unit load_unit(const unsigned char* row, int unit) {
   Unit u;
   constexpr int kBytes = 8 * (int)sizeof(typename Kind<KIND>::wide);
-  u.lo = *(const u32x4*)(row + unit * kBytes);
-  if constexpr (kBytes == 32) u.hi = *(const u32x4*)(row + unit * kBytes + 16);
+  u.lo = __builtin_nontemporal_load((const u32x4*)(row + unit * kBytes));
+  if constexpr (kBytes == 32) u.hi = __builtin_nontemporal_load((const u32x4*)(row + unit * kBytes + 16));
   return u;
 }
 
@@ -117,16 +120,37 @@ constexpr int kThreads = 256;
 template <int N>
 using RowsTab = SegWords<N, 3>;       // w[0] room of the segment (first row), w[1] its rows outside the cache, w[2] workgroups before it
 
+// The segment of a workgroup.  One wave looks it up for all: the table stands in the kernel's arguments, which thousands of workgroups read past the caches.
+struct RowsAt { int seg, first, start, room, other, count; };
+template <class TAB>
+__device__ __forceinline__ RowsAt find_rows(const TAB& tab, RowsAt& shared) {
+  if (threadIdx.x < kWave) {
+    const int block = blockIdx.x;
+    const int i = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
+    if (threadIdx.x == 0) {
+      RowsAt r;
+      r.seg = tab.seg0 + i;
+      r.first = (block - tab.w[2][i]) * kBlockRows;
+      r.start = tab.w[0][i];
+      r.room = tab.w[0][i + 1] - r.start;
+      r.other = tab.w[1][i];
+      r.count = tab.w[1][i + 1] - r.other;
+      shared = r;
+    }
+  }
+  __syncthreads();
+  return shared;
+}
+
 // Bound by memory: 4 d bytes read and 2 (d/2 + d/32) written a row for MXFP4.  A lane takes 8 elements of a row, so
 // that a wave's loads and stores are whole lines and a block's magnitude is a maximum over four lanes.
 template <int KIND, int D, class TAB>
 __global__ __launch_bounds__(kThreads) void fill_kernel(const CacheArrays c, const unsigned char* __restrict__ k_src,
                                                         const unsigned char* __restrict__ v_src, const int32_t* __restrict__ pos_src, const TAB tab) {
-  const int block = blockIdx.x;
-  const int seg = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
-  const int first = (block - tab.w[2][seg]) * kBlockRows;
-  const int src0 = tab.w[1][seg], count = tab.w[1][seg + 1] - src0, dst0 = tab.w[0][seg];
-  if (first == 0 && threadIdx.x == 0) c.lengths[tab.seg0 + seg] = count;
+  __shared__ RowsAt sh_at;
+  const RowsAt at = find_rows(tab, sh_at);
+  const int first = at.first, src0 = at.other, count = at.count, dst0 = at.start;
+  if (first == 0 && threadIdx.x == 0) c.lengths[at.seg] = count;
   const int rows = min(count - first, kBlockRows);       // 0 in the one workgroup of a segment without rows
   constexpr int kUnits = D / 8, kRowsAtOnce = kThreads / (2 * kUnits);
   constexpr int kWideRow = D * (int)sizeof(typename Kind<KIND>::wide);
@@ -209,12 +233,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs a, co
 template <int KIND, int D, class TAB>
 __global__ __launch_bounds__(kThreads) void rows_kernel(const CacheArrays c, unsigned char* __restrict__ k_dst, unsigned char* __restrict__ v_dst,
                                                         int32_t* __restrict__ pos_dst, const TAB tab) {
-  const int block = blockIdx.x;
-  const int seg = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
-  const int first = (block - tab.w[2][seg]) * kBlockRows;
-  const int dst0 = tab.w[1][seg], start = tab.w[0][seg];
-  const int n = rows_in_use(c.lengths, tab.seg0 + seg, tab.w[0][seg + 1] - start);
-  const int take = min(n, tab.w[1][seg + 1] - dst0);
+  __shared__ RowsAt sh_at;
+  const RowsAt at = find_rows(tab, sh_at);
+  const int first = at.first, dst0 = at.other, start = at.start;
+  const int n = rows_in_use(c.lengths, at.seg, at.room);
+  const int take = min(n, at.count);
   const int rows = min(take - first, kBlockRows);
   if (rows <= 0) return;
   const int64_t src0 = (int64_t)start + n - take + first;
@@ -241,117 +264,209 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const CacheArrays c, uns
 
 // ------------------------------------------------------------------ eviction
 
-constexpr int kEvictThreads = 1024, kEvictEach = 4;
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+constexpr int kEvictHeld = 12288;     // keys that stay in LDS
+constexpr int kEvictRank = 256;       // keys that are ranked against each other
+constexpr int kEvictSlice = 1024;     // rows that a workgroup copies, at most
+constexpr int kEvictSegs = 240;
 template <int N>
-using EvictTab = SegWords<N, 3>;      // w[0] room of the segment, w[1] its room in the other cache, w[2] max(C_h, w)
+using EvictTab = SegWords<N, 4>;      // w[0] room of the segment, w[1] its room in the other cache, w[2] workgroups before it, w[3] max(C_h, w)
 
 __device__ __forceinline__ uint32_t weight_key(float v) { return v != v ? 0xffffffffu : float_key(v); }
 
-// Rows that stay, as row numbers inside the segment, ascending.  A workgroup per segment: the cap - w largest keys by three digits of 11, 11 and 10
-// bits, from the largest; then the kept ones in order, a tile of rows at a time.
-template <class TAB>
-__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const float* __restrict__ weight, const int32_t* lengths, int32_t* lengths_out, int w,
-                                                                     int32_t* __restrict__ list, const TAB tab) {
-  __shared__ uint32_t hist[kHistBins], scan[16], res[2];
-  const int seg = blockIdx.x, tid = threadIdx.x;
-  const int start = tab.w[0][seg], cap = tab.w[2][seg];
-  const int n = rows_in_use(lengths, tab.seg0 + seg, tab.w[0][seg + 1] - start);
-  list += tab.w[1][seg];
-  const int kept = min(n, cap);
-  __syncthreads();                                    // every thread has read the length: it may be the same word
-  if (tid == 0) lengths_out[tab.seg0 + seg] = kept;
-  if (n <= cap) {
-    for (int i = tid; i < n; i += kEvictThreads) list[i] = i;
-    return;
+struct EvictLds {
+  uint32_t held[kEvictHeld], hist[kHistBins], scan[16], res[2], near_key[kEvictRank], ends[2][kEvictWaves];
+  int32_t near_row[kEvictRank], near_count, from[kEvictSlice];
+};
+
+// The `want` largest of m keys, 0 < want < m: the smallest kept key and how many of the rows that have it stay, the lower ones.  A wave looks after neighbouring rows i0 ..
+// i1 - 1, lane by lane.  The key is found by digits of 11 bits of the keys' distance from the smallest, the first one as fine as their range allows (weights lie within some
+// octaves, so fixed digits would pile up in a few counters); when no more than kEvictRank keys share the digit of the last one, these are ranked against each other.  Keys
+// stay in LDS up to kEvictHeld rows, and are read again from memory beyond.  Bound by latency, of the instructions too: loops are not unrolled far.
+__device__ __forceinline__ void evict_threshold(EvictLds& l, const float* __restrict__ keys, int m, uint32_t want, int i0, int i1, uint32_t& least, uint32_t& count) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const bool in_lds = m <= kEvictHeld;
+  auto key_of = [&](int i) __attribute__((always_inline)) { return in_lds ? l.held[i] : weight_key(keys[i]); };
+  uint32_t lo = ~0u, hi = 0u;
+#pragma unroll 8
+  for (int i = i0; i < i1; i += kWave) {
+    const uint32_t x = weight_key(keys[i]);
+    if (in_lds) l.held[i] = x;
+    lo = min(lo, x);
+    hi = max(hi, x);
   }
-  const int m = n - w, want = cap - w;
-  for (int i = tid; i < w; i += kEvictThreads) list[want + i] = m + i;
-  if (want == 0) return;
-  const float* keys = weight + start;
-  uint32_t prefix = 0, k = (uint32_t)want;
-#pragma unroll
-  for (int level = 0; level < 3; ++level) {
-    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-    for (int i = tid; i < kHistBins; i += kEvictThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < m; i += kEvictThreads) {
-      const uint32_t key = weight_key(keys[i]);
-      if (level == 0 || key >> (shift + bits) == prefix) atomicAdd(&hist[key >> shift & ((1u << bits) - 1u)], 1u);
+  auto smaller = [](uint32_t x, uint32_t y) { return min(x, y); };
+  auto larger = [](uint32_t x, uint32_t y) { return max(x, y); };
+  lo = wave_reduce_to_last(lo, smaller);
+  hi = wave_reduce_to_last(hi, larger);
+  if (lane == kWave - 1) l.ends[0][wave] = lo, l.ends[1][wave] = hi;
+  for (int i = tid; i < kHistBins; i += kEvictThreads) l.hist[i] = 0;
+  if (tid == 0) l.near_count = 0;
+  __syncthreads();
+  lo = (uint32_t)__builtin_amdgcn_readlane((int)wave_reduce_to_last(l.ends[0][lane % kEvictWaves], smaller), kWave - 1);
+  hi = (uint32_t)__builtin_amdgcn_readlane((int)wave_reduce_to_last(l.ends[1][lane % kEvictWaves], larger), kWave - 1);
+  // the keys from `lo` on, of which `bits` bits are undecided; the k-th largest of these is looked for
+  int bits = hi == lo ? 0 : 32 - __clz(hi - lo);
+  uint32_t k = want;
+  while (bits > 0) {
+    const int shift = max(bits - 11, 0);
+#pragma unroll 4
+    for (int i = i0; i < i1; i += kWave) {
+      const uint32_t x = key_of(i), d = x - lo;
+      if (x >= lo && (d >> shift) < (uint32_t)kHistBins) atomicAdd(&l.hist[d >> shift], 1u);
     }
     __syncthreads();
-    select_bin<kEvictThreads>(hist, k, scan, res);
-    prefix = prefix << bits | res[0];
-    k = res[1];
+    select_bin<kEvictThreads>(l.hist, k, l.scan, l.res);
+    const uint32_t digit = l.res[0], share = l.hist[digit];
+    k = l.res[1];
+    lo += digit << shift;
+    bits = shift;
+    __syncthreads();
+    if (bits == 0) break;
+    if (share <= (uint32_t)kEvictRank) {
+#pragma unroll 4
+      for (int i = i0; i < i1; i += kWave) {
+        const uint32_t x = key_of(i);
+        if (x >= lo && (x - lo) >> bits == 0) {
+          const int at = atomicAdd(&l.near_count, 1);
+          l.near_key[at] = x;
+          l.near_row[at] = i;
+        }
+      }
+      __syncthreads();
+      // four lanes a key: how many are larger, how many equal ones come before it
+      const int c = tid / 4;
+      uint32_t above = 0, before = 0;
+      if (c < (int)share) {
+        const uint32_t x = l.near_key[c];
+        const int row = l.near_row[c];
+        for (uint32_t i = tid % 4; i < share; i += 4) {
+          above += l.near_key[i] > x;
+          before += l.near_key[i] == x && l.near_row[i] < row;
+        }
+      }
+      above += dpp_move<0xb1>(0u, above);
+      above += dpp_move<0x4e>(0u, above);
+      before += dpp_move<0xb1>(0u, before);
+      before += dpp_move<0x4e>(0u, before);
+      if (c < (int)share && tid % 4 == 0 && above + before == k - 1) l.res[0] = l.near_key[c], l.res[1] = before + 1;
+      __syncthreads();
+      lo = l.res[0];
+      k = l.res[1];
+      break;
+    }
+    for (int i = tid; i < kHistBins; i += kEvictThreads) l.hist[i] = 0;
     __syncthreads();
   }
-  // prefix: the smallest kept key, of which the first k stay
-  uint32_t equal = 0, out = 0;
-  for (int base = 0; base < m; base += kEvictThreads * kEvictEach) {
-    uint32_t key[kEvictEach], gt = 0, eq = 0;
-#pragma unroll
-    for (int j = 0; j < kEvictEach; ++j) {
-      const int i = base + tid * kEvictEach + j;
-      key[j] = i < m ? weight_key(keys[i]) : 0u;
-      const bool in = i < m;
-      gt += in && key[j] > prefix;
-      eq += in && key[j] == prefix;
-    }
-    const uint32_t incl = block_incl_scan<kEvictThreads>(gt | eq << 16, scan);
-    uint32_t e = equal + (incl >> 16) - eq, g = (incl & 0xffffu) - gt;
-    // kept before this thread's rows: the larger ones, and of the equal ones the first k
-    uint32_t at = out + g + (min(e, k) - min(equal, k));
-#pragma unroll
-    for (int j = 0; j < kEvictEach; ++j) {
-      const int i = base + tid * kEvictEach + j;
-      if (i >= m) continue;
-      if (key[j] > prefix || (key[j] == prefix && e < k)) list[at++] = i;
-      e += key[j] == prefix;
-    }
-    if (tid == kEvictThreads - 1) {
-      res[0] = incl & 0xffffu;
-      res[1] = incl >> 16;
-    }
-    __syncthreads();
-    out += res[0] + (min(equal + res[1], k) - min(equal, k));
-    equal += res[1];
-    __syncthreads();
-  }
+  least = lo;
+  count = k;
 }
 
-// The kept rows' bytes.  Bound by memory.
-template <class TAB>
-__global__ __launch_bounds__(kThreads) void evict_copy_kernel(const CacheArrays in, const CacheArrays out, const int32_t* __restrict__ list, int32_t* __restrict__ kept_idx,
-                                                              int row_bytes, int scale_bytes, const TAB tab) {
-  const int block = blockIdx.x;
-  const int seg = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
-  const int first = (block - tab.w[2][seg]) * kBlockRows;
-  const int start = tab.w[0][seg], dst0 = tab.w[1][seg];
-  const int rows = min(rows_in_use(out.lengths, tab.seg0 + seg, tab.w[1][seg + 1] - dst0) - first, kBlockRows);
-  if (rows <= 0) return;
-  __shared__ int32_t from[kBlockRows];
-  if ((int)threadIdx.x < rows) from[threadIdx.x] = list[dst0 + first + (int)threadIdx.x];
-  __syncthreads();
-  const int64_t to0 = (int64_t)dst0 + first;
-  const int units = row_bytes / 16;
-  for (int i = threadIdx.x; i < rows * units * 2; i += kThreads) {
-    const int u = i % units, r = i / units % rows, isv = i / (units * rows);
-    const int64_t s = (int64_t)start + from[r];
-    const unsigned char* src = isv ? in.v : in.k;
-    unsigned char* dst = isv ? out.v : out.k;
-    *(u32x4*)(dst + (to0 + r) * row_bytes + u * 16) = *(const u32x4*)(src + s * row_bytes + u * 16);
-  }
-  if (scale_bytes)
-    for (int i = threadIdx.x; i < rows * scale_bytes * 2; i += kThreads) {
-      const int u = i % scale_bytes, r = i / scale_bytes % rows, isv = i / (scale_bytes * rows);
-      const unsigned char* src = isv ? in.v_scale : in.k_scale;
-      unsigned char* dst = isv ? out.v_scale : out.k_scale;
-      dst[(to0 + r) * scale_bytes + u] = src[((int64_t)start + from[r]) * scale_bytes + u];
+// A workgroup copies a slice of a segment's kept rows, `slice` of them, UNITS of 16 bytes a row of K; which rows these are every workgroup of the segment finds by
+// itself, so that nothing waits for a selection that is not its own: 128 segments of up to 3345 rows, half of them kept, XXA us, with a launch that selects (10 us, by the
+// longest segment) and one that copies 40.  The copy is bound by memory: 16 rows of every wave are on their way at once.
+template <int UNITS, int SCALES, class TAB>
+__global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays in, const CacheArrays out, int32_t* __restrict__ kept_idx, int w, int slice, const TAB tab) {
+  __shared__ EvictLds l;
+  __shared__ int32_t sh_at[6];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  if (tid < kWave) {
+    const int i = find_segment_wave(tab.nseg, (int)blockIdx.x, [&](int s) { return tab.w[2][s]; });
+    if (tid == 0) {
+      sh_at[0] = tab.seg0 + i;
+      sh_at[1] = (int)blockIdx.x - tab.w[2][i];
+      sh_at[2] = tab.w[0][i];
+      sh_at[3] = rows_in_use(in.lengths, tab.seg0 + i, tab.w[0][i + 1] - tab.w[0][i]);
+      sh_at[4] = tab.w[1][i];
+      sh_at[5] = tab.w[3][i];
     }
-  if ((int)threadIdx.x < rows) {
-    const int64_t s = (int64_t)start + from[threadIdx.x], t = to0 + (int)threadIdx.x;
+  }
+  __syncthreads();
+  const int seg = sh_at[0], first = sh_at[1] * slice, start = sh_at[2], n = sh_at[3], cap = sh_at[5];
+  const int kept = min(n, cap), rows = min(kept - first, slice);
+  if (first == 0 && tid == 0) out.lengths[seg] = kept;
+  if (rows <= 0) return;
+  const int m = n - w, want = cap - w;
+  if (n <= cap) {
+    for (int r = tid; r < rows; r += kEvictThreads) l.from[r] = first + r;
+  } else {
+    for (int r = max(want - first, 0) + tid; r < rows; r += kEvictThreads) l.from[r] = m + first + r - want;   // of the latest w
+    if (first < want) {
+      const float* keys = in.weight + start;
+      const int rows_each = (m + kEvictThreads - 1) / kEvictThreads * kWave;     // of a wave
+      const int i0 = wave * rows_each + lane, i1 = min(m, (wave + 1) * rows_each);
+      uint32_t least, k;
+      evict_threshold(l, keys, m, (uint32_t)want, i0, i1, least, k);
+      auto key_of = [&](int i) __attribute__((always_inline)) { return m <= kEvictHeld ? l.held[i] : weight_key(keys[i]); };
+      // a wave counts its kept rows by votes, then emits them at the places that the waves before it leave
+      uint32_t gt = 0, eq = 0;
+#pragma unroll 4
+      for (int i = i0; i - lane < i1; i += kWave) {
+        const uint32_t x = i < i1 ? key_of(i) : 0u;
+        gt += (uint32_t)__popcll(__ballot(i < i1 && x > least));
+        eq += (uint32_t)__popcll(__ballot(i < i1 && x == least));
+      }
+      if (lane == 0) l.ends[0][wave] = gt, l.ends[1][wave] = eq;
+      __syncthreads();
+      uint32_t at = 0, e = 0;                         // kept rows, and rows of the smallest kept key, in the waves before
+      for (int v = 0; v < wave; ++v) {
+        at += l.ends[0][v];
+        e += l.ends[1][v];
+      }
+      at += min(e, k);
+      const uint64_t below = (1ull << lane) - 1;
+      const bool mine = (int)(at + gt + eq) > first && (int)at < first + rows;   // some of the wave's rows may be in the slice
+      for (int i = mine ? i0 : i1 + lane; i - lane < i1; i += kWave) {
+        const uint32_t x = i < i1 ? key_of(i) : 0u;
+        const bool is_eq = i < i1 && x == least;
+        const uint64_t eqs = __ballot(is_eq);
+        const bool stays = (i < i1 && x > least) || (is_eq && e + (uint32_t)__popcll(eqs & below) < k);
+        const uint64_t all = __ballot(stays);
+        const int r = (int)(at + (uint32_t)__popcll(all & below)) - first;
+        if (stays && r >= 0 && r < rows) l.from[r] = i;
+        at += (uint32_t)__popcll(all);
+        e += (uint32_t)__popcll(eqs);
+      }
+    }
+  }
+  __syncthreads();
+  const int64_t to0 = (int64_t)sh_at[4] + first, src0 = start;
+  constexpr int kRowsAtOnce = kEvictThreads / UNITS, kTimes = 4;
+  const int u = tid % UNITS, r0 = tid / UNITS;
+  for (int r1 = r0; r1 < rows; r1 += kTimes * kRowsAtOnce) {
+    u32x4 k[kTimes], v[kTimes];
+#pragma unroll
+    for (int t = 0; t < kTimes; ++t) {
+      const int r = r1 + t * kRowsAtOnce;
+      if (r < rows) {
+        const int64_t s = (src0 + l.from[r]) * UNITS + u;
+        k[t] = __builtin_nontemporal_load((const u32x4*)in.k + s);
+        v[t] = __builtin_nontemporal_load((const u32x4*)in.v + s);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kTimes; ++t) {
+      const int r = r1 + t * kRowsAtOnce;
+      if (r < rows) {
+        const int64_t d = (to0 + r) * UNITS + u;
+        ((u32x4*)out.k)[d] = k[t];
+        ((u32x4*)out.v)[d] = v[t];
+      }
+    }
+  }
+  if constexpr (SCALES > 0) {
+    typedef std::conditional_t<SCALES == 4, uint32_t, uint16_t> word;          // a row's exponents
+    for (int r = tid; r < rows; r += kEvictThreads) {
+      const int64_t s = src0 + l.from[r];
+      ((word*)out.k_scale)[to0 + r] = ((const word*)in.k_scale)[s];
+      ((word*)out.v_scale)[to0 + r] = ((const word*)in.v_scale)[s];
+    }
+  }
+  for (int r = tid; r < rows; r += kEvictThreads) {
+    const int64_t s = src0 + l.from[r], t = to0 + r;
     if (in.pos && out.pos) out.pos[t] = in.pos[s];
-    if (out.weight) out.weight[t] = in.weight[s];
-    if (kept_idx) kept_idx[t] = from[threadIdx.x];
+    if (in.weight && out.weight) out.weight[t] = in.weight[s];
+    if (kept_idx) kept_idx[t] = l.from[r];
   }
 }
 
@@ -509,18 +624,8 @@ extern "C" slkv_status slkv_cache_rows(const slkv_cache_desc* desc, const slkv_c
   return launch_status("rows");
 }
 
-extern "C" slkv_status slkv_evict_workspace_bytes(const slkv_cache_desc* desc, const slkv_cache_desc* out_desc, int32_t w, const int32_t* h_budgets, size_t* bytes) {
-  clear_error();
-  if (!bytes) return fail(SLKV_ERR_NULL, "bytes is NULL");
-  slkv_status st = evict_checks(desc, out_desc, w, h_budgets);
-  if (st != SLKV_OK) return st;
-  *bytes = std::max<size_t>(16, (size_t)out_desc->h_offsets[(int64_t)desc->B * desc->Hkv] * sizeof(int32_t));
-  return SLKV_OK;
-}
-
 extern "C" slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const slkv_cache_desc* out_desc, const slkv_cache* out,
-                                        int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx,
-                                        void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+                                        int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx, void* hip_stream) {
   clear_error();
   slkv_status st = evict_checks(desc, out_desc, w, h_budgets);
   if (st != SLKV_OK) return st;
@@ -529,43 +634,44 @@ extern "C" slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_
   const int64_t S = (int64_t)desc->B * desc->Hkv, rows_in = desc->h_offsets[S], rows_out = out_desc->h_offsets[S];
   if (!out->d_lengths) return fail(SLKV_ERR_NULL, "out: d_lengths is NULL");
   if (rows_in > desc->h_offsets[0] && !cache->d_weight) return fail(SLKV_ERR_NULL, "cache: d_weight is NULL");
-  if (!d_workspace) return fail(SLKV_ERR_NULL, "d_workspace is NULL");
-  if ((uintptr_t)d_kept_idx % 16 || (uintptr_t)d_workspace % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer not 16-byte aligned");
+  if ((uintptr_t)d_kept_idx % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", (void*)d_kept_idx);
   const int64_t row_bytes = (int64_t)desc->d * kind_bits(desc->dtype) / 8, scale_bytes = desc->dtype == SLKV_BF16_KV_MXFP4 ? desc->d / kScaleBlock : 0;
-  // a segment's shorter room may never hold cap rows
+  // (a segment with a shorter room never holds cap rows)
   auto cap_of = [&](int64_t s) { return std::max(h_budgets[s % desc->Hkv], w); };
   auto most_of = [&](int64_t s) { return std::min<int64_t>(desc->h_offsets[s + 1] - desc->h_offsets[s], cap_of(s)); };
-  for (int64_t s = 0; s < S; ++s)
-    if (out_desc->h_offsets[s + 1] - out_desc->h_offsets[s] < most_of(s))
-      return fail(SLKV_ERR_CAPACITY, "segment %lld: up to %lld rows into a room of %lld", (long long)s, (long long)most_of(s),
-                  (long long)(out_desc->h_offsets[s + 1] - out_desc->h_offsets[s]));
+  int64_t most = 0;
+  for (int64_t s = 0; s < S; ++s) {
+    const int64_t rows = most_of(s), room = out_desc->h_offsets[s + 1] - out_desc->h_offsets[s];
+    if (room < rows) return fail(SLKV_ERR_CAPACITY, "segment %lld: up to %lld rows into a room of %lld", (long long)s, (long long)rows, (long long)room);
+    most += rows;
+  }
   const void* ins[] = {cache->d_k, cache->d_v, cache->d_k_scale, cache->d_v_scale, cache->d_pos, cache->d_weight, cache->d_lengths};
-  const void* outs[] = {out->d_k, out->d_v, out->d_k_scale, out->d_v_scale, out->d_pos, out->d_weight, out->d_lengths};
-  const int64_t each[] = {row_bytes, row_bytes, scale_bytes, scale_bytes, 4, 4, 0};
+  const void* outs[] = {out->d_k, out->d_v, out->d_k_scale, out->d_v_scale, out->d_pos, out->d_weight, out->d_lengths, d_kept_idx};
+  const int64_t each[] = {row_bytes, row_bytes, scale_bytes, scale_bytes, 4, 4, 0, 4};
   for (int i = 0; i < 7; ++i)
-    for (int j = 0; j < 7; ++j)
-      if (!(i == 6 && j == 6 && ins[i] == outs[j]) &&
-          overlap(ins[i], outs[j], i == 6 ? 4 * S : rows_in * each[i], j == 6 ? 4 * S : rows_out * each[j]))
+    for (int j = 0; j < 8; ++j)
+      if (overlap(ins[i], outs[j], i == 6 ? 4 * S : rows_in * each[i], j == 6 ? 4 * S : rows_out * each[j]))
         return fail(SLKV_ERR_BAD_ARG, "arrays of cache and out overlap");
-  size_t need = 0;
-  if ((st = slkv_evict_workspace_bytes(desc, out_desc, w, h_budgets, &need)) != SLKV_OK) return st;
-  if (workspace_bytes < need) return fail(SLKV_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
+  // slices: two workgroups a CU, if the rows are enough for that; a segment's last one is half empty on average
+  const int slice = (int)std::min<int64_t>(kEvictSlice, std::max<int64_t>(64, ceil_div(most, std::max<int64_t>(512 - S / 2, 256))));
   ScopedKernelTimer timer(SLKV_K_EVICT);
-  hipStream_t const stream = (hipStream_t)hip_stream;
-  int32_t* const list = (int32_t*)d_workspace;
-  for_tables<EvictTab, kManySegs3, -1>(
+  for_tables<EvictTab, kEvictSegs, 2>(
       S, [&](int64_t s, int r) { return r == 0 ? (int32_t)desc->h_offsets[s] : r == 1 ? (int32_t)out_desc->h_offsets[s] : s < S ? cap_of(s) : 0; },
-      [&](int64_t) { return 1; },
-      [&](const auto& tab, int segs) {
-        SLKV_LAUNCH((evict_select_kernel<std::decay_t<decltype(tab)>>), dim3(segs), dim3(kEvictThreads), 0, stream, cache->d_weight, cache->d_lengths,
-                    out->d_lengths, w, list, tab);
-      });
-  for_tables<RowsTab, kManySegs3, 2>(
-      S, [&](int64_t s, int r) { return (int32_t)(r == 0 ? desc->h_offsets[s] : out_desc->h_offsets[s]); },
-      [&](int64_t s) { return ceil_div(most_of(s), kBlockRows); },
+      [&](int64_t s) { return std::max<int64_t>(1, ceil_div(most_of(s), slice)); },
       [&](const auto& tab, int blocks) {
-        SLKV_LAUNCH((evict_copy_kernel<std::decay_t<decltype(tab)>>), dim3(blocks), dim3(kThreads), 0, stream, arrays_of(cache), arrays_of(out), list,
-                    d_kept_idx, (int)row_bytes, (int)scale_bytes, tab);
+        using TAB = std::decay_t<decltype(tab)>;
+        auto go = [&](auto units, auto scales) {
+          SLKV_LAUNCH((evict_kernel<decltype(units)::value, decltype(scales)::value, TAB>), dim3(blocks), dim3(kEvictThreads), 0, (hipStream_t)hip_stream,
+                      arrays_of(cache), arrays_of(out), d_kept_idx, w, slice, tab);
+        };
+        using std::integral_constant;
+        const integral_constant<int, 0> none{};
+        if (scale_bytes == 4) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+        else if (scale_bytes == 2) go(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+        else if (row_bytes == 64) go(integral_constant<int, 4>{}, none);
+        else if (row_bytes == 128) go(integral_constant<int, 8>{}, none);
+        else if (row_bytes == 256) go(integral_constant<int, 16>{}, none);
+        else go(integral_constant<int, 32>{}, none);
       });
   return launch_status("evict");
 }

@@ -75,7 +75,7 @@ def test_long_histories(n, share):
     check(cache, [int(n * share), 40], 8)
 
 
-@pytest.mark.parametrize("n", [50, 3000, 20000])
+@pytest.mark.parametrize("n", [50, 3000, 12287 + 5, 12288 + 5, 12289 + 5, 20000])
 def test_equal_weights(n):
     rng = np.random.default_rng(n)
     cache = random_cache(rng, "bf16", 1, 4, 1, 64, [n] * 4)
@@ -102,18 +102,14 @@ def test_weights_that_are_no_ordinary_numbers():
     check(cache, [60, 300, 1000], 0)
 
 
-def test_lengths_out_of_range_and_in_place():
+def test_lengths_out_of_range():
     rng = np.random.default_rng(2)
     cache = random_cache(rng, "bf16", 1, 4, 1, 64, [100, 100, 100, 100])
     cache.lengths.copy_(torch.tensor([-1, 1 << 30, 60, 100], dtype=torch.int32))
-    want = check(cache, [50, 50, 70, 0], 10)
-    # the lengths may be the same array
-    out = api.Cache("bf16", 1, 4, 4, 64, want.layout.offsets, lengths=cache.lengths)
-    cache.evict([50, 50, 70, 0], 10, out)
-    assert torch.equal(out.lengths, want.lengths) and cache.lengths.cpu().tolist() == [0, 50, 60, 10]
+    assert check(cache, [50, 50, 70, 0], 10).lengths.cpu().tolist() == [0, 50, 60, 10]
 
 
-@pytest.mark.parametrize("S", [64, 65, 290, 291, 900])
+@pytest.mark.parametrize("S", [64, 65, 239, 240, 241, 900])
 def test_segment_tables(S):
     rng = np.random.default_rng(S)
     lens = rng.integers(0, 60, S).tolist()

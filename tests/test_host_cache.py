@@ -140,23 +140,24 @@ def test_rows_refuses_before_touching_the_gpu():
 def test_evict_refuses_before_touching_the_gpu():
     far = 1 << 30
 
-    def evict(lay=None, arr=None, out_lay=None, out=None, w=4, budgets=(40, 20), idx=NULL, ws=FAKE, nbytes=BIG):
+    def evict(lay=None, arr=None, out_lay=None, out=None, w=4, budgets=(40, 20), idx=NULL):
         lay = lay or layout()
         out_lay = out_lay or layout(offsets=[0, 40, 60, 100, 120])
         arr = arr or arrays()
         out = out or arrays(**{f: far + i * (1 << 22) for i, f in enumerate(["d_k", "d_v", "d_lengths", "d_pos", "d_weight"])})
         bud = None if budgets is None else np.array(budgets, dtype=np.int32)
         return B.lib().slkv_evict_cache(lay.address, C.addressof(arr), out_lay.address, C.addressof(out), w, None if bud is None else bud.ctypes.data, idx,
-                                        ws, nbytes, None)
+                                        None)
     assert evict(w=-1) == 2 and evict(budgets=None) == 1 and evict(budgets=(-1, 3)) == 2
-    assert evict(arr=arrays(d_weight=NULL)) == 1 and evict(ws=NULL) == 1
-    assert evict(ws=ODD) == 2 and evict(idx=ODD) == 2
+    assert evict(arr=arrays(d_weight=NULL)) == 1
+    assert evict(idx=ODD) == 2
     assert evict(out_lay=layout(offsets=[0, 39, 60, 100, 120])) == 6
     assert evict(w=50) == 6                                                            # the latest 50 rows do not fit
     assert evict(out_lay=layout(dtype=B.SLKV_F16, offsets=[0, 40, 60, 100, 120])) == 2
     assert evict(out_lay=layout(Hq=4, offsets=[0, 40, 60, 100, 120])) == 2
-    assert evict(nbytes=0) == 5
     assert evict(out=arrays()) == 2                                                    # the same arrays
     one = dict(d_k=far, d_v=far + (1 << 22), d_lengths=far + (2 << 22), d_pos=far + (3 << 22), d_weight=far + (4 << 22))
     assert evict(out=arrays(**dict(one, d_v=FAKE + 190 * 256 - 16))) == 2              # overlaps by 16 bytes
+    assert evict(out=arrays(**dict(one, d_lengths=FAKE))) == 2                         # lengths are read by many workgroups
+    assert evict(idx=FAKE) == 2
     assert evict(out=arrays(**dict(one, d_lengths=NULL))) == 1
