@@ -326,7 +326,7 @@ slkv_status slkv_recompress_layer(const slkv_ragged_desc* desc, const void* d_qw
  * d_lengths[s] are in use, oldest first.  The lengths live on the device, so that a recorded HIP graph that appends,
  * attends and evicts replays on a cache that has grown since; what a call reads of them is bounded by the room whatever they hold
  * (below 0 counts as 0, above the room as the room).  Rows that are not in use are neither read as keys or values nor changed.
- * The rooms may total 2^31 - 1 rows, one of them 2^30; addresses are 64-bit.
+ * The rooms may total 2^31 - 1 rows, one of them 2^25; addresses are 64-bit.
  */
 typedef struct {
   uint32_t struct_size;        /* sizeof(slkv_cache_desc) */

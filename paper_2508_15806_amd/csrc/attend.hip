@@ -21,7 +21,7 @@ constexpr int kAttendThreads = 256;  // of the joining kernel
 constexpr int kTileRows = 32;        // rows of a tile of stored logits, and what parts of a segment are a multiple of
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-constexpr int kJoinPairs = 2048;     // (part, query) pairs of a segment whose references a workgroup holds in LDS
+constexpr int kJoinPairs = 4096;     // (part, query) pairs of a segment, at most: the joining kernel holds a number of each
 
 // Segments of a launch: first row of their rooms.  A table of more than 64 says in which order the segments' parts are launched, and how many parts come before every
 // 16th segment of that order.
@@ -51,13 +51,14 @@ struct AttendArgs {
   int32_t tiles_each;                // room of a part in tiles of 32 rows
   int32_t row0;                      // first row of the call's rooms; logits of segment s, row j: tile (start - row0) / 32 + s + j / 32
   float c_log2;                      // log2(e) / sqrt(d)
-  double per_tiles_each;             // 1 / tiles_each
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Rows of a part: ceil(n / parts) rounded up to tiles, so that the work is spread over the same workgroups whatever the length is.
-__device__ __forceinline__ int part_rows(int n, int parts) { return ((n + parts - 1) / parts + kTileRows - 1) / kTileRows * kTileRows; }
+// x / y for 0 <= x < 2^21, y > 0: (x + 1/2) / y is at least 1 / (2 y) from a whole number, and what reciprocal and product are off by, 2^-22 of it, is less.
+__device__ __forceinline__ int divide(int x, int y) { return (int)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)y)); }
+// ceil(n / 32), at most 2^20: rooms have at most 2^25 rows.
+__device__ __forceinline__ int tiles_of(int n) { return (n + kTileRows - 1) / kTileRows; }
 
 template <int KIND, int D>
 struct Attend {
@@ -271,7 +272,7 @@ __device__ __forceinline__ void add_weights(WeightsAhead& h, const AttendArgs& a
     for (int r = 0; r < kAheadQueries; ++r)
       if (r < a.R) add(h.x[r], lse[r]);
     const float* l = logits_of(a, tile, j);
-#pragma unroll 4
+#pragma unroll 8
     for (int r = kAheadQueries; r < a.R; ++r) add(*(const f32x4*)(l + r * kTileRows), lse[r]);
     s += h.w;
     load_weights(h, a, start, tile, j + 4 * NT, j1);
@@ -283,7 +284,7 @@ __device__ __forceinline__ void add_weights(WeightsAhead& h, const AttendArgs& a
 
 // The segment of a workgroup, which is a part of one: segments have max(1, ceil(room / rows_each)) parts.  One wave looks it up and reads the length for all: the
 // table is read from the kernel's arguments, where a workgroup that goes through 3 KB of it with every wave waits up to 20 us behind the others (768 workgroups; this way 1 to 2).
-struct Where { int seg, start, part, parts, first, n, tile; };
+struct Where { int seg, start, part, first, n, tile, each, active; };   // rows of a part; parts that have any: the rows in use are spread over the parts of the room
 template <class TAB>
 __device__ __forceinline__ Where find_part(const AttendArgs& a, const TAB& tab, Where& shared) {
   if (threadIdx.x < kWave) {
@@ -301,19 +302,19 @@ __device__ __forceinline__ Where find_part(const AttendArgs& a, const TAB& tab, 
     }
     s = min(s, tab.nseg - 1);
     const int in_use = a.lengths ? a.lengths[tab.seg0 + s] : 0, at = tab.start[s], room = tab.start[s + 1] - at;
-    // tiles of 32 rows: below 2^26, and 2^15 a part at most, so a double's quotient of (numerator + 1/2) is never on the wrong side of a whole number
-    const int tiles = (room + kTileRows - 1) / kTileRows;
-    const int parts = in ? max(1, (int)((tiles + a.tiles_each - 1 + 0.5) * a.per_tiles_each)) : 0;
+    const int parts = in ? max(1, divide(tiles_of(room) + a.tiles_each - 1, a.tiles_each)) : 0;
     const int first = first0 + (int)wave_incl_scan((uint32_t)parts) - parts;
     if (parts && first <= part_id && part_id < first + parts) {
       Where w;
       w.seg = tab.seg0 + s;
       w.start = at;
       w.part = part_id - first;
-      w.parts = parts;
       w.first = first;
       w.n = a.lengths ? min(max(in_use, 0), room) : room;
       w.tile = (at - a.row0) / kTileRows + w.seg;
+      const int tiles = tiles_of(w.n), each = divide(tiles + parts - 1, parts);
+      w.each = each * kTileRows;
+      w.active = each ? divide(tiles + each - 1, each) : 0;
       shared = w;
     }
   }
@@ -322,7 +323,8 @@ __device__ __forceinline__ Where find_part(const AttendArgs& a, const TAB& tab, 
   w.seg = __builtin_amdgcn_readfirstlane(shared.seg);
   w.start = __builtin_amdgcn_readfirstlane(shared.start);
   w.part = __builtin_amdgcn_readfirstlane(shared.part);
-  w.parts = __builtin_amdgcn_readfirstlane(shared.parts);
+  w.each = __builtin_amdgcn_readfirstlane(shared.each);
+  w.active = __builtin_amdgcn_readfirstlane(shared.active);
   w.first = __builtin_amdgcn_readfirstlane(shared.first);
   w.n = __builtin_amdgcn_readfirstlane(shared.n);
   w.tile = __builtin_amdgcn_readfirstlane(shared.tile);
@@ -342,8 +344,7 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
   __shared__ Where sh_at;
   const Where at = find_part(a, tab, sh_at);
   const int seg = at.seg, start = at.start, part = at.part, n = at.n;
-  const int each = part_rows(n, at.parts);
-  const int begin = part * each, end = min(n, begin + each);
+  const int begin = part * at.each, end = min(n, begin + at.each);
   if (begin >= end && part > 0) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = threadIdx.x % kWave;
   const int rq = lane & 15, g = lane >> 4, R = a.R, T = a.T;
@@ -573,8 +574,7 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
     }
   }
   __syncthreads();
-  const int active = each ? (n + each - 1) / each : 0;
-  const bool whole = active <= 1;
+  const bool whole = at.active <= 1;
   float* const ml = a.part_ml + (int64_t)blockIdx.x * 2 * R;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -644,92 +644,81 @@ __device__ __forceinline__ float reduce_lanes(float v, int share, OP op) {
 }
 
 // Segments of more than one part: the parts put together, in their order.  The workgroup of part p of a segment adds up the references and sums of its R queries over
-// all parts, 256 / R lanes a query, 4 to 64, and finishes a slice of the outputs and the weights of the part's rows.  What it reads is asked for at once: behind the table
-// and the length there is one round trip.  (Two other ways were measured.  The workgroups of a segment waiting for each other in the launch above: 40 us instead of 34 for
-// one long history, whose memory traffic their meeting competes with, nothing gained elsewhere; the last one to arrive joining the segment alone: 25 to 40 % slower.)
-constexpr int kJoinFirst = 4;          // parts of an output that a thread asks for at once
+// all parts, 256 / R lanes a query, 4 to 64, and finishes every active'th group of 64 to 512 outputs and the weights of the part's rows.  What it reads is asked for at once: behind
+// the table and the length there is one round trip.  Bound by latency, of the instructions too.  (Two other ways were measured.  The workgroups of a segment waiting for
+// each other in the launch above: 40 us instead of 34 for one long history, whose memory traffic their meeting competes with, nothing gained elsewhere; the last one to
+// arrive joining the segment alone: 25 to 40 % slower.)
 template <int KIND, int D, class TAB>
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a, const TAB tab) {
   __shared__ Where sh_at;
-  __shared__ float sh_lse[64], sh_top[64], sh_total[64], sh_factor[kJoinPairs];   // [part][query], where all fit
-  __shared__ f32x4 sh_o[kAttendThreads];
+  __shared__ float sh_lse[64], sh_total[64], sh_factor[kJoinPairs];   // [part][query]
+  __shared__ f32x4 sh_o[kAttendThreads / kWave][16];
   const Where w = find_part(a, tab, sh_at);
-  const int n = w.n, part = w.part, each = part_rows(n, w.parts), active = each ? (n + each - 1) / each : 0;
+  const int n = w.n, part = w.part, active = w.active;
   if (active <= 1 || part >= active) return;
   const int R = a.R, T = a.T, tid = threadIdx.x;
   const float* ml = a.part_ml + (int64_t)w.first * 2 * R;
   const float* po = a.part_o + (int64_t)w.first * R * D;
-  const bool fit = R * active <= kJoinPairs;
-  // the queries: `share` lanes each, a lane per part
-  const int share = R <= 4 ? 64 : R <= 8 ? 32 : R <= 16 ? 16 : R <= 32 ? 8 : 4;
-  const int r = tid / share, lane = tid % share;
+  // the queries: 1 << bits lanes each, a lane per part
+  const int bits = R <= 4 ? 6 : R <= 8 ? 5 : R <= 16 ? 4 : R <= 32 ? 3 : 2, share = 1 << bits;
+  const int r = tid >> bits, lane = tid & (share - 1);
   f32x2 pair = f32x2{-INFINITY, 0.f};
   if (r < R && lane < active) pair = *(const f32x2*)(ml + 2 * (lane * R + r));
-  // a slice of the outputs, four at a time: a thread per kJoinFirst parts of an output, as far as there are threads
-  const int all = R * (D / 4);
-  const int f0 = (int)((uint32_t)(all * part) / (uint32_t)active), f1 = (int)((uint32_t)(all * (part + 1)) / (uint32_t)active), mine = f1 - f0;
-  const int nf = max(min(mine, kAttendThreads), 1);
-  const int groups = min(kAttendThreads / nf, (active + kJoinFirst - 1) / kJoinFirst);
-  const int grp = tid / nf, fi = tid - grp * nf;
-  f32x4 x[kJoinFirst];
-#pragma unroll
-  for (int k = 0; k < kJoinFirst; ++k) {
-    const int p = grp + k * groups;
-    if (grp < groups && fi < mine && p < active) x[k] = *(const f32x4*)(po + (int64_t)p * R * D + (f0 + fi) * 4);
-  }
+  // the outputs, in units of 64: 16 threads take four each, `groups` of these the parts, 2 to 16, and what is left other units
+  const int groups = active <= 2 ? 2 : active <= 4 ? 4 : active <= 8 ? 8 : 16, grp_bits = active <= 2 ? 1 : active <= 4 ? 2 : active <= 8 ? 3 : 4;
+  const int units = R * (D / 64), f = tid & 15, grp = (tid >> 4) & (groups - 1), at_once = 16 >> grp_bits, sub = tid >> (4 + grp_bits);
+  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (part * at_once + sub < units && grp < active) x = *(const f32x4*)(po + (int64_t)grp * R * D + (part * at_once + sub) * 64 + f * 4);
   WeightsAhead h;
-  const int end = min(n, (part + 1) * each);
-  if (a.w_out) load_weights(h, a, w.start, w.tile, part * each + 4 * tid, end);
+  const int end = min(n, (part + 1) * w.each);
+  if (a.w_out) load_weights(h, a, w.start, w.tile, part * w.each + 4 * tid, end);
 
   auto factor_of = [](float m, float top) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : exp2_fast(m - top); };
   float top = pair[0];
   if (r < R)
     for (int p = lane + share; p < active; p += share) top = fmaxf(top, ml[2 * (p * R + r)]);
   top = reduce_lanes(top, share, [](float u, float v) { return fmaxf(u, v); });
-  float f = factor_of(pair[0], top), total = pair[1] * f;
-  if (r < R) {
-    if (fit && lane < active) sh_factor[lane * R + r] = f;
-    for (int p = lane + share; p < active; p += share) {
-      f = factor_of(ml[2 * (p * R + r)], top);
-      total += ml[2 * (p * R + r) + 1] * f;
-      if (fit) sh_factor[p * R + r] = f;
+  float total = 0.f;
+  if (r < R)
+    for (int p = lane; p < active; p += share) {
+      if (p != lane) pair = *(const f32x2*)(ml + 2 * (p * R + r));
+      const float s = factor_of(pair[0], top);
+      sh_factor[p * R + r] = s;
+      total += pair[1] * s;
     }
-  }
   total = reduce_lanes(total, share, [](float u, float v) { return u + v; });
   if (r < R && lane == 0) {
     const bool none = n - T + 1 + r % T <= 0;
     const float lse2 = lse_of(top, total, none);
-    sh_top[r] = top;
     sh_total[r] = total;
     sh_lse[r] = lse2;
     if (part == 0 && a.lse) a.lse[(int64_t)w.seg * R + r] = lse_out(lse2, none);
   }
   __syncthreads();
-  for (int f4 = f0; f4 < f1; f4 += kAttendThreads) {
-    const int at = f4 + fi, row = min(at / (D / 4), R - 1);
-    auto factor = [&](int p) __attribute__((always_inline)) { return fit ? sh_factor[p * R + row] : factor_of(ml[2 * (p * R + row)], sh_top[row]); };
+  for (int first = part * at_once; first < units; first += active * at_once) {
+    const int unit = min(first + sub, units - 1), row = unit / (D / 64), at = unit * 64 + f * 4;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (grp < groups && at < f1) {
-      int p = grp;
-      if (f4 == f0) {
-#pragma unroll
-        for (int k = 0; k < kJoinFirst; ++k, p += groups)
-          if (p < active) o += x[k] * factor(p);
-      }
-#pragma unroll 4
-      for (; p < active; p += groups) o += *(const f32x4*)(po + (int64_t)p * R * D + at * 4) * factor(p);
+#pragma unroll 2
+    for (int p = grp; p < active; p += groups) {
+      if (first != part * at_once || p != grp || first + sub >= units) x = *(const f32x4*)(po + (int64_t)p * R * D + at);
+      o += x * sh_factor[p * R + row];
     }
-    if (groups > 1) {                                  // (then this is the only round)
-      sh_o[tid] = o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[e] += __shfl_xor(o[e], 16);
+      if (groups > 2) o[e] += __shfl_xor(o[e], 32);
+    }
+    if (groups > 4) {
+      if ((tid & (kWave - 1)) < 16) sh_o[tid / kWave][f] = o;
       __syncthreads();
       if (grp == 0)
-        for (int u = 1; u < groups; ++u) o += sh_o[u * nf + fi];
+        for (int v = 1; v < groups / 4; ++v) o += sh_o[tid / kWave + v][f];
+      __syncthreads();
     }
-    if (grp == 0 && at < f1)
-      store_out<KIND>(a.out + ((int64_t)w.seg * R * D + at * 4) * (int)sizeof(typename Kind<KIND>::wide),
-                      output_of(o, sh_total[row], n - T + 1 + row % T <= 0));
+    if (grp == 0 && first + sub < units)
+      store_out<KIND>(a.out + ((int64_t)w.seg * R * D + at) * (int)sizeof(typename Kind<KIND>::wide), output_of(o, sh_total[row], n - T + 1 + row % T <= 0));
   }
-  if (a.w_out) add_weights<kAttendThreads>(h, a, w.start, w.tile, part * each, end, sh_lse);
+  if (a.w_out) add_weights<kAttendThreads>(h, a, w.start, w.tile, part * w.each, end, sh_lse);
 }
 
 // ------------------------------------------------------------------ host
@@ -751,7 +740,7 @@ static AttendPlan plan_attend(const slkv_cache_desc* d, int T, bool weights) {
   AttendPlan p;
   const int64_t S = (int64_t)d->B * d->Hkv, rows = d->h_offsets[S] - d->h_offsets[0];
   const int64_t R = (int64_t)(d->Hq / d->Hkv) * T;
-  constexpr int64_t kMost = 1 << 20;                   // a part's bytes are a 32-bit number
+  constexpr int64_t kMost = 1 << 21;                   // a part's bytes are a 32-bit number
   auto round = [](int64_t n) { return (n + kTileRows - 1) / kTileRows * kTileRows; };
   const double row_bytes = d->d * kind_bits(d->dtype) / 4;
   const int rt = R <= 16 ? 1 : R <= 32 ? 2 : 4;
@@ -769,7 +758,8 @@ static AttendPlan plan_attend(const slkv_cache_desc* d, int T, bool weights) {
     p.rows_each = std::max<int64_t>(kTileRows, round(most));
   } else {
     // The workgroups that are on the chip at once share the rows.  Segments end inside a part, so a part is made larger until all are on the chip.
-    p.rows_each = std::min(kMost, std::max<int64_t>(p.waves * 32, round((rows + places - 1) / places)));
+    const int64_t least = std::max<int64_t>(p.waves * 32, round(most / (kJoinPairs / R) + 1));
+    p.rows_each = std::min(kMost, std::max<int64_t>(least, round((rows + places - 1) / places)));
     for (int tries = 0; tries < 4 && S <= places / 4 * 3 && p.rows_each < kMost; ++tries) {
       int64_t parts = 0;
       for (int64_t s = 0; s < S; ++s) parts += parts_of(d, s, p.rows_each);
@@ -868,7 +858,6 @@ extern "C" slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv
   hipStream_t const stream = (hipStream_t)hip_stream;
 
   a.tiles_each = (int32_t)(p.rows_each / kTileRows);
-  a.per_tiles_each = 1.0 / a.tiles_each;
   auto launch = [&](auto tab, int64_t s0, int64_t ns) {
     using TAB = decltype(tab);
     tab.nseg = (int32_t)ns;

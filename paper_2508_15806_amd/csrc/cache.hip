@@ -394,17 +394,22 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays 
     if (first < want) {
       const float* keys = in.weight + start;
       const int rows_each = (m + kEvictThreads - 1) / kEvictThreads * kWave;     // of a wave
-      const int i0 = wave * rows_each + lane, i1 = min(m, (wave + 1) * rows_each);
+      const int b0 = wave * rows_each, i0 = b0 + lane, i1 = min(m, b0 + rows_each);
       uint32_t least, k;
       evict_threshold(l, keys, m, (uint32_t)want, i0, i1, least, k);
       auto key_of = [&](int i) __attribute__((always_inline)) { return m <= kEvictHeld ? l.held[i] : weight_key(keys[i]); };
       // a wave counts its kept rows by votes, then emits them at the places that the waves before it leave
       uint32_t gt = 0, eq = 0;
-#pragma unroll 4
-      for (int i = i0; i - lane < i1; i += kWave) {
-        const uint32_t x = i < i1 ? key_of(i) : 0u;
-        gt += (uint32_t)__popcll(__ballot(i < i1 && x > least));
-        eq += (uint32_t)__popcll(__ballot(i < i1 && x == least));
+      for (int b = b0; b < i1; b += 4 * kWave) {
+        uint32_t x[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x[t] = b + t * kWave + lane < i1 ? key_of(b + t * kWave + lane) : 0u;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const bool in = b + t * kWave + lane < i1;
+          gt += (uint32_t)__popcll(__ballot(in && x[t] > least));
+          eq += (uint32_t)__popcll(__ballot(in && x[t] == least));
+        }
       }
       if (lane == 0) l.ends[0][wave] = gt, l.ends[1][wave] = eq;
       __syncthreads();
@@ -416,7 +421,8 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays 
       at += min(e, k);
       const uint64_t below = (1ull << lane) - 1;
       const bool mine = (int)(at + gt + eq) > first && (int)at < first + rows;   // some of the wave's rows may be in the slice
-      for (int i = mine ? i0 : i1 + lane; i - lane < i1; i += kWave) {
+      for (int b = mine ? b0 : i1; b < i1; b += kWave) {
+        const int i = b + lane;
         const uint32_t x = i < i1 ? key_of(i) : 0u;
         const bool is_eq = i < i1 && x == least;
         const uint64_t eqs = __ballot(is_eq);

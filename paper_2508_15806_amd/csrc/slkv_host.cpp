@@ -115,8 +115,8 @@ slkv_status validate_cache_desc(const slkv_cache_desc* d, const char* name) {
   if (d->reserved[0] || d->reserved[1]) return fail(SLKV_ERR_BAD_ARG, "%s.reserved must be 0", name);
   const int64_t S = (int64_t)d->B * d->Hkv;
   slkv_status st = validate_offsets(d->h_offsets, S, "h_offsets");
-  for (int64_t s = 0; st == SLKV_OK && s < S; ++s)     // the kernels round a segment's rows up in 32-bit numbers
-    if (d->h_offsets[s + 1] - d->h_offsets[s] > (int64_t(1) << 30)) st = fail(SLKV_ERR_UNSUPPORTED, "segment %lld: a room of more than 2^30 rows", (long long)s);
+  for (int64_t s = 0; st == SLKV_OK && s < S; ++s)     // the kernels divide numbers of 32 rows as fp32
+    if (d->h_offsets[s + 1] - d->h_offsets[s] > (int64_t(1) << 25)) st = fail(SLKV_ERR_UNSUPPORTED, "segment %lld: a room of more than 2^25 rows", (long long)s);
   return st;
 }
 

@@ -36,7 +36,7 @@ def test_struct_sizes_match_the_header():
 @pytest.mark.parametrize("over,status", [
     (dict(d=96), 4), (dict(Hq=7), 2), (dict(dtype=5), 2), (dict(dtype=-1), 2), (dict(B=0, offsets=[0]), 2),
     (dict(offsets=[0, 100, 90, 130, 190]), 2), (dict(offsets=[-1, 100, 130, 130, 190]), 2), (dict(offsets=[0, 100, 130, 130, 2 ** 31]), 2),
-    (dict(Hkv=0, Hq=0, offsets=[0]), 2), (dict(offsets=[0, 0, 2 ** 30 + 1, 2 ** 30 + 1, 2 ** 30 + 1]), 4),
+    (dict(Hkv=0, Hq=0, offsets=[0]), 2), (dict(offsets=[0, 0, 2 ** 25 + 1, 2 ** 25 + 1, 2 ** 25 + 1]), 4),
 ])
 def test_descriptors(over, status):
     lay = layout(**over)
