@@ -119,23 +119,46 @@ constexpr int kBlockRows = 32;        // rows of a workgroup of fill and of rows
 constexpr int kThreads = 256;
 template <int N>
 using RowsTab = SegWords<N, 3>;       // w[0] room of the segment (first row), w[1] its rows outside the cache, w[2] workgroups before it
+// The same for more segments, whose rooms and rows outside are below 2^16: a launch for each 290 segments took 512 of them 4 us longer, and the host 4.
+struct RowsTabShort {
+  static constexpr int kSegs = 800, kGroup = 16;
+  int32_t nseg, seg0, least;          // least: workgroups of a segment without rows
+  int32_t w[3][kSegs / kGroup];       // as above, of every 16th segment
+  uint16_t room[kSegs], count[kSegs];
+};
 
 // The segment of a workgroup.  One wave looks it up for all: the table stands in the kernel's arguments, which thousands of workgroups read past the caches.
 struct RowsAt { int seg, first, start, room, other, count; };
 template <class TAB>
 __device__ __forceinline__ RowsAt find_rows(const TAB& tab, RowsAt& shared) {
   if (threadIdx.x < kWave) {
-    const int block = blockIdx.x;
-    const int i = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
-    if (threadIdx.x == 0) {
+    const int block = blockIdx.x, lane = threadIdx.x;
+    if constexpr (std::is_same_v<TAB, RowsTabShort>) {
+      const int groups = (tab.nseg + TAB::kGroup - 1) / TAB::kGroup;
+      const int g = __popcll(__ballot(lane < groups && tab.w[2][min(lane, groups - 1)] <= block)) - 1, i = g * TAB::kGroup + lane;
+      const bool in = lane < TAB::kGroup && i < tab.nseg;
       RowsAt r;
+      r.room = in ? tab.room[i] : 0;
+      r.count = in ? tab.count[i] : 0;
+      const int blocks = in ? max(tab.least, (min(r.room, r.count) + kBlockRows - 1) / kBlockRows) : 0;
+      const int first = tab.w[2][g] + (int)row_incl_scan((uint32_t)blocks) - blocks;
+      r.start = tab.w[0][g] + (int)row_incl_scan((uint32_t)r.room) - r.room;
+      r.other = tab.w[1][g] + (int)row_incl_scan((uint32_t)r.count) - r.count;
       r.seg = tab.seg0 + i;
-      r.first = (block - tab.w[2][i]) * kBlockRows;
-      r.start = tab.w[0][i];
-      r.room = tab.w[0][i + 1] - r.start;
-      r.other = tab.w[1][i];
-      r.count = tab.w[1][i + 1] - r.other;
-      shared = r;
+      r.first = (block - first) * kBlockRows;
+      if (blocks && first <= block && block < first + blocks) shared = r;
+    } else {
+      const int i = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
+      if (lane == 0) {
+        RowsAt r;
+        r.seg = tab.seg0 + i;
+        r.first = (block - tab.w[2][i]) * kBlockRows;
+        r.start = tab.w[0][i];
+        r.room = tab.w[0][i + 1] - r.start;
+        r.other = tab.w[1][i];
+        r.count = tab.w[1][i + 1] - r.other;
+        shared = r;
+      }
     }
   }
   __syncthreads();
@@ -497,6 +520,33 @@ static void for_tables(int64_t S, WORD word, BLOCKS blocks_of, F f) {
   for (int64_t s0 = 0; s0 < S; s0 += MANY) one(TABLE<MANY>{}, s0, std::min<int64_t>(MANY, S - s0));
 }
 
+// The launches of fill and rows: room offsets, offsets outside, workgroups of a segment without rows.
+template <class F>
+static void for_rows(int64_t S, const int64_t* room, const int64_t* other, int least, F f) {
+  auto blocks_of = [&](int64_t s) { return std::max<int64_t>(least, (std::min(other[s + 1] - other[s], room[s + 1] - room[s]) + kBlockRows - 1) / kBlockRows); };
+  bool is_short = S > kFewSegs;
+  for (int64_t s = 0; is_short && s < S; ++s) is_short = room[s + 1] - room[s] < 65536 && other[s + 1] - other[s] < 65536;
+  if (!is_short) return for_tables<RowsTab, kManySegs3, 2>(S, [&](int64_t s, int r) { return (int32_t)(r == 0 ? room[s] : other[s]); }, blocks_of, f);
+  for (int64_t s0 = 0; s0 < S; s0 += RowsTabShort::kSegs) {
+    RowsTabShort tab;
+    tab.nseg = (int32_t)std::min<int64_t>(RowsTabShort::kSegs, S - s0);
+    tab.seg0 = (int32_t)s0;
+    tab.least = least;
+    int64_t blocks = 0;
+    for (int i = 0; i < tab.nseg; ++i) {
+      if (i % RowsTabShort::kGroup == 0) {
+        tab.w[0][i / RowsTabShort::kGroup] = (int32_t)room[s0 + i];
+        tab.w[1][i / RowsTabShort::kGroup] = (int32_t)other[s0 + i];
+        tab.w[2][i / RowsTabShort::kGroup] = (int32_t)blocks;
+      }
+      tab.room[i] = (uint16_t)(room[s0 + i + 1] - room[s0 + i]);
+      tab.count[i] = (uint16_t)(other[s0 + i + 1] - other[s0 + i]);
+      blocks += blocks_of(s0 + i);
+    }
+    if (blocks) f(tab, (int)blocks);
+  }
+}
+
 template <class F>
 static void with_dim(int d, F f) {
   if (d == 64) f(std::integral_constant<int, 64>{});
@@ -547,13 +597,10 @@ extern "C" slkv_status slkv_fill_cache(const slkv_cache_desc* desc, const slkv_c
   ScopedKernelTimer timer(SLKV_K_CACHE_STORE);
   with_kind(desc->dtype, [&](auto kind) {
     with_dim(desc->d, [&](auto dim) {
-      for_tables<RowsTab, kManySegs3, 2>(
-          S, [&](int64_t s, int r) { return (int32_t)(r == 0 ? desc->h_offsets[s] : h_src_offsets[s]); },
-          [&](int64_t s) { return std::max<int64_t>(1, ceil_div(h_src_offsets[s + 1] - h_src_offsets[s], kBlockRows)); },
-          [&](const auto& tab, int blocks) {
-            SLKV_LAUNCH((fill_kernel<decltype(kind)::value, decltype(dim)::value, std::decay_t<decltype(tab)>>), dim3(blocks), dim3(kThreads), 0,
-                        (hipStream_t)hip_stream, arrays_of(cache), (const unsigned char*)d_k_rows, (const unsigned char*)d_v_rows, d_pos_rows, tab);
-          });
+      for_rows(S, desc->h_offsets, h_src_offsets, 1, [&](const auto& tab, int blocks) {
+        SLKV_LAUNCH((fill_kernel<decltype(kind)::value, decltype(dim)::value, std::decay_t<decltype(tab)>>), dim3(blocks), dim3(kThreads), 0,
+                    (hipStream_t)hip_stream, arrays_of(cache), (const unsigned char*)d_k_rows, (const unsigned char*)d_v_rows, d_pos_rows, tab);
+      });
     });
   });
   return launch_status("fill");
@@ -618,13 +665,10 @@ extern "C" slkv_status slkv_cache_rows(const slkv_cache_desc* desc, const slkv_c
   ScopedKernelTimer timer(SLKV_K_CACHE_ROWS);
   with_kind(desc->dtype, [&](auto kind) {
     with_dim(desc->d, [&](auto dim) {
-      for_tables<RowsTab, kManySegs3, 2>(
-          S, [&](int64_t s, int r) { return (int32_t)(r == 0 ? desc->h_offsets[s] : h_out_offsets[s]); },
-          [&](int64_t s) { return ceil_div(std::min(h_out_offsets[s + 1] - h_out_offsets[s], desc->h_offsets[s + 1] - desc->h_offsets[s]), kBlockRows); },
-          [&](const auto& tab, int blocks) {
-            SLKV_LAUNCH((rows_kernel<decltype(kind)::value, decltype(dim)::value, std::decay_t<decltype(tab)>>), dim3(blocks), dim3(kThreads), 0,
-                        (hipStream_t)hip_stream, arrays_of(cache), (unsigned char*)d_k_rows, (unsigned char*)d_v_rows, d_pos_rows, tab);
-          });
+      for_rows(S, desc->h_offsets, h_out_offsets, 0, [&](const auto& tab, int blocks) {
+        SLKV_LAUNCH((rows_kernel<decltype(kind)::value, decltype(dim)::value, std::decay_t<decltype(tab)>>), dim3(blocks), dim3(kThreads), 0,
+                    (hipStream_t)hip_stream, arrays_of(cache), (unsigned char*)d_k_rows, (unsigned char*)d_v_rows, d_pos_rows, tab);
+      });
     });
   });
   return launch_status("rows");

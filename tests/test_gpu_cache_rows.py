@@ -106,6 +106,31 @@ def as_bf16(values):
     return np.where(np.abs(values) >= 2.0 ** 128, np.copysign(np.inf, values), values)
 
 
+@pytest.mark.parametrize("S,long", [(64, 0), (65, 0), (300, 65535), (300, 65536), (301, 70001), (799, 0), (800, 0), (801, 0), (1700, 0)])
+def test_segment_tables(S, long):
+    """Segments at the ends of the tables that launches hold, one of them longer than a 16-bit count."""
+    rng = np.random.default_rng(S + long)
+    counts = rng.integers(0, 40, S)
+    counts[rng.integers(0, S, S // 4)] = 0
+    if long:
+        counts[S // 3] = long
+    rooms = counts + rng.integers(0, 3, S) * (counts < 40)
+    src, offsets = np.concatenate([[0], np.cumsum(counts)]) + 3, np.concatenate([[0], np.cumsum(rooms)]) + 1
+    cache = api.Cache("bf16", S, 1, 1, 64, offsets)
+    mark(cache)
+    k, v = normal(rng, (int(src[-1]), 64), "bf16"), normal(rng, (int(src[-1]), 64), "bf16")
+    cache.fill(k, v, src)
+    rows = torch.from_numpy(np.concatenate([offsets[s] + np.arange(c) for s, c in enumerate(counts)]).astype(np.int64)).cuda()
+    assert cache.lengths.cpu().tolist() == counts.tolist()
+    assert torch.equal(cache.k[rows], k[3:]) and torch.equal(cache.v[rows], v[3:])
+    assert bool((cache.weight[rows] == 0).all()) and bool((cache.pos == -9).all())
+    other = torch.ones(cache.rows_in_all, dtype=torch.bool, device="cuda")
+    other[rows] = False
+    assert bool((cache.k.view(torch.uint8).reshape(-1, 128)[other] == 0x5A).all())
+    back = cache.rows(src)
+    assert torch.equal(back[0][3:], k[3:]) and torch.equal(back[1][3:], v[3:])
+
+
 @pytest.mark.parametrize("dtype", ["bf16_kv8", "bf16_kv4"])
 def test_every_bf16_value(dtype):
     """All 65536 codes: as they are (E4M3), and in blocks of like magnitude and against a larger neighbour (MXFP4)."""
