@@ -384,16 +384,31 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
   auto step = [&](auto careful_c, const typename A::KRegs& kr, const typename A::VRegs& vr, const int key0) __attribute__((always_inline)) {
     constexpr bool careful = decltype(careful_c)::value;
     f32x4 x[RT][A::kTiles];
+    if constexpr (A::kF32) {
+      // several sums side by side: one chain of D/4 additions is what the result's error comes from
+      constexpr int kChains = RT == 4 ? 2 : 4;
+      f32x4 s[RT][kChains];
 #pragma unroll
-    for (int t = 0; t < A::kTiles; ++t) {
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) x[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < kChains; ++i) s[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < kProducts; ++u) {
-        if constexpr (A::kF32) {
+      for (int u = 0; u < kProducts; ++u)
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) x[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr.w[t][u]), qf[rt][u], x[rt][t], 0, 0, 0);
-        } else {
+        for (int rt = 0; rt < RT; ++rt)
+          s[rt][u % kChains] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr.w[0][u]), qf[rt][u], s[rt][u % kChains], 0, 0, 0);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        x[rt][0] = s[rt][0] + s[rt][1];
+        if constexpr (kChains == 4) x[rt][0] += s[rt][2] + s[rt][3];
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < A::kTiles; ++t) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) x[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < kProducts; ++u) {
           const u32x4 ko = A::k_operand(kr, t, u);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) x[rt][t] = A::mfma(ko, q[rt][u], x[rt][t]);
