@@ -353,14 +353,15 @@ typedef struct {
  *   MXFP4: the exponent of a block of 32 is the smallest, not below -127, at which its largest magnitude is at most 7 (half
  *     a step above 6); elements go to the nearest value, ties to the even code, beyond 6 to 6; a block with an infinity or
  *     NaN is a block of NaN.
- * d_pos_rows [rows] int32 (d_kept_idx of slkv_compress_layer), may be NULL: the cache's positions stay as they are then.
+ * d_pos_rows [rows] int32 (d_kept_idx of slkv_compress_layer; needs cache->d_pos), may be NULL: the cache's positions stay as they are then.
+ * The sources may not overlap the cache.
  * Errors: NULL, BAD_ARG, UNSUPPORTED, CAPACITY (a segment's rows exceed its room), HIP. */
 slkv_status slkv_fill_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const int64_t* h_src_offsets,
                             const void* d_k_rows, const void* d_v_rows, const int32_t* d_pos_rows, void* hip_stream);
 
 /* T rows of every segment enter behind those in use, converted as by slkv_fill_cache, with weight 0; d_lengths grows by T.
  * Element (b, h, t, :) of d_k at b*k_stride[0] + h*k_stride[1] + t*k_stride[2], rows of d elements contiguous, strides
- * multiples of 16 bytes, >= 0; the same for d_v.  d_pos [B][T] int32, may be NULL.  1 <= T <= 64.
+ * multiples of 16 bytes, >= 0; the same for d_v.  d_pos [B][T] int32 (needs cache->d_pos), may be NULL: as above.  1 <= T <= 64.
  * d_at [B*Hkv] int32, may be NULL (d_lengths): the rows enter behind the first d_at[s] instead, and the new length is d_at[s] + T.
  * It may be d_lengths itself.  Rows that the room does not hold are left out, and the length is the room then.
  * Errors: NULL, BAD_ARG, UNSUPPORTED, HIP. */

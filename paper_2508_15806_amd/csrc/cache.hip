@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const CacheArrays c, con
   }
   if ((int)threadIdx.x < rows) {
     const int64_t row = dst0 + first + (int)threadIdx.x;
-    if (c.pos && pos_src) c.pos[row] = pos_src[src0 + first + (int)threadIdx.x];
+    if (pos_src) c.pos[row] = pos_src[src0 + first + (int)threadIdx.x];
     if (c.weight) c.weight[row] = 0.f;
   }
 }
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs a, co
     }
   }
   if (lane < fit) {
-    if (a.c.pos && a.pos_src) a.c.pos[(int64_t)start + n + lane] = a.pos_src[(int64_t)b * T + lane];
+    if (a.pos_src) a.c.pos[(int64_t)start + n + lane] = a.pos_src[(int64_t)b * T + lane];
     if (a.c.weight) a.c.weight[(int64_t)start + n + lane] = 0.f;
   }
   if (lane == 0) a.c.lengths[seg] = n + fit;
@@ -336,7 +336,7 @@ __device__ __forceinline__ void evict_threshold(EvictLds& l, const float* __rest
 #pragma unroll 4
     for (int i = i0; i < i1; i += kWave) {
       const uint32_t x = key_of(i), d = x - lo;
-      if (x >= lo && (d >> shift) < (uint32_t)kHistBins) atomicAdd(&l.hist[d >> shift], 1u);
+      if (x >= lo && (d >> shift) < (1u << (bits - shift))) atomicAdd(&l.hist[d >> shift], 1u);   // (a last digit may have fewer bits)
     }
     __syncthreads();
     select_bin<kEvictThreads>(l.hist, k, l.scan, l.res);
@@ -587,6 +587,7 @@ extern "C" slkv_status slkv_fill_cache(const slkv_cache_desc* desc, const slkv_c
   if ((st = validate_offsets(h_src_offsets, S, "h_src_offsets")) != SLKV_OK) return st;
   if (!cache->d_lengths) return fail(SLKV_ERR_NULL, "cache: d_lengths is NULL");
   if (h_src_offsets[S] > h_src_offsets[0] && (!d_k_rows || !d_v_rows)) return fail(SLKV_ERR_NULL, "a required device pointer is NULL");
+  if (d_pos_rows && !cache->d_pos) return fail(SLKV_ERR_NULL, "cache: d_pos is NULL");
   const void* ptrs[] = {d_k_rows, d_v_rows, d_pos_rows};
   for (const void* ptr : ptrs)
     if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);
@@ -617,6 +618,7 @@ extern "C" slkv_status slkv_append_cache(const slkv_cache_desc* desc, const slkv
   if (T < 1) return fail(SLKV_ERR_BAD_ARG, "T must be >= 1");
   if (T > 64) return fail(SLKV_ERR_UNSUPPORTED, "T = %d > 64", T);
   if (!d_k || !d_v || !k_stride || !v_stride) return fail(SLKV_ERR_NULL, "a required pointer is NULL");
+  if (d_pos && !cache->d_pos) return fail(SLKV_ERR_NULL, "cache: d_pos is NULL");
   const void* ptrs[] = {d_k, d_v, d_pos, d_at};
   for (const void* ptr : ptrs)
     if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);

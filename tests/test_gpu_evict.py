@@ -88,6 +88,20 @@ def test_equal_weights(n):
     check(cache, [n // 3, n // 2, n // 5, n - 7], 5)
 
 
+@pytest.mark.parametrize("around", [0x3F800000, 0x3F800100, 0x3F7FFF00, 0x40000000])
+@pytest.mark.parametrize("width,low", [(64, 0.0), (64, -1.0), (300, 1e-30), (2, 0.0), (1000, 0.999)])
+def test_many_weights_a_few_steps_apart(around, width, low):
+    """Thousands of weights among neighbouring floats on both sides of a digit's end, and one far below that widens the range: the last digit is decided
+    among them."""
+    n = 9000
+    rng = np.random.default_rng([around, width])
+    cache = random_cache(rng, "bf16", 1, 4, 1, 64, [n] * 4)
+    bits = around + rng.integers(-(width // 2), width - width // 2, 4 * n)
+    cache.weight.copy_(torch.from_numpy(bits.astype(np.uint32).view(np.float32)))
+    cache.weight[::n] = low
+    check(cache, [700, n // 2, n - 300, 5000], 7)
+
+
 def test_weights_that_are_no_ordinary_numbers():
     n = 2000
     rng = np.random.default_rng(1)

@@ -111,6 +111,7 @@ def test_fill_refuses_before_touching_the_gpu():
     assert fill(src=[0, 10, 5, 30, 60]) == 2 and fill(src=[-1, 10, 15, 30, 60]) == 2
     assert fill(src=[2 ** 31 - 61, 2 ** 31 - 1, 2 ** 31, 2 ** 31, 2 ** 31]) == 2
     assert fill(k=ODD) == 2 and fill(pos=ODD) == 2
+    assert fill(arr=arrays(d_pos=NULL)) == 1                                          # positions without a place for them
 
 
 def append(arr=None, T=1, k=FAKE, v=FAKE, ks=(256, 128, 128), vs=(256, 128, 128), pos=NULL, at=NULL, **over):
@@ -126,6 +127,7 @@ def test_append_refuses_before_touching_the_gpu():
     assert append(T=0) == 2 and append(T=65) == 4
     assert append(ks=(256, 128, 4)) == 2 and append(vs=(-256, 128, 128)) == 2         # 8 bytes; negative
     assert append(k=ODD) == 2 and append(pos=ODD) == 2 and append(at=ODD) == 2
+    assert append(pos=FAKE, arr=arrays(d_pos=NULL)) == 1
 
 
 def test_rows_refuses_before_touching_the_gpu():
