@@ -50,6 +50,37 @@ def test_long_segments_are_split(dtype):
     check(cache, normal(rng, (2, 4, 3, 128), dtype), 3)
 
 
+@pytest.mark.parametrize("dtype,d,G,T,n", [("bf16", 64, 1, 1, 150001), ("bf16_kv4", 128, 2, 1, 300007), ("f32", 64, 64, 1, 20011), ("f16", 128, 16, 4, 30001), ("bf16_kv8", 64, 3, 10, 40009)])
+def test_one_segment_over_the_whole_chip(dtype, d, G, T, n):
+    # one segment in as many parts as there are workgroups on the chip, or as the joining launch takes with many queries
+    rng = np.random.default_rng(n)
+    cache = random_cache(rng, dtype, 1, 1, G, d, [n], rooms=[n + 100])
+    check(cache, normal(rng, (1, G, T, d), dtype), T)
+
+
+@pytest.mark.parametrize("S", [90, 700])
+def test_many_segments_with_long_ones_among_them(S):
+    rng = np.random.default_rng(S)
+    lens = rng.integers(0, 200, S)
+    lens[[3, S // 2, S - 1]] = [9000, 4001, 12000]
+    cache = random_cache(rng, "bf16_kv8", S, 1, 4, 64, lens.tolist(), rooms=(lens + 5).tolist())
+    check(cache, normal(rng, (S, 4, 2, 64), "bf16_kv8"), 2)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_shapes(seed):
+    rng = np.random.default_rng([77, seed])
+    dtype, d = DTYPES[seed % 5], int(rng.choice([64, 128]))
+    G = int(rng.choice([1, 2, 3, 4, 5, 8, 12]))
+    T = int(rng.integers(1, 64 // G + 1)) if seed % 3 else 1
+    B_, Hkv = int(rng.integers(1, 7)), int(rng.choice([1, 2, 3, 8]))
+    top = int(2.0 ** rng.uniform(0, 12))
+    lens = [int(x) for x in rng.integers(0, top + 1, B_ * Hkv)]
+    rooms = [n + int(x) for n, x in zip(lens, rng.integers(0, 400, B_ * Hkv))]
+    cache = random_cache(rng, dtype, B_, Hkv, G, d, lens, rooms=rooms, before=int(rng.integers(0, 70)))
+    check(cache, normal(rng, (B_, G * Hkv, T, d), dtype), T)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_lengths_far_below_the_room(dtype):
     # the parts are planned for the room: they are spread over what is in use
