@@ -202,7 +202,7 @@ class Cache:
         self._workspaces = {}
 
     def _tensor(self, t, shape, tdt, name, contiguous=True):
-        if t.dtype != tdt or tuple(t.shape) != shape:
+        if t.dtype != tdt or t.shape != shape:
             raise ValueError("%s: %s of shape %s wanted, got %s of shape %s" % (name, tdt, shape, t.dtype, tuple(t.shape)))
         if t.device != self.device:
             raise ValueError("%s is on %s, the cache on %s" % (name, t.device, self.device))

@@ -387,7 +387,7 @@ def slkv_attend_workspace_bytes(layout, T, want_weights):
 def slkv_attend_cache(layout, cache, q, out, workspace, lse=None, weight_out=None, stream=None):
     """q, out: [B, Hq, T, d]; lse [B, Hq, T] fp32; weight_out [rows] fp32."""
     _check(lib().slkv_attend_cache(layout.address, cache.address, q.shape[2], _ptr(q), _ptr(out), _ptr(lse), _ptr(weight_out), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream(stream)))
+                                   workspace.nbytes, _stream(stream)))
 
 
 def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, kept_idx=None, stream=None):

@@ -373,7 +373,13 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
       for (int u = 0; u < kProducts; ++u) q[rt][u] = *(const u32x4*)(p + A::dim_of(u, g) * 2);
     }
   }
-  const int64_t tile_seg = at.tile;
+  // Logits go through a buffer as well, of no bytes where nobody asks for weights, and at places beyond its end for queries that are not there, so that a step has no
+  // branch for them.  (256 segments of 536 to 5994 E4M3 rows: 34.5 us with the logits, 29.1 without, of which the stores are 2.5 to 3, whole segments' weights 2.)
+  const __amdgpu_buffer_rsrc_t logits = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(a.logits ? a.logits + (int64_t)(at.tile + begin / kTileRows) * R * kTileRows : nullptr), 0, a.logits ? tiles_of(end - begin) * kTileRows * R * 4 : 0, 0x00027000);
+  uint32_t logit_at[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) logit_at[rt] = rt * 16 + rq < R ? (rt * 16 + rq) * kTileRows * 4 + g * kEach * 4 : 0x80000000u;
 
   float ref[RT], sum[RT];
   f32x4 acc[RT][kVD];
@@ -416,6 +422,7 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
       }
     }
     const int mine = key0 + g * kEach;                 // the lane's rows: mine .. mine + kEach - 1
+    const uint32_t logit_step = ((key0 - begin) / kTileRows * R * kTileRows + key0 % kTileRows) * 4;
     const bool tail = key0 + A::kStep > min(end, n - T + 1);
     float p[RT][kEach];
 #pragma unroll
@@ -431,10 +438,10 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
 #pragma unroll
       for (int j = 0; j < kEach; ++j) top = fmaxf(top, p[rt][j]);
       top *= a.c_log2;
-      if (a.logits && rt * 16 + rq < R) {
-        float* l = a.logits + ((tile_seg + key0 / kTileRows) * R + rt * 16 + rq) * kTileRows + mine % kTileRows;
 #pragma unroll
-        for (int j = 0; j < kEach; j += 4) *(f32x4*)(l + j) = f32x4{p[rt][j], p[rt][j + 1], p[rt][j + 2], p[rt][j + 3]};
+      for (int j = 0; j < kEach; j += 4) {
+        const f32x4 l = f32x4{p[rt][j], p[rt][j + 1], p[rt][j + 2], p[rt][j + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, l), logits, logit_at[rt] + logit_step + j * 4, 0, 0);
       }
       if (__ballot(top > ref[rt] + A::kAbove)) {
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -559,14 +566,14 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
       A::load_v(vr0, rows, place);
     }
   }
-  bool finite = true;
+  float zero[4] = {0.f, 0.f, 0.f, 0.f};                // NaN where a sum is not finite
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int m = 0; m < kVD; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) finite = finite && fabsf(acc[rt][m][e]) < INFINITY;
-  if (__ballot(!finite)) {
+      for (int e = 0; e < 4; ++e) zero[e] = fmaf(acc[rt][m][e], 0.f, zero[e]);
+  if (__ballot((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.f)) {
     clear();
     place = A::place_of(wave, lane);
     for (int key0 = begin + wave * A::kStep; key0 < end; key0 += kStride) {
