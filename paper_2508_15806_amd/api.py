@@ -277,8 +277,8 @@ class Cache:
         row in the cache hold nothing in particular."""
         rows = int(out_offsets[-1])
         with self._on(stream):
-            k, v = torch.empty((2, rows, self.d), dtype=self.query_dtype, device=self.device).unbind(0)
-            pos = torch.empty((rows,), dtype=torch.int32, device=self.device) if self.pos is not None else None
+            k, v = self.k.new_empty((2, rows, self.d), dtype=self.query_dtype).unbind(0)
+            pos = self.pos.new_empty((rows,)) if self.pos is not None else None
             B.slkv_cache_rows(self.layout, self._arrays, out_offsets, k, v, pos)
         return k, v, pos
 

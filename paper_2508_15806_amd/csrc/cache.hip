@@ -386,8 +386,8 @@ __device__ __forceinline__ void evict_threshold(EvictLds& l, const float* __rest
 }
 
 // A workgroup copies a slice of a segment's kept rows, `slice` of them, UNITS of 16 bytes a row of K; which rows these are every workgroup of the segment finds by
-// itself, so that nothing waits for a selection that is not its own: 128 segments of up to 3345 rows, half of them kept, XXA us, with a launch that selects (10 us, by the
-// longest segment) and one that copies 40.  The copy is bound by memory: 16 rows of every wave are on their way at once.
+// itself, so that nothing waits for a selection that is not its own: 128 segments of up to 3345 rows, nearly all of them kept, 31 us (137 MB), with a launch that selects
+// (10 us, by the longest segment) and one that copies 40.  Of 16 segments of up to 10047 rows down to 1024 on average (MXFP4) the selection is 11 of 19 us.  The copy is bound by memory: 16 rows of every wave are on their way at once.
 template <int UNITS, int SCALES, class TAB>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays in, const CacheArrays out, int32_t* __restrict__ kept_idx, int w, int slice, const TAB tab) {
   __shared__ EvictLds l;
