@@ -290,10 +290,18 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const CacheArrays c, uns
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
 constexpr int kEvictHeld = 12288;     // keys that stay in LDS
 constexpr int kEvictRank = 256;       // keys that are ranked against each other
-constexpr int kEvictSlice = 1024;     // rows that a workgroup copies, at most
+constexpr int kEvictSlice = 512;      // rows that a workgroup copies, at most (512 segments of 512 rows: 69 us; 79 with 1024)
 constexpr int kEvictSegs = 240;
 template <int N>
 using EvictTab = SegWords<N, 4>;      // w[0] room of the segment, w[1] its room in the other cache, w[2] workgroups before it, w[3] max(C_h, w)
+// The same for more than kEvictSegs segments, whose rooms are below 2^16: one launch (512 segments of up to 1634 rows to 512: 79 us at 1024 rows a slice;
+// 113 in three launches).
+struct EvictTabShort {
+  static constexpr int kSegs = 560, kGroup = 16;
+  int32_t nseg, seg0;
+  int32_t w[3][kSegs / kGroup];       // as above, of every 16th segment
+  uint16_t room[kSegs], other[kSegs], cap[kSegs];
+};
 
 __device__ __forceinline__ uint32_t weight_key(float v) { return v != v ? 0xffffffffu : float_key(v); }
 
@@ -391,17 +399,36 @@ __device__ __forceinline__ void evict_threshold(EvictLds& l, const float* __rest
 template <int UNITS, int SCALES, class TAB>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays in, const CacheArrays out, int32_t* __restrict__ kept_idx, int w, int slice, const TAB tab) {
   __shared__ EvictLds l;
-  __shared__ int32_t sh_at[6];
+  __shared__ int32_t sh_at[6];                         // segment, its slice, first row of the room, rows in use, first row of the other room, max(C_h, w)
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   if (tid < kWave) {
-    const int i = find_segment_wave(tab.nseg, (int)blockIdx.x, [&](int s) { return tab.w[2][s]; });
-    if (tid == 0) {
-      sh_at[0] = tab.seg0 + i;
-      sh_at[1] = (int)blockIdx.x - tab.w[2][i];
-      sh_at[2] = tab.w[0][i];
-      sh_at[3] = rows_in_use(in.lengths, tab.seg0 + i, tab.w[0][i + 1] - tab.w[0][i]);
-      sh_at[4] = tab.w[1][i];
-      sh_at[5] = tab.w[3][i];
+    const int block = blockIdx.x;
+    if constexpr (std::is_same_v<TAB, EvictTabShort>) {
+      const int groups = (tab.nseg + TAB::kGroup - 1) / TAB::kGroup;
+      const int g = __popcll(__ballot(lane < groups && tab.w[2][min(lane, groups - 1)] <= block)) - 1, i = g * TAB::kGroup + lane;
+      const bool here = lane < TAB::kGroup && i < tab.nseg;
+      const int room = here ? tab.room[i] : 0, other = here ? tab.other[i] : 0, cap = here ? tab.cap[i] : 0;
+      const int blocks = here ? max(1, (min(room, cap) + slice - 1) / slice) : 0;
+      const int before = tab.w[2][g] + (int)row_incl_scan((uint32_t)blocks) - blocks;
+      const int start = tab.w[0][g] + (int)row_incl_scan((uint32_t)room) - room, to = tab.w[1][g] + (int)row_incl_scan((uint32_t)other) - other;
+      if (blocks && before <= block && block < before + blocks) {
+        sh_at[0] = tab.seg0 + i;
+        sh_at[1] = block - before;
+        sh_at[2] = start;
+        sh_at[3] = rows_in_use(in.lengths, tab.seg0 + i, room);
+        sh_at[4] = to;
+        sh_at[5] = cap;
+      }
+    } else {
+      const int i = find_segment_wave(tab.nseg, block, [&](int s) { return tab.w[2][s]; });
+      if (tid == 0) {
+        sh_at[0] = tab.seg0 + i;
+        sh_at[1] = block - tab.w[2][i];
+        sh_at[2] = tab.w[0][i];
+        sh_at[3] = rows_in_use(in.lengths, tab.seg0 + i, tab.w[0][i + 1] - tab.w[0][i]);
+        sh_at[4] = tab.w[1][i];
+        sh_at[5] = tab.w[3][i];
+      }
     }
   }
   __syncthreads();
@@ -707,23 +734,49 @@ extern "C" slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_
   // slices: two workgroups a CU, if the rows are enough for that; a segment's last one is half empty on average
   const int slice = (int)std::min<int64_t>(kEvictSlice, std::max<int64_t>(64, ceil_div(most, std::max<int64_t>(512 - S / 2, 256))));
   ScopedKernelTimer timer(SLKV_K_EVICT);
-  for_tables<EvictTab, kEvictSegs, 2>(
-      S, [&](int64_t s, int r) { return r == 0 ? (int32_t)desc->h_offsets[s] : r == 1 ? (int32_t)out_desc->h_offsets[s] : s < S ? cap_of(s) : 0; },
-      [&](int64_t s) { return std::max<int64_t>(1, ceil_div(most_of(s), slice)); },
-      [&](const auto& tab, int blocks) {
-        using TAB = std::decay_t<decltype(tab)>;
-        auto go = [&](auto units, auto scales) {
-          SLKV_LAUNCH((evict_kernel<decltype(units)::value, decltype(scales)::value, TAB>), dim3(blocks), dim3(kEvictThreads), 0, (hipStream_t)hip_stream,
-                      arrays_of(cache), arrays_of(out), d_kept_idx, w, slice, tab);
-        };
-        using std::integral_constant;
-        const integral_constant<int, 0> none{};
-        if (scale_bytes == 4) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-        else if (scale_bytes == 2) go(integral_constant<int, 2>{}, integral_constant<int, 2>{});
-        else if (row_bytes == 64) go(integral_constant<int, 4>{}, none);
-        else if (row_bytes == 128) go(integral_constant<int, 8>{}, none);
-        else if (row_bytes == 256) go(integral_constant<int, 16>{}, none);
-        else go(integral_constant<int, 32>{}, none);
-      });
+  auto blocks_of = [&](int64_t s) { return std::max<int64_t>(1, (most_of(s) + slice - 1) / slice); };
+  auto launch = [&](const auto& tab, int blocks) {
+    using TAB = std::decay_t<decltype(tab)>;
+    auto go = [&](auto units, auto scales) {
+      SLKV_LAUNCH((evict_kernel<decltype(units)::value, decltype(scales)::value, TAB>), dim3(blocks), dim3(kEvictThreads), 0, (hipStream_t)hip_stream,
+                  arrays_of(cache), arrays_of(out), d_kept_idx, w, slice, tab);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 0> none{};
+    if (scale_bytes == 4) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    else if (scale_bytes == 2) go(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+    else if (row_bytes == 64) go(integral_constant<int, 4>{}, none);
+    else if (row_bytes == 128) go(integral_constant<int, 8>{}, none);
+    else if (row_bytes == 256) go(integral_constant<int, 16>{}, none);
+    else go(integral_constant<int, 32>{}, none);
+  };
+  const int64_t* const from = desc->h_offsets;
+  const int64_t* const to = out_desc->h_offsets;
+  bool is_short = S > kEvictSegs;
+  for (int64_t s = 0; is_short && s < S; ++s) is_short = from[s + 1] - from[s] < 65536 && to[s + 1] - to[s] < 65536;
+  if (!is_short) {
+    for_tables<EvictTab, kEvictSegs, 2>(
+        S, [&](int64_t s, int r) { return r == 0 ? (int32_t)from[s] : r == 1 ? (int32_t)to[s] : s < S ? cap_of(s) : 0; }, blocks_of, launch);
+    return launch_status("evict");
+  }
+  for (int64_t s0 = 0; s0 < S; s0 += EvictTabShort::kSegs) {
+    EvictTabShort tab;
+    tab.nseg = (int32_t)std::min<int64_t>(EvictTabShort::kSegs, S - s0);
+    tab.seg0 = (int32_t)s0;
+    int64_t blocks = 0;
+    for (int i = 0; i < tab.nseg; ++i) {
+      const int64_t s = s0 + i;
+      if (i % EvictTabShort::kGroup == 0) {
+        tab.w[0][i / EvictTabShort::kGroup] = (int32_t)from[s];
+        tab.w[1][i / EvictTabShort::kGroup] = (int32_t)to[s];
+        tab.w[2][i / EvictTabShort::kGroup] = (int32_t)blocks;
+      }
+      tab.room[i] = (uint16_t)(from[s + 1] - from[s]);
+      tab.other[i] = (uint16_t)(to[s + 1] - to[s]);
+      tab.cap[i] = (uint16_t)std::min(cap_of(s), 65535);        // (above every room)
+      blocks += blocks_of(s);
+    }
+    launch(tab, (int)blocks);
+  }
   return launch_status("evict");
 }

@@ -131,6 +131,19 @@ def test_segment_tables(S):
     check(cache, [25], 3, slack=1)
 
 
+@pytest.mark.parametrize("S", [241, 560, 561, 1121])
+@pytest.mark.parametrize("longest", [1200, 65535, 65536])
+def test_many_segments_around_a_long_one(S, longest):
+    rng = np.random.default_rng(S + longest)
+    lens = rng.integers(0, 40, S)
+    lens[[3, 300 % S, S - 1]] = 700, 1100, 90
+    rooms = lens + rng.integers(0, 9, S)
+    lens[S // 2], rooms[S // 2] = min(longest, 1300), longest
+    cache = random_cache(rng, "bf16_kv4", S, 1, 1, 64, lens.tolist(), rooms=rooms.tolist(), before=11)
+    check(cache, [1100], 4, before=7)
+    check(cache, [20], 0, slack=2)
+
+
 def test_without_positions_or_weights():
     rng = np.random.default_rng(3)
     cache = random_cache(rng, "f32", 1, 2, 1, 128, [90, 40])
