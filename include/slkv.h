@@ -68,7 +68,8 @@ const char* slkv_status_str(slkv_status s);
 /* Detail of the last error on the calling thread; valid until its next slkv call. */
 const char* slkv_last_error(void);
 /* ABI version: major * 1000 + minor.  slkv_score_heads_first and slkv_score_heads_qk_first joined 1.5 without a
- * number of their own: a program that loads the library at run time looks these two symbols up. */
+ * number of their own, and so did the calls on a cache (slkv_fill_cache to slkv_evict_cache): a program that loads the library at run time looks
+ * these symbols up. */
 int32_t slkv_version(void);
 /* One-time set-up on the CURRENT device (host pointer arguments: none): raises the LDS limit of
  * the selection kernels and looks up the scratch of slkv_compress_layer_static.  Optional: a
@@ -326,7 +327,8 @@ slkv_status slkv_recompress_layer(const slkv_ragged_desc* desc, const void* d_qw
  * d_lengths[s] are in use, oldest first.  The lengths live on the device, so that a recorded HIP graph that appends,
  * attends and evicts replays on a cache that has grown since; what a call reads of them is bounded by the room whatever they hold
  * (below 0 counts as 0, above the room as the room).  Rows that are not in use are neither read as keys or values nor changed.
- * The rooms may total 2^31 - 1 rows, one of them 2^25; addresses are 64-bit.
+ * The rooms may total 2^31 - 1 rows, one of them 2^25; addresses are 64-bit.  What a call writes may not overlap what it reads or
+ * writes elsewhere, but for what is said to be allowed below.
  */
 typedef struct {
   uint32_t struct_size;        /* sizeof(slkv_cache_desc) */
@@ -416,6 +418,7 @@ slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cach
  * (two passes, long histories: 1 + 1 + 6 + 1; one pass: 1 + 4 + 3 + 1; histories up to 32768: 1 + 1 + 1 + 1, both passes in
  * one launch 0 + 1 + 1 + 1, one pass 1 + 4 + 1 + 1, in each of these without the last one where the selection copies all rows; ragged
  * caches and batches of many short histories: one SLKV_K_SCORE_ACCUM record in all, where the scoring launch selects and copies too).
+ * Fill, append, rows and evict make one each; attend one or two for every 600 segments.
  * Process-wide; not meant for production.
  */
 typedef enum {

@@ -213,6 +213,8 @@ class Cache:
     def _on(self, stream):
         """The call's stream as the current one, so that what it allocates belongs to it; without one, the cache's device, where it is not current."""
         if stream is not None:
+            if stream.device != self.device:
+                raise ValueError("stream is of %s, the cache on %s" % (stream.device, self.device))
             return torch.cuda.stream(stream)
         return self._here if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
 

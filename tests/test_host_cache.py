@@ -1,10 +1,13 @@
 """CPU-only tests of the calls on a cache: descriptors, refusals before any GPU call, workspace sizes."""
 
 import ctypes as C
+import types
 
 import numpy as np
 import pytest
+import torch
 
+from paper_2508_15806_amd import api
 from paper_2508_15806_amd import binding as B
 
 FAKE, ODD, NULL = 4096, 4100, None
@@ -163,3 +166,10 @@ def test_evict_refuses_before_touching_the_gpu():
     assert evict(out=arrays(**dict(one, d_lengths=FAKE))) == 2                         # lengths are read by many workgroups
     assert evict(idx=FAKE) == 2
     assert evict(out=arrays(**dict(one, d_lengths=NULL))) == 1
+
+
+def test_a_stream_of_another_device_is_refused():
+    cache = api.Cache.__new__(api.Cache)
+    cache.device = torch.device("cuda", 0)
+    with pytest.raises(ValueError, match="stream"):
+        cache._on(types.SimpleNamespace(device=torch.device("cuda", 1)))
