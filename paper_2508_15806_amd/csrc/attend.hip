@@ -244,43 +244,75 @@ __device__ __forceinline__ f32x4 output_of(f32x4 o, float total, bool none) {
   return o;
 }
 
-// Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread; lse: of its R queries, in LDS.  The first rows' numbers can
-// be asked for before the log-sum-exp is known.
+// Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread, and, where rows are few and queries many, 1 << bits threads
+// that share the R queries (36 segments, 15 queries: the join 6.7 us -> 6.4; 8 segments, 64 queries: 14.2 -> 11.9); lse: of these, in LDS.  The first numbers can be asked for before the log-sum-exp is known.
 constexpr int kAheadQueries = 4;
 struct WeightsAhead { f32x4 x[kAheadQueries], w; };
-__device__ __forceinline__ const float* logits_of(const AttendArgs& a, int tile, int j) {
-  return a.logits + (int64_t)(tile + j / kTileRows) * a.R * kTileRows + j % kTileRows;
-}
-__device__ __forceinline__ void load_weights(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j, int j1) {
-  if (j >= j1) return;
-  const float* l = logits_of(a, tile, j);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) h.w[e] = a.w_in && j + e < j1 ? a.w_in[start + j + e] : 0.f;
-#pragma unroll
-  for (int r = 0; r < kAheadQueries; ++r)
-    if (r < a.R) h.x[r] = *(const f32x4*)(l + r * kTileRows);
-}
 template <int NT>
-__device__ __forceinline__ void add_weights(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j0, int j1, const float* lse) {
-  for (int j = j0 + 4 * (int)threadIdx.x; j < j1; j += 4 * NT) {
-    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto add = [&](f32x4 x, float l) __attribute__((always_inline)) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += exp2_fast(fmaf(x[e], a.c_log2, -l));
-    };
-#pragma unroll
-    for (int r = 0; r < kAheadQueries; ++r)
-      if (r < a.R) add(h.x[r], lse[r]);
+struct Weights {
+  int bits, sp, j;                                     // the thread's queries sp, sp + (1 << bits), .., its first row
+  __device__ __forceinline__ Weights(const AttendArgs& a, int j0, int j1) {
+    bits = 0;
+    while (bits < 4 && 4 * (NT >> (bits + 1)) >= j1 - j0 && (kAheadQueries << bits) < a.R) ++bits;
+    sp = (int)threadIdx.x / (NT >> bits);
+    j = j0 + 4 * ((int)threadIdx.x & ((NT >> bits) - 1));
+  }
+  static __device__ __forceinline__ const float* logits_of(const AttendArgs& a, int tile, int j) {
+    return a.logits + (int64_t)(tile + j / kTileRows) * a.R * kTileRows + j % kTileRows;
+  }
+  __device__ __forceinline__ void load(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j1) const {
+    if (j >= j1) return;
     const float* l = logits_of(a, tile, j);
-#pragma unroll 8
-    for (int r = kAheadQueries; r < a.R; ++r) add(*(const f32x4*)(l + r * kTileRows), lse[r]);
-    s += h.w;
-    load_weights(h, a, start, tile, j + 4 * NT, j1);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h.w[e] = sp == 0 && a.w_in && j + e < j1 ? a.w_in[start + j + e] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kAheadQueries; ++i) {
+      const int r = sp + (i << bits);
+      if (r < a.R) h.x[i] = *(const f32x4*)(l + r * kTileRows);
+    }
+  }
+  // shared: NT places
+  __device__ __forceinline__ void add(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j1, const float* lse, f32x4* shared) {
+    auto sum = [&]() __attribute__((always_inline)) {
+      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+      auto one = [&](f32x4 x, float l) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += exp2_fast(fmaf(x[e], a.c_log2, -l));
+      };
+#pragma unroll
+      for (int i = 0; i < kAheadQueries; ++i) {
+        const int r = sp + (i << bits);
+        if (r < a.R) one(h.x[i], lse[r]);
+      }
+      const float* l = logits_of(a, tile, j);
+#pragma unroll 4
+      for (int r = sp + (kAheadQueries << bits); r < a.R; r += 1 << bits) one(*(const f32x4*)(l + r * kTileRows), lse[r]);
+      return s + h.w;
+    };
+    if (bits == 0) {
+      while (j < j1) {
+        const f32x4 s = sum();
+        const Weights at = *this;
+        j += 4 * NT;
+        load(h, a, start, tile, j1);
+        at.put(a, start, j1, s);
+      }
+      return;
+    }
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (j < j1) shared[threadIdx.x] = s = sum();
+    __syncthreads();
+    if (sp == 0 && j < j1) {
+      for (int v = 1; v < 1 << bits; ++v) s += shared[v * (NT >> bits) + (int)threadIdx.x];
+      put(a, start, j1, s);
+    }
+  }
+  __device__ __forceinline__ void put(const AttendArgs& a, int64_t start, int j1, f32x4 s) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (j + e < j1) a.w_out[start + j + e] = s[e];
   }
-}
+};
 
 // The segment of a workgroup, which is a part of one: segments have max(1, ceil(room / rows_each)) parts.  One wave looks it up and reads the length for all: the
 // table is read from the kernel's arguments, where a workgroup that goes through 3 KB of it with every wave waits up to 20 us behind the others (768 workgroups; this way 1 to 2).
@@ -646,9 +678,10 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
   if (!whole || !a.w_out) return;
   __threadfence_block();
   __syncthreads();
+  Weights<W * kWave> weights(a, 0, n);
   WeightsAhead h;
-  load_weights(h, a, base, at.tile, 4 * (int)threadIdx.x, n);
-  add_weights<W * kWave>(h, a, base, at.tile, 0, n, sh_lse);
+  weights.load(h, a, base, at.tile, n);
+  weights.add(h, a, base, at.tile, n, sh_lse, (f32x4*)&sh_o[0][0][0]);
 }
 
 // Over `share` neighbouring lanes, 4 to 64, in every lane.
@@ -670,11 +703,11 @@ __device__ __forceinline__ float reduce_lanes(float v, int share, OP op) {
 // the table and the length there is one round trip.  Bound by latency, of the instructions too.  (Two other ways were measured.  The workgroups of a segment waiting for
 // each other in the launch above: 40 us instead of 34 for one long history, whose memory traffic their meeting competes with, nothing gained elsewhere; the last one to
 // arrive joining the segment alone: 25 to 40 % slower.)
-template <int KIND, int D, class TAB>
+template <int KIND, int D, int UNITS, class TAB>
 __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const AttendArgs a, const TAB tab) {
   __shared__ Where sh_at;
-  __shared__ float sh_lse[64], sh_total[64], sh_factor[kJoinPairs];   // [part][query]
-  __shared__ f32x4 sh_o[kAttendThreads / kWave][16];
+  __shared__ float sh_lse[64], sh_total[64], sh_factor[kJoinPairs], sh_sum[kJoinPairs];   // [part][query] (sh_factor: references at first)
+  __shared__ f32x4 sh_o[UNITS][kAttendThreads / kWave][16], sh_w[kAttendThreads];
   const Where w = find_part(a, tab, sh_at);
   const int n = w.n, part = w.part, active = w.active;
   if (active <= 1 || part >= active) return;
@@ -684,26 +717,51 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
   // the queries: 1 << bits lanes each, a lane per part
   const int bits = R <= 4 ? 6 : R <= 8 ? 5 : R <= 16 ? 4 : R <= 32 ? 3 : 2, share = 1 << bits;
   const int r = tid >> bits, lane = tid & (share - 1);
+  // (more parts than lanes: through LDS, so that all are asked for at once; the same case 15.5 us -> 14.7)
+  const bool staged = active > share;
   f32x2 pair = f32x2{-INFINITY, 0.f};
-  if (r < R && lane < active) pair = *(const f32x2*)(ml + 2 * (lane * R + r));
-  // the outputs, in units of 64: 16 threads take four each, `groups` of these the parts, 2 to 16, and what is left other units
+  if (staged) {
+    for (int i0 = tid; i0 < active * R; i0 += 8 * kAttendThreads) {
+      f32x2 t[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i0 + i * kAttendThreads < active * R) t[i] = *(const f32x2*)(ml + 2 * (i0 + i * kAttendThreads));
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i0 + i * kAttendThreads < active * R) sh_factor[i0 + i * kAttendThreads] = t[i][0], sh_sum[i0 + i * kAttendThreads] = t[i][1];
+    }
+  } else if (r < R && lane < active) {
+    pair = *(const f32x2*)(ml + 2 * (lane * R + r));
+  }
+  // the outputs, in units of 64: 16 threads take four each, `groups` of these the parts, 2 to 16, and what is left other units, UNITS of them at a time
+  // (64 queries, 32 segments of 4000 rows on average, 128 units a segment: 12.4 us with four; 16.5 with one; 14.7 with 16, whose code has to be fetched too)
   const int groups = active <= 2 ? 2 : active <= 4 ? 4 : active <= 8 ? 8 : 16, grp_bits = active <= 2 ? 1 : active <= 4 ? 2 : active <= 8 ? 3 : 4;
   const int units = R * (D / 64), f = tid & 15, grp = (tid >> 4) & (groups - 1), at_once = 16 >> grp_bits, sub = tid >> (4 + grp_bits);
-  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (part * at_once + sub < units && grp < active) x = *(const f32x4*)(po + (int64_t)grp * R * D + (part * at_once + sub) * 64 + f * 4);
-  WeightsAhead h;
+  f32x4 x[UNITS];
+  int first = part * at_once;
+  auto unit_of = [&](int i) __attribute__((always_inline)) { return first + i * active * at_once + sub; };
+  auto load_units = [&](int p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+      if (unit_of(i) < units && p < active) x[i] = *(const f32x4*)(po + (int64_t)p * R * D + unit_of(i) * 64 + f * 4);
+  };
+  load_units(grp);
   const int end = min(n, (part + 1) * w.each);
-  if (a.w_out) load_weights(h, a, w.start, w.tile, part * w.each + 4 * tid, end);
+  Weights<kAttendThreads> weights(a, part * w.each, end);
+  WeightsAhead h;
+  if (a.w_out) weights.load(h, a, w.start, w.tile, end);
 
   auto factor_of = [](float m, float top) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : exp2_fast(m - top); };
-  float top = pair[0];
-  if (r < R)
-    for (int p = lane + share; p < active; p += share) top = fmaxf(top, ml[2 * (p * R + r)]);
+  float top = pair[0], total = 0.f;
+  if (staged) {
+    __syncthreads();
+    if (r < R)
+      for (int p = lane; p < active; p += share) top = fmaxf(top, sh_factor[p * R + r]);
+  }
   top = reduce_lanes(top, share, [](float u, float v) { return fmaxf(u, v); });
-  float total = 0.f;
   if (r < R)
     for (int p = lane; p < active; p += share) {
-      if (p != lane) pair = *(const f32x2*)(ml + 2 * (p * R + r));
+      if (staged) pair = f32x2{sh_factor[p * R + r], sh_sum[p * R + r]};
       const float s = factor_of(pair[0], top);
       sh_factor[p * R + r] = s;
       total += pair[1] * s;
@@ -717,30 +775,41 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     if (part == 0 && a.lse) a.lse[(int64_t)w.seg * R + r] = lse_out(lse2, none);
   }
   __syncthreads();
-  for (int first = part * at_once; first < units; first += active * at_once) {
-    const int unit = min(first + sub, units - 1), row = unit / (D / 64), at = unit * 64 + f * 4;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
+  while (true) {
+    f32x4 o[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int p = grp; p < active; p += groups) {
-      if (first != part * at_once || p != grp || first + sub >= units) x = *(const f32x4*)(po + (int64_t)p * R * D + at);
-      o += x * sh_factor[p * R + row];
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i)
+        if (unit_of(i) < units) o[i] += x[i] * sh_factor[p * R + unit_of(i) / (D / 64)];
+      load_units(p + groups);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[e] += __shfl_xor(o[e], 16);
-      if (groups > 2) o[e] += __shfl_xor(o[e], 32);
+    for (int i = 0; i < UNITS; ++i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[i][e] += __shfl_xor(o[i][e], 16);
+        if (groups > 2) o[i][e] += __shfl_xor(o[i][e], 32);
+      }
+      if (groups > 4 && (tid & (kWave - 1)) < 16) sh_o[i][tid / kWave][f] = o[i];
     }
-    if (groups > 4) {
-      if ((tid & (kWave - 1)) < 16) sh_o[tid / kWave][f] = o;
-      __syncthreads();
-      if (grp == 0)
-        for (int v = 1; v < groups / 4; ++v) o += sh_o[tid / kWave + v][f];
-      __syncthreads();
+    if (groups > 4) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      if (grp != 0 || unit_of(i) >= units) continue;
+      if (groups > 4)
+        for (int v = 1; v < groups / 4; ++v) o[i] += sh_o[i][tid / kWave + v][f];
+      const int row = unit_of(i) / (D / 64);
+      store_out<KIND>(a.out + ((int64_t)w.seg * R * D + unit_of(i) * 64 + f * 4) * (int)sizeof(typename Kind<KIND>::wide),
+                      output_of(o[i], sh_total[row], n - T + 1 + row % T <= 0));
     }
-    if (grp == 0 && first + sub < units)
-      store_out<KIND>(a.out + ((int64_t)w.seg * R * D + at) * (int)sizeof(typename Kind<KIND>::wide), output_of(o, sh_total[row], n - T + 1 + row % T <= 0));
+    first += UNITS * active * at_once;
+    if (first >= units) break;
+    __syncthreads();
+    load_units(grp);
   }
-  if (a.w_out) add_weights<kAttendThreads>(h, a, w.start, w.tile, part * w.each, end, sh_lse);
+  if (a.w_out) weights.add(h, a, w.start, w.tile, end, sh_lse, sh_w);
 }
 
 // ------------------------------------------------------------------ host
@@ -909,7 +978,9 @@ extern "C" slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv
         }
         if (p.split) {
           ScopedKernelTimer timer(SLKV_K_ATTEND_JOIN);
-          SLKV_LAUNCH((attend_join_kernel<kKind, kDim, TAB>), grid, dim3(kAttendThreads), 0, stream, a, tab);
+          // a workgroup has R d / 64 units of outputs, divided by 9 to 17 (or the parts, if they are more)
+          if (a.R * (kDim / 64) <= 9) SLKV_LAUNCH((attend_join_kernel<kKind, kDim, 1, TAB>), grid, dim3(kAttendThreads), 0, stream, a, tab);
+          else SLKV_LAUNCH((attend_join_kernel<kKind, kDim, 4, TAB>), grid, dim3(kAttendThreads), 0, stream, a, tab);
         }
       };
       if (desc->d == 64) with_dim(std::integral_constant<int, 64>{});
