@@ -220,8 +220,15 @@ def prepare(case, seed):
             s["cache"] = api.Cache(*shape, s["offsets"], k=s["k"], v=s["v"], k_scale=s["k_scale"], v_scale=s["v_scale"],
                                    lengths=s["lengths"].clone(), pos=s["pos"], weight=s["weight"])
         if c["op"] == "evict":
-            s["kept"] = api.Cache(*shape, s["out_offsets"])
-            s["kept_idx"] = torch.empty(int(s["out_offsets"][-1]), dtype=torch.int32, device=s["lengths"].device)
+            # rooms for as many rows as may stay, whatever the lengths on the device
+            most = [min(int(n), max(int(s["caps"][i % c["Hkv"]]), c["keep"])) for i, n in enumerate(np.diff(s["offsets"]))]
+            rooms, out = _offsets(most), s["out_offsets"]
+            s["kept"] = api.Cache(*shape, rooms)
+            s["kept_idx"] = torch.empty(int(rooms[-1]), dtype=torch.int32, device=s["lengths"].device)
+            s["kept_at"] = None
+            if rooms[-1] != out[-1]:
+                at = np.concatenate([np.arange(out[i + 1] - out[i]) + rooms[i] for i in range(len(most))])
+                s["kept_at"] = torch.from_numpy(at).to(s["lengths"].device)
         if c["op"] == "attend":
             s["sums"] = s["weight"].clone()
     return s
@@ -263,8 +270,11 @@ def _own_append(s):
 def _own_evict(s):
     kept = s["kept"]
     s["cache"].evict(s["caps"], s["case"]["keep"], kept, s["kept_idx"])
-    k, v, pos = kept.rows(s["out_offsets"]) if s["case"]["dtype"] in ("bf16_kv8", "bf16_kv4") else (kept.k, kept.v, kept.pos)
-    return {"k": k, "v": v, "pos": pos, "weight": kept.weight, "idx": s["kept_idx"], "lengths": kept.lengths}
+    at = s["kept_at"]
+    whole = at is None and s["case"]["dtype"] not in ("bf16_kv8", "bf16_kv4")
+    k, v, pos = (kept.k, kept.v, kept.pos) if whole else kept.rows(s["out_offsets"])
+    weight, idx = (kept.weight, s["kept_idx"]) if at is None else (kept.weight[at], s["kept_idx"][at])
+    return {"k": k, "v": v, "pos": pos, "weight": weight, "idx": idx, "lengths": kept.lengths}
 
 
 # ---------------------------------------------------------------- the plain forms
