@@ -244,73 +244,70 @@ __device__ __forceinline__ f32x4 output_of(f32x4 o, float total, bool none) {
   return o;
 }
 
-// Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread, and, where rows are few and queries many, 1 << bits threads
-// that share the R queries (36 segments, 15 queries: the join 6.7 us -> 6.4; 8 segments, 64 queries: 14.2 -> 11.9); lse: of these, in LDS.  The first numbers can be asked for before the log-sum-exp is known.
+// Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread; SHARED: where rows are few and queries many, 1 << bits threads
+// share the R queries (36 segments, 15 queries: the join 6.7 us -> 6.4; 8 segments, 64 queries: 14.2 -> 11.9).  lse: of the queries, in LDS.  The first numbers can
+// be asked for before the log-sum-exp is known.
 constexpr int kAheadQueries = 4;
 struct WeightsAhead { f32x4 x[kAheadQueries], w; };
-template <int NT>
+template <int NT, bool SHARED>
 struct Weights {
-  int bits, sp, j;                                     // the thread's queries sp, sp + (1 << bits), .., its first row
-  __device__ __forceinline__ Weights(const AttendArgs& a, int j0, int j1) {
-    bits = 0;
-    while (bits < 4 && 4 * (NT >> (bits + 1)) >= j1 - j0 && (kAheadQueries << bits) < a.R) ++bits;
-    sp = (int)threadIdx.x / (NT >> bits);
-    j = j0 + 4 * ((int)threadIdx.x & ((NT >> bits) - 1));
+  const AttendArgs& a;
+  const int64_t start;
+  const int tile, j1;
+  int bits = 0, sp = 0, first;                         // the thread's queries sp, sp + (1 << bits), .., its first row
+  __device__ __forceinline__ Weights(const AttendArgs& args, int64_t start_row, int first_tile, int j0, int end) : a(args), start(start_row), tile(first_tile), j1(end) {
+    if constexpr (SHARED) {
+      while (bits < 4 && 4 * (NT >> (bits + 1)) >= j1 - j0 && (kAheadQueries << bits) < a.R) ++bits;
+      sp = (int)threadIdx.x / (NT >> bits);
+    }
+    first = j0 + 4 * ((int)threadIdx.x & ((NT >> bits) - 1));
   }
-  static __device__ __forceinline__ const float* logits_of(const AttendArgs& a, int tile, int j) {
-    return a.logits + (int64_t)(tile + j / kTileRows) * a.R * kTileRows + j % kTileRows;
-  }
-  __device__ __forceinline__ void load(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j1) const {
+  __device__ __forceinline__ const float* logits_of(int j) const { return a.logits + (int64_t)(tile + j / kTileRows) * a.R * kTileRows + j % kTileRows; }
+  __device__ __forceinline__ void load(WeightsAhead& h, int j) const {
     if (j >= j1) return;
-    const float* l = logits_of(a, tile, j);
+    const float* l = logits_of(j);
 #pragma unroll
     for (int e = 0; e < 4; ++e) h.w[e] = sp == 0 && a.w_in && j + e < j1 ? a.w_in[start + j + e] : 0.f;
 #pragma unroll
-    for (int i = 0; i < kAheadQueries; ++i) {
-      const int r = sp + (i << bits);
-      if (r < a.R) h.x[i] = *(const f32x4*)(l + r * kTileRows);
-    }
+    for (int i = 0; i < kAheadQueries; ++i)
+      if (sp + (i << bits) < a.R) h.x[i] = *(const f32x4*)(l + (sp + (i << bits)) * kTileRows);
   }
-  // shared: NT places
-  __device__ __forceinline__ void add(WeightsAhead& h, const AttendArgs& a, int64_t start, int tile, int j1, const float* lse, f32x4* shared) {
-    auto sum = [&]() __attribute__((always_inline)) {
-      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-      auto one = [&](f32x4 x, float l) __attribute__((always_inline)) {
+  __device__ __forceinline__ f32x4 sum(const WeightsAhead& h, int j, const float* lse) const {
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto one = [&](f32x4 x, float l) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += exp2_fast(fmaf(x[e], a.c_log2, -l));
-      };
-#pragma unroll
-      for (int i = 0; i < kAheadQueries; ++i) {
-        const int r = sp + (i << bits);
-        if (r < a.R) one(h.x[i], lse[r]);
-      }
-      const float* l = logits_of(a, tile, j);
-#pragma unroll 4
-      for (int r = sp + (kAheadQueries << bits); r < a.R; r += 1 << bits) one(*(const f32x4*)(l + r * kTileRows), lse[r]);
-      return s + h.w;
+      for (int e = 0; e < 4; ++e) s[e] += exp2_fast(fmaf(x[e], a.c_log2, -l));
     };
-    if (bits == 0) {
-      while (j < j1) {
-        const f32x4 s = sum();
-        const Weights at = *this;
-        j += 4 * NT;
-        load(h, a, start, tile, j1);
-        at.put(a, start, j1, s);
+#pragma unroll
+    for (int i = 0; i < kAheadQueries; ++i)
+      if (sp + (i << bits) < a.R) one(h.x[i], lse[sp + (i << bits)]);
+    const float* l = logits_of(j);
+#pragma unroll 8
+    for (int r = sp + (kAheadQueries << bits); r < a.R; r += 1 << bits) one(*(const f32x4*)(l + r * kTileRows), lse[r]);
+    return s + h.w;
+  }
+  __device__ __forceinline__ void store(f32x4 s, int j) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < j1) a.w_out[start + j + e] = s[e];
+  }
+  // h: loaded at `first`; shared: NT places
+  __device__ __forceinline__ void add(WeightsAhead& h, const float* lse, f32x4* shared) const {
+    if (!SHARED || bits == 0) {
+      for (int j = first; j < j1; j += 4 * NT) {
+        const f32x4 s = sum(h, j, lse);
+        load(h, j + 4 * NT);
+        store(s, j);
       }
       return;
     }
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (j < j1) shared[threadIdx.x] = s = sum();
+    if (first < j1) shared[threadIdx.x] = s = sum(h, first, lse);
     __syncthreads();
-    if (sp == 0 && j < j1) {
+    if (sp == 0 && first < j1) {
       for (int v = 1; v < 1 << bits; ++v) s += shared[v * (NT >> bits) + (int)threadIdx.x];
-      put(a, start, j1, s);
+      store(s, first);
     }
-  }
-  __device__ __forceinline__ void put(const AttendArgs& a, int64_t start, int j1, f32x4 s) const {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j + e < j1) a.w_out[start + j + e] = s[e];
   }
 };
 
@@ -678,10 +675,10 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
   if (!whole || !a.w_out) return;
   __threadfence_block();
   __syncthreads();
-  Weights<W * kWave> weights(a, 0, n);
+  const Weights<W * kWave, false> weights(a, base, at.tile, 0, n);
   WeightsAhead h;
-  weights.load(h, a, base, at.tile, n);
-  weights.add(h, a, base, at.tile, n, sh_lse, (f32x4*)&sh_o[0][0][0]);
+  weights.load(h, weights.first);
+  weights.add(h, sh_lse, nullptr);
 }
 
 // Over `share` neighbouring lanes, 4 to 64, in every lane.
@@ -747,9 +744,9 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
   };
   load_units(grp);
   const int end = min(n, (part + 1) * w.each);
-  Weights<kAttendThreads> weights(a, part * w.each, end);
+  const Weights<kAttendThreads, true> weights(a, w.start, w.tile, part * w.each, end);
   WeightsAhead h;
-  if (a.w_out) weights.load(h, a, w.start, w.tile, end);
+  if (a.w_out) weights.load(h, weights.first);
 
   auto factor_of = [](float m, float top) __attribute__((always_inline)) { return m == -INFINITY ? 1.f : exp2_fast(m - top); };
   float top = pair[0], total = 0.f;
@@ -809,7 +806,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
     __syncthreads();
     load_units(grp);
   }
-  if (a.w_out) weights.add(h, a, w.start, w.tile, end, sh_lse, sh_w);
+  if (a.w_out) weights.add(h, sh_lse, sh_w);
 }
 
 // ------------------------------------------------------------------ host
