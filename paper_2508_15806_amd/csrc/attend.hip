@@ -838,10 +838,11 @@ static AttendPlan plan_attend(const slkv_cache_desc* d, int T, bool weights) {
   // otherwise: two workgroups on a CU fill each other's beginnings and ends (128 segments of 270 to 3012 rows 22.9 us, 256 of E4M3 43.8; eight waves 23.5, 50.6).
   p.waves = rt == 1 && S <= 64 && rows >= 32768 ? 8 : 4;
   const int64_t places = 256 * attend_waves_per_cu(rt) / p.waves;
-  // Whole segments while the longest takes one workgroup no longer than all rows take the chip and a second launch that joins parts.  One workgroup: 10.2 ns a row of 512
-  // bytes, 4.9 of 136; the chip: 5 TB/s; the launch: 5 to 8 us.  (8 segments of 96 to 440 rows: whole 10.2 us, in parts 12.8; 8 of 1016 rows of 512 bytes: 15.3 and 12.5;
-  // 512 of 280 to 2189 rows of 136 bytes: 24.2 and 33.2.)
-  const double whole_us = most * (0.0035 * rt + row_bytes / 75e3), split_us = rows * row_bytes / 5e6 + 5;
+  // Whole segments while the longest is done, beside the others, before parts and the second launch that joins them would be.  One workgroup: 10.2 ns a row of 512
+  // bytes, 4.9 of 136, and 0.4 of the time that the chip takes for all rows at 5 TB/s, which it shares with the others; the second launch: 5 us.  (Whole and in parts, us: 8 segments of 96 to
+  // 440 rows 10.2, 12.8; 8 of 1016 rows of 512 bytes 15.3, 12.5; 512 of 280 to 2189 rows of 136 bytes 23.5, 32.7; 256 of up to 3140 rows of 512 bytes 54.0, 40.4; 512 of up to 3140 of
+  // 256 bytes 45.0, 46.6; 256 of up to 3140 of 136 bytes 25.6, 20.9.)
+  const double whole_us = most * (0.0035 * rt + row_bytes / 75e3), split_us = rows * row_bytes / 5e6 * 0.6 + 5;
   if (most <= kMost && whole_us <= split_us) {
     p.rows_each = std::max<int64_t>(kTileRows, round(most));
   } else {
