@@ -245,7 +245,7 @@ __device__ __forceinline__ f32x4 output_of(f32x4 o, float total, bool none) {
 }
 
 // Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread; SHARED: where rows are few and queries many, 1 << bits threads
-// share the R queries (36 segments, 15 queries: the join 6.7 us -> 6.4; 8 segments, 64 queries: 14.2 -> 11.9).  lse: of the queries, in LDS.  The first numbers can
+// share the R queries (48 segments, 15 queries: the join 6.7 us -> 6.4; 8 segments, 64 queries: 14.2 -> 11.9).  lse: of the queries, in LDS.  The first numbers can
 // be asked for before the log-sum-exp is known.
 constexpr int kAheadQueries = 4;
 struct WeightsAhead { f32x4 x[kAheadQueries], w; };
