@@ -58,6 +58,16 @@ def test_one_segment_over_the_whole_chip(dtype, d, G, T, n):
     check(cache, normal(rng, (1, G, T, d), dtype), T)
 
 
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("bf16", 128), ("bf16_kv4", 64)])
+@pytest.mark.parametrize("G,T", [(5, 1), (3, 3), (1, 17), (11, 3), (8, 8)])
+@pytest.mark.parametrize("n", [130, 700, 2500])
+def test_many_queries_on_parts_of_few_rows(dtype, d, G, T, n):
+    # threads of the joining launch share the queries; outputs take it several turns
+    rng = np.random.default_rng([d, G, T, n])
+    cache = random_cache(rng, dtype, 1, 2, G, d, [n, n - 60], rooms=[n + 9, n + 300], before=1)
+    check(cache, normal(rng, (1, 2 * G, T, d), dtype), T)
+
+
 @pytest.mark.parametrize("S", [90, 700])
 def test_many_segments_with_long_ones_among_them(S):
     rng = np.random.default_rng(S)
