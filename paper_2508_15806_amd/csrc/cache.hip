@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const CacheArrays c, uns
 // ------------------------------------------------------------------ eviction
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
-constexpr int kEvictHeld = 12288;     // keys that stay in LDS
+constexpr int kEvictHeld = 12288, kEvictHeldLong = 36864;   // keys that stay in LDS: with two workgroups on a CU, with one
 constexpr int kEvictRank = 256;       // keys that are ranked against each other
 constexpr int kEvictSlice = 512;      // rows that a workgroup copies, at most (512 segments of 512 rows: 69 us; 79 with 1024)
 constexpr int kEvictSegs = 240;
@@ -305,24 +305,30 @@ struct EvictTabShort {
 
 __device__ __forceinline__ uint32_t weight_key(float v) { return v != v ? 0xffffffffu : float_key(v); }
 
+template <int HELD>
 struct EvictLds {
-  uint32_t held[kEvictHeld], hist[kHistBins], scan[16], res[2], near_key[kEvictRank], ends[2][kEvictWaves];
-  int32_t near_row[kEvictRank], near_count, from[kEvictSlice];
+  uint32_t held[HELD], hist[kHistBins], scan[16], res[2], near_key[kEvictRank], ends[2][kEvictWaves];
+  int32_t near_row[kEvictRank], near_count, from[kEvictSlice * (HELD == kEvictHeld ? 1 : 2)];
 };
 
 // The `want` largest of m keys, 0 < want < m: the smallest kept key and how many of the rows that have it stay, the lower ones.  A wave looks after neighbouring rows i0 ..
 // i1 - 1, lane by lane.  The key is found by digits of 11 bits of the keys' distance from the smallest, the first one as fine as their range allows (weights lie within some
-// octaves, so fixed digits would pile up in a few counters); when no more than kEvictRank keys share the digit of the last one, these are ranked against each other.  Keys
-// stay in LDS up to kEvictHeld rows, and are read again from memory beyond.  Bound by latency, of the instructions too: loops are not unrolled far.
-__device__ __forceinline__ void evict_threshold(EvictLds& l, const float* __restrict__ keys, int m, uint32_t want, int i0, int i1, uint32_t& least, uint32_t& count) {
+// octaves, so fixed digits would pile up in a few counters); when no more than kEvictRank keys share the digit of the last one, these are ranked against each other.  The first
+// HELD keys stay in LDS, others are read again from memory.  Bound by latency, of the instructions too: loops are not unrolled far.
+template <int HELD>
+__device__ __forceinline__ uint32_t evict_key(const EvictLds<HELD>& l, const float* __restrict__ keys, int i) {
+  if constexpr (HELD == kEvictHeld) return l.held[i];
+  else return i < HELD ? l.held[i] : weight_key(keys[i]);
+}
+template <int HELD>
+__device__ __forceinline__ void evict_threshold(EvictLds<HELD>& l, const float* __restrict__ keys, int m, uint32_t want, int i0, int i1, uint32_t& least, uint32_t& count) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const bool in_lds = m <= kEvictHeld;
-  auto key_of = [&](int i) __attribute__((always_inline)) { return in_lds ? l.held[i] : weight_key(keys[i]); };
+  auto key_of = [&](int i) __attribute__((always_inline)) { return evict_key<HELD>(l, keys, i); };
   uint32_t lo = ~0u, hi = 0u;
 #pragma unroll 8
   for (int i = i0; i < i1; i += kWave) {
     const uint32_t x = weight_key(keys[i]);
-    if (in_lds) l.held[i] = x;
+    if (HELD == kEvictHeld || i < HELD) l.held[i] = x;
     lo = min(lo, x);
     hi = max(hi, x);
   }
@@ -396,9 +402,9 @@ __device__ __forceinline__ void evict_threshold(EvictLds& l, const float* __rest
 // A workgroup copies a slice of a segment's kept rows, `slice` of them, UNITS of 16 bytes a row of K; which rows these are every workgroup of the segment finds by
 // itself, so that nothing waits for a selection that is not its own: 128 segments of up to 3345 rows, nearly all of them kept, 31 us (137 MB), with a launch that selects
 // (10 us, by the longest segment) and one that copies 40.  Of 16 segments of up to 10047 rows down to 1024 on average (MXFP4) the selection is 11 of 19 us.  The copy is bound by memory: 16 rows of every wave are on their way at once.
-template <int UNITS, int SCALES, class TAB>
+template <int UNITS, int SCALES, int HELD, class TAB>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays in, const CacheArrays out, int32_t* __restrict__ kept_idx, int w, int slice, const TAB tab) {
-  __shared__ EvictLds l;
+  __shared__ EvictLds<HELD> l;
   __shared__ int32_t sh_at[6];                         // segment, its slice, first row of the room, rows in use, first row of the other room, max(C_h, w)
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   if (tid < kWave) {
@@ -447,7 +453,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays 
       const int b0 = wave * rows_each, i0 = b0 + lane, i1 = min(m, b0 + rows_each);
       uint32_t least, k;
       evict_threshold(l, keys, m, (uint32_t)want, i0, i1, least, k);
-      auto key_of = [&](int i) __attribute__((always_inline)) { return m <= kEvictHeld ? l.held[i] : weight_key(keys[i]); };
+      auto key_of = [&](int i) __attribute__((always_inline)) { return evict_key<HELD>(l, keys, i); };
       // a wave counts its kept rows by votes, then emits them at the places that the waves before it leave
       uint32_t gt = 0, eq = 0;
       for (int b = b0; b < i1; b += 4 * kWave) {
@@ -718,11 +724,12 @@ extern "C" slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_
   // (a segment with a shorter room never holds cap rows)
   auto cap_of = [&](int64_t s) { return std::max(h_budgets[s % desc->Hkv], w); };
   auto most_of = [&](int64_t s) { return std::min<int64_t>(desc->h_offsets[s + 1] - desc->h_offsets[s], cap_of(s)); };
-  int64_t most = 0;
+  int64_t most = 0, longest = 0;
   for (int64_t s = 0; s < S; ++s) {
     const int64_t rows = most_of(s), room = out_desc->h_offsets[s + 1] - out_desc->h_offsets[s];
     if (room < rows) return fail(SLKV_ERR_CAPACITY, "segment %lld: up to %lld rows into a room of %lld", (long long)s, (long long)rows, (long long)room);
     most += rows;
+    longest = std::max(longest, desc->h_offsets[s + 1] - desc->h_offsets[s]);
   }
   const void* ins[] = {cache->d_k, cache->d_v, cache->d_k_scale, cache->d_v_scale, cache->d_pos, cache->d_weight, cache->d_lengths};
   const void* outs[] = {out->d_k, out->d_v, out->d_k_scale, out->d_v_scale, out->d_pos, out->d_weight, out->d_lengths, d_kept_idx};
@@ -731,15 +738,23 @@ extern "C" slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_
     for (int j = 0; j < 8; ++j)
       if (overlap(ins[i], outs[j], i == 6 ? 4 * S : rows_in * each[i], j == 6 ? 4 * S : rows_out * each[j]))
         return fail(SLKV_ERR_BAD_ARG, "arrays of cache and out overlap");
-  // slices: two workgroups a CU, if the rows are enough for that; a segment's last one is half empty on average
-  const int slice = (int)std::min<int64_t>(kEvictSlice, std::max<int64_t>(64, ceil_div(most, std::max<int64_t>(512 - S / 2, 256))));
+  // Rooms of up to kEvictHeld rows: two workgroups a CU and all keys in LDS.  Longer ones: one workgroup a CU, with three times the keys in LDS and slices of twice the rows (8
+  // segments of up to 34 K rows to 1024 54.7 -> 40.4 us, 64 of them in 4 bits 73.3 -> 44.6, 16 of up to 37 K to 16 K 94.5 -> 90.4).
+  const bool held_all = longest <= kEvictHeld;
+  // slices: as many workgroups, if the rows are enough for that; a segment's last one is half empty on average
+  const int64_t places = held_all ? 512 : 256;
+  const int slice = (int)std::min<int64_t>(held_all ? kEvictSlice : 2 * kEvictSlice, std::max<int64_t>(64, ceil_div(most, std::max(places - S / 2, places / 2))));
   ScopedKernelTimer timer(SLKV_K_EVICT);
   auto blocks_of = [&](int64_t s) { return std::max<int64_t>(1, (most_of(s) + slice - 1) / slice); };
   auto launch = [&](const auto& tab, int blocks) {
     using TAB = std::decay_t<decltype(tab)>;
     auto go = [&](auto units, auto scales) {
-      SLKV_LAUNCH((evict_kernel<decltype(units)::value, decltype(scales)::value, TAB>), dim3(blocks), dim3(kEvictThreads), 0, (hipStream_t)hip_stream,
-                  arrays_of(cache), arrays_of(out), d_kept_idx, w, slice, tab);
+      auto with = [&](auto held) {
+        SLKV_LAUNCH((evict_kernel<decltype(units)::value, decltype(scales)::value, decltype(held)::value, TAB>), dim3(blocks), dim3(kEvictThreads), 0,
+                    (hipStream_t)hip_stream, arrays_of(cache), arrays_of(out), d_kept_idx, w, slice, tab);
+      };
+      if (held_all) with(std::integral_constant<int, kEvictHeld>{});
+      else with(std::integral_constant<int, kEvictHeldLong>{});
     };
     using std::integral_constant;
     const integral_constant<int, 0> none{};

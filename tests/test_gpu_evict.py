@@ -88,6 +88,17 @@ def test_equal_weights(n):
     check(cache, [n // 3, n // 2, n // 5, n - 7], 5)
 
 
+@pytest.mark.parametrize("n", [12289, 36864, 36870, 36871, 50000])
+@pytest.mark.parametrize("cap", [7, 300, 9000])
+def test_keys_in_lds_and_in_memory(n, cap):
+    # w = 6: up to 36864 ranked keys stay in LDS
+    rng = np.random.default_rng(n + cap)
+    cache = random_cache(rng, "bf16_kv4", 1, 3, 1, 64, [n, 40, n - 1], rooms=[n + 30, 50, n], before=3)
+    check(cache, [cap, 20, cap + 1], 6, slack=1)
+    cache.weight.copy_((cache.weight * 8).floor())         # many equal weights, some in LDS and some not
+    check(cache, [cap, 20, cap + 1], 6)
+
+
 @pytest.mark.parametrize("around", [0x3F800000, 0x3F800100, 0x3F7FFF00, 0x40000000])
 @pytest.mark.parametrize("width,low", [(64, 0.0), (64, -1.0), (300, 1e-30), (2, 0.0), (1000, 0.999)])
 def test_many_weights_a_few_steps_apart(around, width, low):
