@@ -307,7 +307,9 @@ __device__ __forceinline__ uint32_t weight_key(float v) { return v != v ? 0xffff
 
 template <int HELD>
 struct EvictLds {
-  uint32_t held[HELD], hist[kHistBins], scan[16], res[2], near_key[kEvictRank], ends[2][kEvictWaves];
+  uint32_t held[HELD], hist[kHistBins], scan[16], res[2], near_key[kEvictRank];
+  uint32_t ends[2][kEvictWaves];      // a wave's smallest and largest key; the barrier behind their writing is the only one between the reading and the end of the selection where all keys are equal
+  uint32_t votes[2][kEvictWaves];     // a wave's keys above the smallest kept one, and equal to it: words of their own, since other waves may still be reading `ends`
   int32_t near_row[kEvictRank], near_count, from[kEvictSlice * (HELD == kEvictHeld ? 1 : 2)];
 };
 
@@ -467,12 +469,12 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(const CacheArrays 
           eq += (uint32_t)__popcll(__ballot(in && x[t] == least));
         }
       }
-      if (lane == 0) l.ends[0][wave] = gt, l.ends[1][wave] = eq;
+      if (lane == 0) l.votes[0][wave] = gt, l.votes[1][wave] = eq;
       __syncthreads();
       uint32_t at = 0, e = 0;                         // kept rows, and rows of the smallest kept key, in the waves before
       for (int v = 0; v < wave; ++v) {
-        at += l.ends[0][v];
-        e += l.ends[1][v];
+        at += l.votes[0][v];
+        e += l.votes[1][v];
       }
       at += min(e, k);
       const uint64_t below = (1ull << lane) - 1;

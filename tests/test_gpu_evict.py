@@ -88,6 +88,24 @@ def test_equal_weights(n):
     check(cache, [n // 3, n // 2, n // 5, n - 7], 5)
 
 
+@pytest.mark.parametrize("value", [0.0, 1.5, float("nan")])
+@pytest.mark.parametrize("n", [40, 100, 700, 1030, 2100, 12300, 40000])
+def test_equal_weights_of_a_cache_that_nobody_attended_to(n, value):
+    """All ranked weights of every segment are equal, as fill leaves them: no digit is looked for, and waves without ranked rows are at the votes while
+    others still read the smallest and largest key."""
+    S = 24 if n < 10000 else 8
+    rng = np.random.default_rng(n)
+    lens = [n - int(x) for x in rng.integers(0, 30, S)]
+    cache = random_cache(rng, "bf16", S // 4, 4, 1, 64, lens, rooms=[n] * S)
+    rows = cache.rows(np.concatenate([[0], np.cumsum(lens)]))
+    cache.fill(rows[0], rows[1], np.concatenate([[0], np.cumsum(lens)]))
+    assert all(bool((cache.weight[int(a):int(a) + m] == 0).all()) for a, m in zip(cache.layout.offsets, lens))
+    cache.weight.fill_(value)
+    for w in (0, 5):
+        out = check(cache, [w + 1, 9, n // 2, n - 33], w)
+        assert out.lengths.cpu().tolist() == [min(m, max(c, w)) for m, c in zip(lens, [w + 1, 9, n // 2, n - 33] * (S // 4))]
+
+
 @pytest.mark.parametrize("n", [12289, 36864, 36870, 36871, 50000])
 @pytest.mark.parametrize("cap", [7, 300, 9000])
 def test_keys_in_lds_and_in_memory(n, cap):
