@@ -246,16 +246,18 @@ __device__ __forceinline__ f32x4 output_of(f32x4 o, float total, bool none) {
 
 // Weights of rows j0 .. j1 - 1 of a segment (j0 a multiple of 32) from its logits, four rows a thread; SHARED: where rows are few and queries many, 1 << bits threads
 // share the R queries (48 segments, 15 queries: the join 6.7 us -> 6.4; 8 segments, 64 queries: 14.2 -> 11.9).  lse: of the queries, in LDS.  The first numbers can
-// be asked for before the log-sum-exp is known.
+// be asked for before the log-sum-exp is known.  Logits of rows that a query does not see are -infinity and add 0, unless the query's log-sum-exp is NaN: sums that
+// come out NaN where not every query sees the row are taken again from the queries that do.
 constexpr int kAheadQueries = 4;
 struct WeightsAhead { f32x4 x[kAheadQueries], w; };
 template <int NT, bool SHARED>
 struct Weights {
   const AttendArgs& a;
   const int64_t start;
-  const int tile, j1;
+  const int tile, j1, all;                             // the segment's first tile, end, rows that every query sees
   int bits = 0, sp = 0, first;                         // the thread's queries sp, sp + (1 << bits), .., its first row
-  __device__ __forceinline__ Weights(const AttendArgs& args, int64_t start_row, int first_tile, int j0, int end) : a(args), start(start_row), tile(first_tile), j1(end) {
+  __device__ __forceinline__ Weights(const AttendArgs& args, int64_t start_row, int first_tile, int n, int j0, int end)
+      : a(args), start(start_row), tile(first_tile), j1(end), all(n - args.T + 1) {
     if constexpr (SHARED) {
       while (bits < 4 && 4 * (NT >> (bits + 1)) >= j1 - j0 && (kAheadQueries << bits) < a.R) ++bits;
       sp = (int)threadIdx.x / (NT >> bits);
@@ -284,6 +286,17 @@ struct Weights {
     const float* l = logits_of(j);
 #pragma unroll 8
     for (int r = sp + (kAheadQueries << bits); r < a.R; r += 1 << bits) one(*(const f32x4*)(l + r * kTileRows), lse[r]);
+    const float any = (s[0] + s[1]) + (s[2] + s[3]);
+    if (a.T > 1 && j + 3 >= all && any != any) {
+      s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int r = sp; r < a.R; r += 1 << bits) {
+        const f32x4 x = *(const f32x4*)(l + r * kTileRows);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < all + r % a.T) s[e] += exp2_fast(fmaf(x[e], a.c_log2, -lse[r]));
+      }
+    }
     return s + h.w;
   }
   __device__ __forceinline__ void store(f32x4 s, int j) const {
@@ -675,7 +688,7 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
   if (!whole || !a.w_out) return;
   __threadfence_block();
   __syncthreads();
-  const Weights<W * kWave, false> weights(a, base, at.tile, 0, n);
+  const Weights<W * kWave, false> weights(a, base, at.tile, n, 0, n);
   WeightsAhead h;
   weights.load(h, weights.first);
   weights.add(h, sh_lse, nullptr);
@@ -744,7 +757,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_join_kernel(const Atten
   };
   load_units(grp);
   const int end = min(n, (part + 1) * w.each);
-  const Weights<kAttendThreads, true> weights(a, w.start, w.tile, part * w.each, end);
+  const Weights<kAttendThreads, true> weights(a, w.start, w.tile, n, part * w.each, end);
   WeightsAhead h;
   if (a.w_out) weights.load(h, weights.first);
 

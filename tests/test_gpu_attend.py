@@ -202,6 +202,30 @@ def test_queries_that_are_not_finite_stay_alone():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [3, 40, 5000])
+@pytest.mark.parametrize("G,T", [(2, 3), (3, 10), (16, 4)])
+def test_queries_without_a_softmax_leave_the_weights_of_rows_behind_them(dtype, n, G, T):
+    """A query that holds a NaN makes NaN of the weights of the rows that it sees, and of no others."""
+    rng = np.random.default_rng([n, G, T])
+    cache = random_cache(rng, dtype, 2, 1, G, 64, [n, n + 1], rooms=[n + 5, n + 40])
+    q = normal(rng, (2, G, T, 64), dtype)
+    q[0, 0, 0, 3] = float("nan")
+    q[1, G - 1, T - 2, 5] = float("nan")
+    _, _, w = check(cache, q, T)
+    off = cache.layout.offsets
+    assert bool(torch.isfinite(w[int(off[0]) + max(n - T + 1, 0):int(off[0]) + n]).all()) and bool(torch.isfinite(w[int(off[1]) + n]))
+    assert bool(torch.isnan(w[int(off[1])]))
+
+
+@pytest.mark.parametrize("n", [20, 5000])
+def test_logits_of_minus_infinity_up_to_a_row_that_later_queries_see(n):
+    cache = random_cache(np.random.default_rng(4), "f32", 1, 1, 1, 64, [n])
+    cache.k[:n - 1, 0] = float("-inf")
+    _, lse, w = check(cache, torch.ones((1, 1, 2, 64), device="cuda"), 2)
+    assert bool(torch.isnan(lse[0, 0, 0])) and bool(torch.isfinite(lse[0, 0, 1])) and bool(torch.isfinite(w[n - 1])) and bool(torch.isnan(w[0]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_same_bits_every_time_and_in_place(dtype):
     rng = np.random.default_rng(9)
     cache = random_cache(rng, dtype, 3, 2, 4, 128, [5000, 10, 700, 0, 129, 33], rooms=[6000, 20, 900, 10, 140, 60])
