@@ -172,7 +172,7 @@ def _ptr(t):
 
 
 def _stream(stream):
-    """The stream's handle; None: the current stream of the current device, read without the Stream object that
+    """The handle of a stream (a handle stays one); None: the current stream of the current device, read without the Stream object that
     torch.cuda.current_stream() makes (3 us of a call's 16) where torch has the function for it, which is not a public one."""
     import torch
     if stream is None:
@@ -180,7 +180,7 @@ def _stream(stream):
         if raw is not None:
             return raw(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
-    return stream.cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def slkv_version():

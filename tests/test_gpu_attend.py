@@ -267,6 +267,68 @@ def test_three_streams_at_once():
         assert all(torch.equal(a, b) for one in g for a, b in zip(w, one))
 
 
+@pytest.mark.parametrize("graph", [False, True])
+def test_one_cache_on_three_streams_at_once(graph):
+    """Calls that only read the cache, nothing orders them: segments in parts, whose sums pass through a workspace."""
+    rng = np.random.default_rng(15)
+    cache = random_cache(rng, "bf16", 1, 8, 4, 128, [6000 + 100 * i for i in range(8)])
+    qs = [normal(rng, (1, 32, 1, 128), "bf16") for _ in range(3)]
+    want = [cache.attend(q, weight=False) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = [[] for _ in qs]
+    torch.cuda.synchronize()
+    if graph:
+        graphs, outs = [], []
+        for q in qs:                                     # captured on one stream, replayed on three
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=streams[0]):
+                outs.append(cache.attend(q, weight=False))
+            graphs.append(g)
+    for _ in range(20):
+        for i, (q, s, g) in enumerate(zip(qs, streams, got)):
+            with torch.cuda.stream(s):
+                if graph:
+                    graphs[i].replay()
+                    g.append(tuple(x.clone() for x in outs[i]))
+                else:
+                    g.append(cache.attend(q, weight=False))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(a, b) for one in g for a, b in zip(w, one))
+
+
+def test_first_call_inside_a_capture():
+    rng = np.random.default_rng(16)
+    cache, other = (random_cache(rng, "bf16_kv8", 1, 2, 4, 128, [5000, 40]) for _ in range(2))
+    other.attend(normal(rng, (1, 8, 2, 128), "bf16_kv8"))      # (the device has loaded the kernels)
+    q, w = normal(rng, (1, 8, 2, 128), "bf16_kv8"), torch.full_like(cache.weight, -1.0)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out, lse = cache.attend(q, weight=w)
+    for i in range(4):
+        q.copy_(normal(rng, q.shape, "bf16_kv8"))
+        before, after, o2, l2 = run(cache, q)            # an eager call between the replays
+        w.fill_(-1.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, o2) and torch.equal(lse, l2) and torch.equal(w, after)
+
+
+def test_scratch_does_not_pile_up():
+    rng = np.random.default_rng(17)
+    cache = random_cache(rng, "bf16", 1, 8, 4, 64, [20000] * 8)
+    torch.cuda.synchronize()
+    for T in range(1, 17):
+        cache.attend(normal(rng, (1, 32, T, 64), "bf16"))
+    held, most = torch.cuda.memory_allocated(), B.slkv_attend_workspace_bytes(cache.layout, 16, True)
+    del cache
+    # its rows and the largest of 16 workspaces (together they would be 8 times that one); torch may leave up to 1 MiB at the end of each of the five
+    assert held - torch.cuda.memory_allocated() < 8 * 20000 * (2 * 128 + 8) + most + (6 << 20)
+
+
 def test_other_stream():
     rng = np.random.default_rng(10)
     cache = random_cache(rng, "bf16_kv4", 2, 2, 4, 128, [3000, 10, 700, 50])

@@ -1,5 +1,6 @@
 """CPU-only tests of the calls on a cache: descriptors, refusals before any GPU call, workspace sizes."""
 
+import contextlib
 import ctypes as C
 import types
 
@@ -173,3 +174,30 @@ def test_a_stream_of_another_device_is_refused():
     cache.device = torch.device("cuda", 0)
     with pytest.raises(ValueError, match="stream"):
         cache._on(types.SimpleNamespace(device=torch.device("cuda", 1)))
+
+
+def test_calls_of_one_cache_share_scratch_on_one_stream_alone(monkeypatch):
+    """Calls that nothing orders have a workspace each: on two streams, and captured ones, whose graphs may be replayed on any."""
+    lay = layout()
+    cache = api.Cache.__new__(api.Cache)
+    cache.__dict__.update(layout=lay, B=2, Hq=8, Hkv=2, d=128, query_dtype=torch.bfloat16, device=torch.device("cpu"), weight=None, rows_in_all=190, _arrays=None,
+                          _workspaces={}, _attend_like={})
+    monkeypatch.setattr(cache, "_on", lambda stream: contextlib.nullcontext(), raising=False)
+    running = []
+    monkeypatch.setattr(B, "slkv_attend_cache", lambda layout_, arrays_, q, out, workspace, lse, weight, stream=None: running.append((workspace, out, lse)))
+
+    def attend(stream, T=1, capturing=False):
+        monkeypatch.setattr(B, "_stream", lambda s: stream)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+        cache.attend(torch.zeros((2, 8, T, 128), dtype=torch.bfloat16), weight=False)
+        return running[-1][0]
+    apart = [attend(0), attend(0x10), attend(0x20), attend(0, capturing=True), attend(0, capturing=True), attend(0x10, capturing=True)]
+    need = B.slkv_attend_workspace_bytes(lay, 1, False)
+    for i in range(3):
+        spans = sorted((x.data_ptr(), x.data_ptr() + x.nbytes) for one in running for x in (one[i],))
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+    assert all(ws.dtype == torch.uint8 and ws.is_contiguous() and ws.nbytes >= need for ws in apart)
+    assert attend(0x10) is apart[1] and attend(0) is apart[0]
+    # it grows with the largest call
+    big = B.slkv_attend_workspace_bytes(lay, 16, False)
+    assert attend(0x10, T=16).nbytes >= big and attend(0x10).nbytes >= big and attend(0).nbytes >= need
