@@ -352,9 +352,13 @@ def _offsets_of(layout, offsets):
 
 
 def _budgets_of(layout, budgets):
-    budgets = np.ascontiguousarray(budgets, dtype=np.int32)
-    if budgets.shape != (layout.Hkv,):
-        raise ValueError("budgets: %d entries wanted, got shape %s" % (layout.Hkv, budgets.shape))
+    given = np.asarray(budgets)
+    if given.shape != (layout.Hkv,):
+        raise ValueError("budgets: %d entries wanted, got shape %s" % (layout.Hkv, given.shape))
+    with np.errstate(invalid="ignore"):
+        budgets = np.ascontiguousarray(given, dtype=np.int32)
+    if given.dtype != np.int32 and not np.array_equal(given, budgets):       # (numpy wraps and truncates)
+        raise ValueError("budgets: 32-bit whole numbers wanted")
     return budgets
 
 
@@ -392,8 +396,10 @@ def slkv_attend_cache(layout, cache, q, out, workspace, lse=None, weight_out=Non
 
 def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, kept_idx=None, stream=None):
     """Enqueues the copy of the rows that stay to another cache."""
-    budgets = _budgets_of(layout, budgets)
-    _check(lib().slkv_evict_cache(layout.address, cache.address, out_layout.address, out.address, int(w), budgets.ctypes.data, _ptr(kept_idx),
+    budgets, w = _budgets_of(layout, budgets), int(w)
+    if not -2 ** 31 <= w < 2 ** 31:                      # (ctypes would wrap it)
+        raise ValueError("w: %d is no 32-bit number" % w)
+    _check(lib().slkv_evict_cache(layout.address, cache.address, out_layout.address, out.address, w, budgets.ctypes.data, _ptr(kept_idx),
                                   _stream(stream)))
 
 

@@ -169,6 +169,28 @@ def test_evict_refuses_before_touching_the_gpu():
     assert evict(out=arrays(**dict(one, d_lengths=NULL))) == 1
 
 
+@pytest.mark.parametrize("budgets,w", [(np.array([2 ** 32 + 40, 20]), 4), (np.array([40, -2 ** 32]), 4), ([40.5, 20], 4), ([40, float("nan")], 4), ([40, 20], 2 ** 32 + 4),
+                                       ([40, 20], 2 ** 31)])
+def test_evict_refuses_numbers_beyond_32_bits(monkeypatch, budgets, w):
+    """A capacity of 2^32 is not one of 0."""
+    calls = types.SimpleNamespace(slkv_evict_cache=lambda *a: pytest.fail("the call went through"))
+    monkeypatch.setattr(B, "lib", lambda: calls)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    there = types.SimpleNamespace(address=FAKE)
+    with pytest.raises(ValueError):
+        B.slkv_evict_cache(layout(), there, layout(), there, w, budgets)
+
+
+def test_evict_takes_whole_numbers_of_any_type(monkeypatch):
+    seen = []
+    monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(slkv_evict_cache=lambda *a: seen.append(((C.c_int32 * 2).from_address(a[5])[:], a[4])) or 0))
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    there = types.SimpleNamespace(address=FAKE)
+    for budgets in ([40, 20], (40, 20), np.array([40, 20], dtype=np.int64), np.array([0, 40, 0, 20], dtype=np.int32)[1::2], np.array([40.0, 20.0])):
+        B.slkv_evict_cache(layout(), there, layout(), there, np.int64(4), budgets)
+    assert seen == [([40, 20], 4)] * 5
+
+
 def test_a_stream_of_another_device_is_refused():
     cache = api.Cache.__new__(api.Cache)
     cache.device = torch.device("cuda", 0)
