@@ -129,6 +129,24 @@ def test_segment_tables(S):
     check(cache, normal(rng, (S, 2, 1, 64), "bf16"), 1)
 
 
+@pytest.mark.parametrize("S", [599, 600, 601, 1199, 1200, 1201])
+@pytest.mark.parametrize("split", [False, True])
+def test_ends_of_the_large_table(S, split):
+    """A launch takes 600 segments: full ones, and a launch of one segment that uses the workspace of the one before, with whole segments in an order of their own and
+    with parts in theirs."""
+    rng = np.random.default_rng([S, split])
+    lens = rng.integers(0, 60, S)
+    rooms = lens + 9
+    ends = [0, 598, 599, 600, 1198, 1199, 1200]
+    for s in ends:
+        if s < S:
+            lens[s], rooms[s] = (1500 + s, 24000) if split else (40 + s % 7, 90)
+    cache = random_cache(rng, "bf16", S, 1, 2, 64, lens.tolist(), rooms=rooms.tolist(), before=4)
+    # (without weights the workspace holds the sums of parts, 16 bytes where there are none)
+    assert (B.slkv_attend_workspace_bytes(cache.layout, 1, False) > 16) == split
+    check(cache, normal(rng, (S, 2, 1, 64), "bf16"), 1)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n", [40, 3000])
 def test_large_and_concentrated_logits(dtype, n):
