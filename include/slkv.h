@@ -24,7 +24,7 @@
  *     buffer; the library allocates no device memory.  What it keeps between calls: per device,
  *     that its one-time set-up has been done (slkv_init), and the optional kernel-timing
  *     recorder at the end of this header.
- *   - slkv_score_heads, slkv_compress_layer and slkv_recompress_layer only enqueue work on `hip_stream` (a
+ *   - slkv_score_heads, slkv_compress_layer, slkv_recompress_layer and the calls on a cache only enqueue work on `hip_stream` (a
  *     hipStream_t passed as void*, NULL = the default stream) and return without
  *     synchronising.  Host-side descriptors are consumed before the call returns.
  *   - Every argument is validated before the first GPU call; on any error nothing is
@@ -383,8 +383,11 @@ slkv_status slkv_cache_rows(const slkv_cache_desc* desc, const slkv_cache* cache
  *   lse = ln sum_j exp(x_j),  out = sum_j exp(x_j - lse) v_j,
  *   weight_out[j] = weight[j] + sum over the queries of the segment that see j of exp(x_j - lse)   for j < n_s.
  * A query that sees no row: out 0, lse -infinity, nothing added.  Infinities and NaN in rows that a query does not see do not
- * reach it.  Products are exact, sums, softmax and weights fp32; out is rounded once.  The result does not depend on
- * what else runs, and has the same bits every time.
+ * reach it.  The result does not depend on what else runs, and has the same bits every time.
+ * Products q . k are exact (fp32 elements: rounded), their sums, the softmax, lse and weight_out fp32; out is rounded once.  A softmax weight enters
+ * the product with v as it is for SLKV_F32, and as two 16-bit numbers otherwise, which hold it to 2^-16 of itself (SLKV_F16: to 2^-22 of itself or 2^-37 of the
+ * query's largest weight, whichever is more; an infinite v beside a weight that they cannot hold gives NaN).  Sums are divided at the end:
+ * results are finite for |x| up to 2^22 and |v| times the rows up to 2^118.
  * d_q   [B][Hq][T][d] (device, read only); T >= 1, (Hq/Hkv)*T <= 64
  * d_out [B][Hq][T][d] in the type of the queries;  d_lse [B][Hq][T] fp32, may be NULL
  * d_weight_out [rows] fp32 or NULL; may be cache->d_weight itself.  cache->d_weight NULL: sums begin at 0.
@@ -418,7 +421,7 @@ slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cach
  * (two passes, long histories: 1 + 1 + 6 + 1; one pass: 1 + 4 + 3 + 1; histories up to 32768: 1 + 1 + 1 + 1, both passes in
  * one launch 0 + 1 + 1 + 1, one pass 1 + 4 + 1 + 1, in each of these without the last one where the selection copies all rows; ragged
  * caches and batches of many short histories: one SLKV_K_SCORE_ACCUM record in all, where the scoring launch selects and copies too).
- * Fill, append, rows and evict make one each; attend one or two for every 600 segments.
+ * Fill, append, rows and evict make one each (more beyond 240 segments; 560 and more share a launch whose rooms and rows outside are below 65536); attend one or two for every 600 segments.
  * Process-wide; not meant for production.
  */
 typedef enum {

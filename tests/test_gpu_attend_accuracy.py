@@ -72,3 +72,51 @@ def test_weights(dtype, n):
     cache.attend(q)
     want = decode.attend(f64(q), *cache_values(cache), cache.layout.offsets, [n] * 32, 4, 1)[2]
     assert rms((f64(cache.weight) - want) / want) <= 12 * U
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("n", [50, 5000])
+def test_logits_at_the_end_of_the_range(dtype, sign, n):
+    """Some rows share the largest logit, 2^22 in magnitude; the others are 2^14 and more below: the mean of their values, whatever the logit."""
+    rng = np.random.default_rng(n)
+    d = 64
+    cache = random_cache(rng, dtype, 1, 2, 2, d, [n, n])
+    k = np.zeros((2 * n, d), np.float32)
+    k[:, 0] = sign * 2.0 ** 13 - (32 + 32 * rng.integers(0, 60, 2 * n))
+    for s in range(2):
+        k[s * n + rng.permutation(n)[:3], 0] = sign * 2.0 ** 13
+    cache.k.copy_(torch.from_numpy(k))                   # (bf16 has steps of 64 above 2^13: more than three rows then)
+    q = torch.zeros((1, 4, 1, d), dtype=cache.query_dtype, device="cuda")
+    q[..., 0] = 2.0 ** 12                                # x = 2^25 / 8
+    cache.weight.zero_()
+    out, lse = cache.attend(q)
+    held, v, w = f64(cache.k)[:, 0], f64(cache.v), f64(cache.weight)
+    half = {"f32": 0.0, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype]
+    for s in range(2):
+        top = s * n + np.flatnonzero(held[s * n:(s + 1) * n] == sign * 2.0 ** 13)
+        want = v[top].mean(0)
+        # equal weights, which carry the same rounding of the logit; fp32 adds the values and divides
+        assert (np.abs(f64(out)[0, 2 * s:2 * s + 2, 0] - want) <= (2.0 ** -15 if half else (5 + len(top)) * U) * np.abs(v[top]).max() + half * np.abs(want)).all()
+        assert (np.abs(f64(lse)[0, 2 * s:2 * s + 2, 0] - (sign * 2.0 ** 22 + np.log(len(top)))) <= 0.5).all()
+        # 2 queries a segment; exp2 of a difference that is off by the roundings of lse: three numbers below 2^23, half a step of 1/4 each at most
+        assert (np.abs(np.log2(w[top] / (2 / len(top)))) <= 0.75).all()
+        w[top] = 0
+    assert (w == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "bf16_kv4"])
+@pytest.mark.parametrize("n", [33, 6000])
+def test_values_at_the_end_of_the_range(dtype, n):
+    """Values of one sign and 2^118 over the rows: their mean, though their sum comes near the largest number."""
+    rng = np.random.default_rng(n)
+    cache = random_cache(rng, dtype, 1, 2, 4, 64, [n, n])
+    e = 118 - int(np.ceil(np.log2(n)))
+    if dtype == "bf16_kv4":
+        cache.v_scale.fill_(127 + e)
+        cache.v.fill_(0x22)
+    else:
+        cache.v.fill_(2.0 ** e)
+    q = normal(rng, (1, 8, 1, 64), dtype) * 3
+    out, _ = cache.attend(q)
+    assert (np.abs(f64(out) / 2.0 ** e - 1) <= 2.0 ** -15 + (2.0 ** -20 + 16 * U if dtype == "f32" else 2.0 ** -8)).all()
