@@ -246,7 +246,7 @@ class Cache:
             B.slkv_fill_cache(self.layout, self._arrays, src_offsets, k_rows, v_rows, pos)
 
     def append(self, k, v, pos=None, at=None, stream=None):
-        """k, v [B, Hkv, T, d] (any strides, rows contiguous), pos [B, T]: the next T tokens enter behind the rows in use, or behind the first at[s]
+        """k, v [B, Hkv, T, d] (strides of multiples of 16 bytes, 0 among them, rows contiguous), pos [B, T]: the next T tokens enter behind the rows in use, or behind the first at[s]
         of them (drafted tokens that were not accepted are overwritten this way)."""
         shape = (self.B, self.Hkv, k.shape[2] if k.dim() == 4 else 0, self.d)
         for t, name in ((k, "k"), (v, "v")):

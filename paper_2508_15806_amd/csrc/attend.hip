@@ -383,7 +383,10 @@ template <int KIND, int D, int RT, int W, class TAB>
 __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend_kernel(const AttendArgs a, const TAB tab) {
   using A = Attend<KIND, D>;
   constexpr int kProducts = A::kF32 ? D / 4 : D / 32, kVD = A::kVD, kEach = A::kEach;
-  constexpr bool kAhead = RT * D <= 128;               // the next step's rows are on their way during a step (more tiles of queries leave no registers for them)
+  // The next step's rows are on their way during a step.  More tiles of queries leave no registers for them beside the careful step, the second copy of the step in
+  // this kernel, which decides how many it takes: with D = 128 two tiles take 197 to 248 of 256 without rows ahead (168 to 244 if the careful step is compiled out, with rows
+  // ahead 213 to 253, fp32 in scratch), and four tiles put 84 to 444 bytes a lane into scratch (none if it is).
+  constexpr bool kAhead = RT * D <= 128;
   __shared__ __align__(16) float sh_o[W][16][D + 4];
   __shared__ float sh_m[W][16 * RT], sh_l[W][16 * RT];
   __shared__ float sh_lse[16 * RT], sh_total[16 * RT];
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(W * kWave, attend_waves_per_cu(RT) / W) void attend
 
   float ref[RT], sum[RT];
   f32x4 acc[RT][kVD];
-  // The weights go into the products with the values as two 16-bit numbers each, which leaves 2^-16 of a weight (one number: 2^-9 of each, as much again as
+  // The weights go into the products with the values as two 16-bit numbers each, which leaves 2^-16 of a weight (fp16: 2^-22, or 2^-25 of the reference; one number: 2^-9 of each, as much again as
   // the rounding of the output).  An infinite value would make NaN of the second one's zero, and values of rows that a query does not see would reach it through
   // a weight of zero: sums that come out not finite are taken again, with such values kept out of the second number's products and, where not every query
   // sees the row, out of both.
@@ -856,9 +859,9 @@ static AttendPlan plan_attend(const slkv_cache_desc* d, int T, bool weights) {
   p.waves = rt == 1 && S <= 64 && rows >= 32768 ? 8 : 4;
   const int64_t places = 256 * attend_waves_per_cu(rt) / p.waves;
   // Whole segments while the longest is done, beside the others, before parts and the second launch that joins them would be.  One workgroup: 10.2 ns a row of 512
-  // bytes, 4.9 of 136, and 0.4 of the time that the chip takes for all rows at 5 TB/s, which it shares with the others; the second launch: 5 us.  (Whole and in parts, us: 8 segments of 96 to
-  // 440 rows 10.2, 12.8; 8 of 1016 rows of 512 bytes 15.3, 12.5; 512 of 280 to 2189 rows of 136 bytes 23.5, 32.7; 256 of up to 3140 rows of 512 bytes 54.0, 40.4; 512 of up to 3140 of
-  // 256 bytes 45.0, 46.6; 256 of up to 3140 of 136 bytes 25.6, 20.9.)
+  // bytes, 4.9 of MXFP4 (128 bytes, which leave its exponents out, as all of this rule's do), and 0.4 of the time that the chip takes for all rows at 5 TB/s, which it shares with the others; the second launch: 5 us.  (Whole, from 65 segments on the longest first, and in parts, which are launched as they stand, us: 8 segments of 96 to
+  // 440 rows 10.2, 12.8; 8 of 1016 rows of 512 bytes 15.3, 12.5; 512 of 280 to 2189 rows of MXFP4 23.5, 32.7; 256 of up to 3140 rows of 512 bytes 54.0, 40.4; 512 of up to 3140 of
+  // 256 bytes 45.0, 46.6; 256 of up to 3140 of MXFP4 25.6, 20.9.)
   const double whole_us = most * (0.0035 * rt + row_bytes / 75e3), split_us = rows * row_bytes / 5e6 * 0.6 + 5;
   if (most <= kMost && whole_us <= split_us) {
     p.rows_each = std::max<int64_t>(kTileRows, round(most));

@@ -22,7 +22,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kScaleBlock = 32;      // MXFP4 elements that share an exponent
 
-// Segments seg0 .. seg0 + nseg - 1 of a call.  a[i], b[i], c[i]: what the launch's kernel says.  The arguments are at most 4 KiB, so a
+// Segments seg0 .. seg0 + nseg - 1 of a call.  w[r][i]: of segment seg0 + i, for each r what the launch's kernel says.  The arguments are at most 4 KiB, so a
 // call with more segments than a table holds makes several launches; the small table spares the ordinary call the larger one's 3.5 KB of arguments.
 template <int N, int WORDS>
 struct SegWords {
