@@ -164,7 +164,7 @@ class Cache:
     k_scale, v_scale [rows, d / 32] uint8; lengths [B * Hkv], pos [rows] int32; weight [rows] fp32); given keys without lengths fill their
     rooms.  positions, weights = False: a cache without these arrays.  Calls run on `stream`, or the current stream of the cache's device; the caller orders those that
     read or write the same arrays on several streams (attend() writes the weights where it has to add to them), and the object outlives the graphs that
-    captured them.  attend() has scratch of its own on every stream and in every graph."""
+    captured them.  attend() has scratch of its own on every stream and in every graph that torch captures."""
 
     def __init__(self, dtype, B_, Hq, Hkv, d, offsets, k=None, v=None, k_scale=None, v_scale=None, lengths=None, pos=None, weight=None,
                  device="cuda", positions=True, weights=True):
