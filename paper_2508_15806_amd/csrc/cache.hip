@@ -308,8 +308,8 @@ __device__ __forceinline__ uint32_t weight_key(float v) { return v != v ? 0xffff
 template <int HELD>
 struct EvictLds {
   uint32_t held[HELD], hist[kHistBins], scan[16], res[2], near_key[kEvictRank];
-  uint32_t ends[2][kEvictWaves];      // a wave's smallest and largest key; the barrier behind their writing is the only one between the reading and the end of the selection where all keys are equal
-  uint32_t votes[2][kEvictWaves];     // a wave's keys above the smallest kept one, and equal to it: words of their own, since other waves may still be reading `ends`
+  uint32_t ends[2][kEvictWaves];      // a wave's smallest and largest key: written before a barrier, read behind it and never written again, since no other barrier follows where all keys are equal
+  uint32_t votes[2][kEvictWaves];     // a wave's keys above the smallest kept one, and equal to it, while others may still be reading `ends`
   int32_t near_row[kEvictRank], near_count, from[kEvictSlice * (HELD == kEvictHeld ? 1 : 2)];
 };
 
