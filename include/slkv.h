@@ -412,6 +412,37 @@ slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv_cache* cac
 slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const slkv_cache_desc* out_desc, const slkv_cache* out,
                              int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx, void* hip_stream);
 
+/* ------------------------------------------------------------------ attention of a prompt
+ * Causal attention of a ragged batch of packed prompts, or of their next pieces behind a history: what makes the outputs of the layer whose K and V
+ * slkv_compress_layer then chooses from.  Sequence b has n_b = h_cu_q[b+1] - h_cu_q[b] queries, those of the last n_b of its m_b = h_cu_k[b+1] - h_cu_k[b]
+ * tokens; query i of head hq sees the keys j <= m_b - n_b + i of KV head hq / (Hq/Hkv).  With x_j = q . k_j / sqrt(d) over these,
+ *   lse = ln sum_j exp(x_j),  out = sum_j exp(x_j - lse) v_j.
+ * A query that sees no key (n_b > m_b): out 0, lse -infinity.  Infinities and NaN in keys and values that a query does not see do not reach it.  The result does
+ * not depend on what else runs, and has the same bits every time.
+ * Products q . k are exact (fp32 elements: rounded), their sums, the softmax and lse fp32; a weight enters the product with v as it is for SLKV_F32, otherwise rounded to
+ * the type of the queries relative to a power of two near the largest one; out is rounded once.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
+ */
+typedef struct {
+  uint32_t struct_size;        /* sizeof(slkv_prompt_desc) */
+  int32_t dtype;               /* slkv_dtype, all but SLKV_BF16_KV_MXFP4 */
+  int32_t B, Hq, Hkv, d;       /* d in {64, 128}; Hq % Hkv == 0 */
+  int32_t reserved[2];         /* 0 */
+  const int64_t* h_cu_q;       /* [B+1] host: queries, non-decreasing, >= 0, last < 2^31 */
+  const int64_t* h_cu_k;       /* [B+1] host: tokens of K and V; NULL: h_cu_q (whole prompts) */
+  /* element (head, token, :) of an array at head*stride_head + token*stride_tok; rows of d elements contiguous; strides >= 0 and multiples of 16
+   * bytes, 0 among them (out: rows may not overlap); token strides of k and v below 2^24 bytes */
+  int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head, out_stride_tok, out_stride_head;
+} slkv_prompt_desc;
+
+/* Device scratch of slkv_attend_prompt: need not be cleared; two calls that may overlap in time need one each. */
+slkv_status slkv_prompt_workspace_bytes(const slkv_prompt_desc* desc, size_t* bytes);
+/* d_q, d_out in the type of the queries, d_k, d_v; may be NULL where the batch has no queries, or no keys
+ * d_lse [Hq][h_cu_q[B]] fp32, may be NULL.  Outputs of tokens outside all sequences (before h_cu_q[0]) are left as they were.
+ * What the call writes may not overlap what it reads.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED, WORKSPACE, HIP. */
+slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const void* d_q, const void* d_k, const void* d_v,
+                               void* d_out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ------------------------------------------------------------------ kernel timing -----
  * Optional instrumentation for benchmarks: between slkv_profile_begin and slkv_profile_end
  * every kernel the library launches is bracketed by a HIP event pair on the call's stream.
@@ -440,7 +471,12 @@ typedef enum {
   SLKV_K_CACHE_ROWS = 10,   /* rows out of a cache */
   SLKV_K_ATTEND = 11,       /* attention over a cache */
   SLKV_K_ATTEND_JOIN = 12,  /* the parts of split segments joined; weights */
-  SLKV_K_EVICT = 13         /* eviction: selection and copy */
+  SLKV_K_EVICT = 13,        /* eviction: selection and copy */
+  SLKV_K_PROMPT = 14,       /* attention of packed prompts */
+  SLKV_K_TREE = 15,         /* attention of a tree of drafted tokens over a cache */
+  SLKV_K_TILES_JOIN = 16,   /* the parts of either put together */
+  SLKV_K_ACCEPT = 17,       /* accepted rows moved, lengths set */
+  SLKV_K_WEIGH = 18         /* weights of the accepted tokens' attention */
 } slkv_kernel_id;
 typedef struct {
   int32_t kernel; /* slkv_kernel_id */

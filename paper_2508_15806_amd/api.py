@@ -53,6 +53,43 @@ class _Buffers:
                 pass
 
 
+class _OnDevice:
+    """What Cache and PromptCall share: the checks of a call's tensors and its stream."""
+
+    def _set_device(self, device):
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._here, self._workspaces = contextlib.nullcontext(), {}
+
+    def _tensor(self, t, shape, tdt, name, contiguous=True):
+        if t.dtype != tdt or t.shape != shape:
+            raise ValueError("%s: %s of shape %s wanted, got %s of shape %s" % (name, tdt, shape, t.dtype, tuple(t.shape)))
+        if t.device != self.device:
+            raise ValueError("%s is on %s, the call on %s" % (name, t.device, self.device))
+        if contiguous and not t.is_contiguous():
+            raise ValueError("%s is not contiguous" % name)
+        return t
+
+    def _on(self, stream):
+        """The call's stream as the current one, so that what it allocates belongs to it; without one, the object's device, where it is not current."""
+        if stream is not None:
+            if stream.device != self.device:
+                raise ValueError("stream is of %s, the call on %s" % (stream.device, self.device))
+            return torch.cuda.stream(stream)
+        return self._here if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
+
+    def _workspace(self, nbytes, stream):
+        """Scratch for a call on the stream of this handle, which is the current one.  Calls that follow each other on a stream share it, and it grows with
+        the largest of them; a captured call has its own, which stays with its graph: the graph may be replayed anywhere.  (0.2 to 0.4 us of the host; a tensor for every call 0.9.)"""
+        ws = None if torch.cuda.is_current_stream_capturing() else self._workspaces.get(stream, _NOTHING)
+        if ws is None:
+            return torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        if ws.nbytes < nbytes:
+            ws = self._workspaces[stream] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        return ws
+
+
 class LayerCall(_Buffers):
     """Device buffers + descriptor for repeated calls on one layer's shapes."""
 
@@ -118,6 +155,43 @@ class RaggedCall(_Buffers):
             raise
 
 
+class PromptCall(_OnDevice):
+    """Causal attention of a batch of packed prompts, or of their next pieces behind a history: what comes before LayerCall in a layer.
+
+    cu_seqlens [B + 1]: the queries of every sequence; cu_k [B + 1]: its keys, of which the queries are the latest; None: the same.  Calls run on `stream`, or the
+    current stream of the device, and have scratch of their own on every stream and in every graph that torch captures; the object outlives these graphs."""
+
+    def __init__(self, dtype, B_, Hq, Hkv, d, cu_seqlens, cu_k=None, device="cuda"):
+        code, self.query_dtype, self.row_dtype = DTYPES[dtype]
+        self.dtype, self.B, self.Hq, self.Hkv, self.d = dtype, B_, Hq, Hkv, d
+        self.batch = B.PromptBatch(code, B_, Hq, Hkv, d, cu_seqlens, cu_k)
+        self.queries = int(self.batch.cu_q[-1])
+        self.keys = self.queries if cu_k is None else int(self.batch.cu_k[-1])
+        self.workspace_bytes = B.slkv_prompt_workspace_bytes(self.batch)
+        self._set_device(device)
+
+    def _rows(self, t, heads, tokens, tdt, name):
+        if self._tensor(t, (heads, tokens, self.d), tdt, name, contiguous=False).stride(2) != 1:
+            raise ValueError("%s: rows are not contiguous" % name)
+        return t
+
+    def run(self, q, k, v, out=None, lse=None, stream=None):
+        """q [Hq, queries, d], k, v [Hkv, keys, d]: strides of multiples of 16 bytes, rows contiguous (a projection's [tokens, heads, d] is q.transpose(0, 1)).
+        Returns (out [Hq, queries, d], laid out as q is unless it is given, and lse [Hq, queries] fp32)."""
+        self._rows(q, self.Hq, self.queries, self.query_dtype, "q")
+        self._rows(k, self.Hkv, self.keys, self.row_dtype, "k")
+        self._rows(v, self.Hkv, self.keys, self.row_dtype, "v")
+        with self._on(stream):
+            handle = B._stream(None)
+            out = torch.empty_like(q) if out is None else self._rows(out, self.Hq, self.queries, self.query_dtype, "out")
+            if lse is None:
+                lse = torch.empty((self.Hq, self.queries), dtype=torch.float32, device=self.device)
+            else:
+                self._tensor(lse, (self.Hq, self.queries), torch.float32, "lse")
+            B.slkv_attend_prompt(self.batch, q, k, v, out, self._workspace(self.workspace_bytes, handle), lse, handle)
+        return out, lse
+
+
 def score_heads(rows, needle_start, needle_len, topk, acc=None, stream=None):
     """rows: [L,H,T,n] fp32 device tensor.  Returns (acc [L,H,5], scores [L,H,3]) float64 device tensors."""
     L, H, T, n = rows.shape
@@ -156,7 +230,7 @@ def score_heads_qk(q, k, needle_start, needle_len, topk, acc=None, stream=None):
     return acc, scores
 
 
-class Cache:
+class Cache(_OnDevice):
     """One layer's cache for decoding: packed K and V rows in a room per segment (sequence b, KV head h: b * Hkv + h), of which the first
     lengths[s] are in use.
 
@@ -178,10 +252,7 @@ class Cache:
             raise ValueError("keys, values and their scales are given together")
         if k is not None:
             device = k.device
-        self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
-        self._here = contextlib.nullcontext()
+        self._set_device(device)
         if lengths is None:
             lengths = torch.zeros((S,), dtype=torch.int32, device=self.device) if k is None else torch.from_numpy(np.diff(offsets).astype(np.int32)).to(self.device)
         width = d // 2 if four else d
@@ -200,38 +271,15 @@ class Cache:
         self.weight = array(weight, (rows,), torch.float32, "weight", torch.zeros) if weights or weight is not None else None
         self.rows_in_all = rows
         self._arrays = B.CacheTensors(self.k, self.v, self.k_scale, self.v_scale, self.lengths, self.pos, self.weight)
-        self._workspaces, self._attend_like = {}, {}
-
-    def _tensor(self, t, shape, tdt, name, contiguous=True):
-        if t.dtype != tdt or t.shape != shape:
-            raise ValueError("%s: %s of shape %s wanted, got %s of shape %s" % (name, tdt, shape, t.dtype, tuple(t.shape)))
-        if t.device != self.device:
-            raise ValueError("%s is on %s, the cache on %s" % (name, t.device, self.device))
-        if contiguous and not t.is_contiguous():
-            raise ValueError("%s is not contiguous" % name)
-        return t
-
-    def _on(self, stream):
-        """The call's stream as the current one, so that what it allocates belongs to it; without one, the cache's device, where it is not current."""
-        if stream is not None:
-            if stream.device != self.device:
-                raise ValueError("stream is of %s, the cache on %s" % (stream.device, self.device))
-            return torch.cuda.stream(stream)
-        return self._here if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
+        self._attend_like = {}
 
     def _attend_buffers(self, T, weights, stream):
-        """A workspace for a call on the stream of this handle, and a tensor in the shape of its lse.  Calls that follow each other on a stream share one, which grows with
-        the largest of them; a captured call has its own, which stays with its graph: the graph may be replayed anywhere.  (0.2 to 0.4 us of the host; a tensor for every call 0.9.)"""
+        """A workspace for a call on the stream of this handle, and a tensor in the shape of its lse."""
         like = self._attend_like.get((T, weights))
         if like is None:
             like = B.slkv_attend_workspace_bytes(self.layout, T, weights), torch.empty((self.B, self.Hq, T), dtype=torch.float32, device=self.device)
             self._attend_like[T, weights] = like
-        ws = None if torch.cuda.is_current_stream_capturing() else self._workspaces.get(stream, _NOTHING)
-        if ws is None:
-            ws = torch.empty((like[0],), dtype=torch.uint8, device=self.device)
-        elif ws.nbytes < like[0]:
-            ws = self._workspaces[stream] = torch.empty((like[0],), dtype=torch.uint8, device=self.device)
-        return ws, like[1]
+        return self._workspace(like[0], stream), like[1]
 
     def fill(self, k_rows, v_rows, src_offsets, pos=None, stream=None):
         """The rows that a prefill kept (LayerCall's k_out, v_out, offsets, kept_idx) become the cache."""

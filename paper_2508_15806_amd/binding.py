@@ -29,14 +29,14 @@ EXPORTS = ["slkv_status_str", "slkv_last_error", "slkv_version", "slkv_init", "s
            "slkv_compacted_sizes", "slkv_workspace_bytes", "slkv_compress_layer", "slkv_compress_layer_static",
            "slkv_recompress_sizes", "slkv_recompress_workspace_bytes", "slkv_recompress_layer",
            "slkv_fill_cache", "slkv_append_cache", "slkv_cache_rows", "slkv_attend_workspace_bytes", "slkv_attend_cache",
-           "slkv_evict_cache",
+           "slkv_evict_cache", "slkv_prompt_workspace_bytes", "slkv_attend_prompt",
            "slkv_profile_begin", "slkv_profile_end"]
 
 SLKV_ERR_HIP = 7
 SLKV_WORKSPACE_HEADER_BYTES = 65536
 
 KERNEL_NAMES = ["score_stats", "combine", "score_accum", "select", "gather", "row_cells", "head_reduce", "qk_cells",
-                "qk_fallback", "cache_store", "cache_rows", "attend", "attend_join", "evict"]
+                "qk_fallback", "cache_store", "cache_rows", "attend", "attend_join", "evict", "attend_prompt", "attend_tree", "tiles_join", "accept", "weigh"]
 
 
 class SlkvError(RuntimeError):
@@ -82,6 +82,12 @@ class CacheArrays(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("reserved", C.c_uint32),
                 ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
                 ("d_lengths", C.c_void_p), ("d_pos", C.c_void_p), ("d_weight", C.c_void_p)]
+
+
+class PromptDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32),
+                ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("reserved", C.c_int32 * 2),
+                ("h_cu_q", C.c_void_p), ("h_cu_k", C.c_void_p), ("strides", C.c_int64 * 8)]
 
 
 _lib = None
@@ -154,6 +160,10 @@ def lib():
         L.slkv_attend_cache.argtypes = [cd, ca, C.c_int32, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.slkv_evict_cache.restype = C.c_int
         L.slkv_evict_cache.argtypes = [cd, ca, cd, ca, C.c_int32, vp, vp, vp]
+        L.slkv_prompt_workspace_bytes.restype = C.c_int
+        L.slkv_prompt_workspace_bytes.argtypes = [cd, vp]
+        L.slkv_attend_prompt.restype = C.c_int
+        L.slkv_attend_prompt.argtypes = [cd, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.slkv_profile_begin.restype = C.c_int
         L.slkv_profile_begin.argtypes = [C.c_int32]
         L.slkv_profile_end.restype = C.c_int
@@ -401,6 +411,40 @@ def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, kept_idx=None, 
         raise ValueError("w: %d is no 32-bit number" % w)
     _check(lib().slkv_evict_cache(layout.address, cache.address, out_layout.address, out.address, w, budgets.ctypes.data, _ptr(kept_idx),
                                   _stream(stream)))
+
+
+class PromptBatch:
+    """Host-side descriptor of a batch of packed prompts; keeps the numpy arrays it points to alive.  Strides are those of the tensors of a call."""
+
+    def __init__(self, dtype, B, Hq, Hkv, d, cu_q, cu_k=None):
+        self.cu_q = np.array(cu_q, dtype=np.int64)                 # copies: the batch stays what it is
+        self.cu_k = None if cu_k is None else np.array(cu_k, dtype=np.int64)
+        for cu, name in ((self.cu_q, "cu_q"), (self.cu_k, "cu_k")):
+            if cu is not None and cu.shape != (B + 1,):
+                raise ValueError("%s: %d entries wanted, got shape %s" % (name, B + 1, cu.shape))
+        self.desc = PromptDesc(C.sizeof(PromptDesc), int(dtype), B, Hq, Hkv, d, (C.c_int32 * 2)(0, 0), self.cu_q.ctypes.data,
+                               None if cu_k is None else self.cu_k.ctypes.data, (C.c_int64 * 8)(0, 0, 0, 0, 0, 0, d, 0))
+        self.desc.strides[7] = d * max(int(self.cu_q[-1]), 1)      # (of out: [Hq][tokens][d] until a call says otherwise)
+        self.address = C.addressof(self.desc)
+
+    def with_strides(self, *tensors):
+        """This batch with the token and head strides of q, k, v and out [heads, tokens, d]."""
+        desc = PromptDesc.from_buffer_copy(self.desc)
+        desc.strides[:] = [t.stride(i) if t.shape[i] > 1 else 0 for t in tensors for i in (1, 0)]    # (torch leaves anything as the stride of one)
+        return desc
+
+
+def slkv_prompt_workspace_bytes(batch):
+    n = C.c_size_t(0)
+    _check(lib().slkv_prompt_workspace_bytes(batch.address, C.addressof(n)))
+    return int(n.value)
+
+
+def slkv_attend_prompt(batch, q, k, v, out, workspace, lse=None, stream=None):
+    """q, out: [Hq, queries, d]; k, v: [Hkv, tokens, d], of any strides with contiguous rows; lse [Hq, queries] fp32."""
+    desc = batch.with_strides(q, k, v, out)
+    _check(lib().slkv_attend_prompt(C.addressof(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(workspace), workspace.nbytes,
+                                    _stream(stream)))
 
 
 def slkv_profile_begin(max_records):

@@ -1,0 +1,227 @@
+// Causal attention of packed prompts (slkv_attend_prompt): the prefill whose keys and values slkv_compress_layer chooses from.
+#include "attend_tiles.h"
+
+#include <algorithm>
+
+namespace slkv {
+
+// Sequences of a launch, those with the most keys first.  Workgroups: sequence, then tiles of queries from the last one (which has the most keys) down, then parts of
+// the keys, then KV heads, so that with 8 of them a head stays on an XCD and its L2.
+struct PromptTab {
+  static constexpr int kSeqs = 64;
+  const unsigned char *k, *v, *q;
+  unsigned char* out;
+  float* lse;
+  int64_t q_tok, q_head, o_tok, o_head, k_row, v_row, k_head, v_head, lse_head;   // bytes; lse_head: elements
+  int32_t nseq, hkv;
+  int32_t first[kSeqs + 1], q0[kSeqs], nq[kSeqs], k0[kSeqs], nk[kSeqs], parts[kSeqs];
+
+  template <int QUERIES, int KEYS, int D, int KIND>
+  __device__ __forceinline__ TileWork find(const TileArgs& a, int block) const {
+    const int s = find_segment_wave(nseq, block, [&](int i) { return first[i]; });
+    const int i = block - first[s], h = i % hkv, rest = i / hkv;
+    const int parts_here = parts[s], new_tokens = nq[s], keys = nk[s], rows = a.G * new_tokens;
+    const int tiles = (rows + QUERIES - 1) / QUERIES, tile = tiles - 1 - rest / parts_here;
+    TileWork w;
+    w.part = rest % parts_here;
+    w.rows = rows;
+    w.r0 = tile * QUERIES;
+    w.hist = keys - new_tokens;
+    w.n = keys;
+    const int last = (min(w.r0 + QUERIES, rows) - 1) / a.G, end = min(max(w.hist + last + 1, 0), keys);
+    const int steps = (end + KEYS - 1) / KEYS, each = (steps + parts_here - 1) / parts_here * KEYS;
+    w.parts = each ? (end + each - 1) / each : 1;
+    w.begin = w.part * each;
+    w.end = min(end, w.begin + each);
+    w.k = k + h * k_head + k0[s] * k_row;
+    w.v = v + h * v_head + k0[s] * v_row;
+    w.ks = w.vs = nullptr;
+    w.q = q + (int64_t)h * a.G * q_head + q0[s] * q_tok;
+    w.out = out + (int64_t)h * a.G * o_head + q0[s] * o_tok;
+    w.lse = lse ? lse + (int64_t)h * a.G * lse_head + q0[s] : nullptr;
+    w.sees = nullptr;
+    w.q_tok = q_tok, w.q_head = q_head, w.o_tok = o_tok, w.o_head = o_head, w.lse_head = lse_head;
+    w.k_row = k_row, w.v_row = v_row;
+    w.slot0 = first[s] + rest / parts_here * parts_here * hkv + h;
+    w.slot_step = hkv;
+    return w;
+  }
+};
+
+struct PromptPlan {
+  int shape;                         // waves and tiles of a workgroup
+  int queries;                       // rows of a workgroup's tile
+  int64_t each;                      // keys of a part, about
+  int64_t slots;                     // workgroups of a launch, the most
+  bool split;
+  size_t off_ml, bytes;
+};
+
+static int64_t seq_tiles(const slkv_prompt_desc* d, int64_t b, int queries) {
+  return ((d->h_cu_q[b + 1] - d->h_cu_q[b]) * (d->Hq / d->Hkv) + queries - 1) / queries;
+}
+static const int64_t* cu_k_of(const slkv_prompt_desc* d) { return d->h_cu_k ? d->h_cu_k : d->h_cu_q; }
+static int64_t seq_parts(const slkv_prompt_desc* d, int64_t b, int64_t each) {
+  return std::max<int64_t>(1, (cu_k_of(d)[b + 1] - cu_k_of(d)[b] + each - 1) / each);
+}
+
+static PromptPlan plan_prompt(const slkv_prompt_desc* d) {
+  PromptPlan p;
+  const int64_t G = d->Hq / d->Hkv;
+  const int64_t* ck = cu_k_of(d);
+  int64_t rows = 0;
+  for (int64_t b = 0; b < d->B; ++b) rows = std::max(rows, (d->h_cu_q[b + 1] - d->h_cu_q[b]) * G);
+  p.shape = rows <= 32 && d->dtype != SLKV_F32 ? 0 : rows <= 64 ? 1 : 2;
+  p.queries = 32 << p.shape;
+  const int64_t places = 256 * (p.shape == 0 || d->dtype == SLKV_F32 ? 1 : 2);
+  int64_t tiles = 0, keys = 0, most = 0;
+  for (int64_t b = 0; b < d->B; ++b) {
+    const int64_t t = seq_tiles(d, b, p.queries) * d->Hkv, n = d->h_cu_q[b + 1] - d->h_cu_q[b], m = ck[b + 1] - ck[b];
+    tiles += t;
+    keys += t * std::max<int64_t>(1, m - n / 2);
+    if (t) most = std::max(most, m);
+  }
+  p.each = std::max<int64_t>(1, most);
+  if (tiles < places) p.each = std::max<int64_t>(256, (keys + places - 1) / places);
+  p.split = most > p.each;
+  p.slots = 0;
+  for (int64_t b0 = 0; b0 < d->B; b0 += PromptTab::kSeqs) {
+    int64_t here = 0;
+    for (int64_t b = b0; b < std::min<int64_t>(d->B, b0 + PromptTab::kSeqs); ++b) here += seq_tiles(d, b, p.queries) * d->Hkv * seq_parts(d, b, p.each);
+    p.slots = std::max(p.slots, here);
+  }
+  const size_t o = p.split ? (size_t)p.slots * p.queries * d->d * sizeof(float) : 0;
+  p.off_ml = o;
+  p.bytes = std::max<size_t>(16, o + (p.split ? (size_t)p.slots * p.queries * 2 * sizeof(float) : 0));
+  return p;
+}
+
+static slkv_status prompt_checks(const slkv_prompt_desc* d) {
+  if (!d) return fail(SLKV_ERR_NULL, "desc is NULL");
+  if (d->struct_size != sizeof(slkv_prompt_desc)) return fail(SLKV_ERR_BAD_ARG, "desc.struct_size %u != %zu", d->struct_size, sizeof(slkv_prompt_desc));
+  if (d->dtype < SLKV_F32 || d->dtype > SLKV_BF16_KV_MXFP4) return fail(SLKV_ERR_BAD_ARG, "unknown dtype %d", d->dtype);
+  if (d->dtype == SLKV_BF16_KV_MXFP4) return fail(SLKV_ERR_UNSUPPORTED, "prompts have no MXFP4 keys and values");
+  if (d->B < 1 || d->Hq < 1 || d->Hkv < 1) return fail(SLKV_ERR_BAD_ARG, "B, Hq, Hkv must be >= 1");
+  if (d->B > (1 << 20) || d->Hkv > (1 << 16) || d->Hq > (1 << 16)) return fail(SLKV_ERR_BAD_ARG, "B, Hq or Hkv too large");
+  if (d->Hq % d->Hkv) return fail(SLKV_ERR_BAD_ARG, "Hq %% Hkv != 0");
+  if (d->d != 64 && d->d != 128) return fail(SLKV_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", d->d);
+  if (d->reserved[0] || d->reserved[1]) return fail(SLKV_ERR_BAD_ARG, "desc.reserved must be 0");
+  slkv_status st = validate_offsets(d->h_cu_q, d->B, "h_cu_q");
+  if (st != SLKV_OK) return st;
+  if (d->h_cu_k && (st = validate_offsets(d->h_cu_k, d->B, "h_cu_k")) != SLKV_OK) return st;
+  const int wide = wide_bytes(d->dtype), narrow = d->dtype == SLKV_BF16_KV_FP8 ? 1 : wide;
+  const int64_t strides[] = {d->q_stride_tok, d->q_stride_head, d->out_stride_tok, d->out_stride_head, d->k_stride_tok, d->k_stride_head, d->v_stride_tok, d->v_stride_head};
+  for (int i = 0; i < 8; ++i) {
+    const int elt = i < 4 ? wide : narrow;
+    if (strides[i] < 0 || strides[i] > (int64_t(1) << 40) || strides[i] * elt % 16) return fail(SLKV_ERR_BAD_ARG, "stride %lld not a non-negative multiple of 16 bytes", (long long)strides[i]);
+    if ((i == 4 || i == 6) && strides[i] * elt >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "token stride %lld of keys or values: 2^24 bytes and more", (long long)strides[i]);
+  }
+  const int64_t n = d->h_cu_q[d->B] - d->h_cu_q[0];
+  const bool by_head = (n < 2 || d->out_stride_tok >= d->d) && (d->Hq < 2 || d->out_stride_head >= (n - 1) * d->out_stride_tok + d->d);
+  const bool by_token = (d->Hq < 2 || d->out_stride_head >= d->d) && (n < 2 || d->out_stride_tok >= (d->Hq - 1) * d->out_stride_head + d->d);
+  if (n && !by_head && !by_token) return fail(SLKV_ERR_BAD_ARG, "out: rows overlap");
+  const int64_t G = d->Hq / d->Hkv;
+  for (int64_t b = 0; b < d->B; ++b)
+    if ((d->h_cu_q[b + 1] - d->h_cu_q[b]) * G >= (int64_t(1) << 31) - 512) return fail(SLKV_ERR_UNSUPPORTED, "sequence %lld: 2^31 - 512 query rows of a KV head and more", (long long)b);
+  if (plan_prompt(d).slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
+  return SLKV_OK;
+}
+
+}  // namespace slkv
+
+using namespace slkv;
+
+extern "C" slkv_status slkv_prompt_workspace_bytes(const slkv_prompt_desc* desc, size_t* bytes) {
+  clear_error();
+  if (!bytes) return fail(SLKV_ERR_NULL, "bytes is NULL");
+  const slkv_status st = prompt_checks(desc);
+  if (st != SLKV_OK) return st;
+  *bytes = plan_prompt(desc).bytes;
+  return SLKV_OK;
+}
+
+extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const void* d_q, const void* d_k, const void* d_v, void* d_out, float* d_lse,
+                                          void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  clear_error();
+  const slkv_status st = prompt_checks(desc);
+  if (st != SLKV_OK) return st;
+  const int64_t* ck = cu_k_of(desc);
+  const int64_t queries = desc->h_cu_q[desc->B] - desc->h_cu_q[0], keys = ck[desc->B] - ck[0];
+  if (!d_workspace || (queries && (!d_q || !d_out)) || (keys && (!d_k || !d_v))) return fail(SLKV_ERR_NULL, "a required device pointer is NULL");
+  const void* ptrs[] = {d_q, d_k, d_v, d_out, d_lse, d_workspace};
+  for (const void* ptr : ptrs)
+    if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);
+  const PromptPlan p = plan_prompt(desc);
+  if (workspace_bytes < p.bytes) return fail(SLKV_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, p.bytes);
+  const int wide = wide_bytes(desc->dtype), narrow = desc->dtype == SLKV_BF16_KV_FP8 ? 1 : wide;
+  TileArgs a;
+  a.G = desc->Hq / desc->Hkv;
+  a.T = 0;
+  a.c_log2 = kTileLog2e / std::sqrt((float)desc->d);
+  a.part_o = (float*)d_workspace;
+  a.part_ml = (float*)((unsigned char*)d_workspace + p.off_ml);
+  hipStream_t const stream = (hipStream_t)hip_stream;
+  for (int64_t b0 = 0; b0 < desc->B; b0 += PromptTab::kSeqs) {
+    PromptTab t;
+    t.k = (const unsigned char*)d_k, t.v = (const unsigned char*)d_v, t.q = (const unsigned char*)d_q;
+    t.out = (unsigned char*)d_out;
+    t.lse = d_lse;
+    t.q_tok = desc->q_stride_tok * wide, t.q_head = desc->q_stride_head * wide;
+    t.o_tok = desc->out_stride_tok * wide, t.o_head = desc->out_stride_head * wide;
+    t.k_row = desc->k_stride_tok * narrow, t.k_head = desc->k_stride_head * narrow;
+    t.v_row = desc->v_stride_tok * narrow, t.v_head = desc->v_stride_head * narrow;
+    t.lse_head = desc->h_cu_q[desc->B];
+    t.hkv = desc->Hkv;
+    t.nseq = (int32_t)std::min<int64_t>(PromptTab::kSeqs, desc->B - b0);
+    int order[PromptTab::kSeqs];
+    for (int i = 0; i < t.nseq; ++i) order[i] = i;
+    std::sort(order, order + t.nseq, [&](int x, int y) {
+      const int64_t kx = ck[b0 + x + 1] - ck[b0 + x], ky = ck[b0 + y + 1] - ck[b0 + y];
+      return kx != ky ? kx > ky : x < y;
+    });
+    int64_t blocks = 0;
+    for (int i = 0; i < t.nseq; ++i) {
+      const int64_t b = b0 + order[i];
+      t.first[i] = (int32_t)blocks;
+      t.q0[i] = (int32_t)desc->h_cu_q[b], t.nq[i] = (int32_t)(desc->h_cu_q[b + 1] - desc->h_cu_q[b]);
+      t.k0[i] = (int32_t)ck[b], t.nk[i] = (int32_t)(ck[b + 1] - ck[b]);
+      t.parts[i] = (int32_t)seq_parts(desc, b, p.each);
+      blocks += seq_tiles(desc, b, p.queries) * desc->Hkv * t.parts[i];
+    }
+    t.first[t.nseq] = (int32_t)blocks;
+    if (!blocks) continue;
+    auto launch = [&](auto kind, auto dim, auto qt, auto wq, auto wk) {
+      constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value, kQT = decltype(qt)::value, kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
+      {
+        ScopedKernelTimer timer(SLKV_K_PROMPT);
+        SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kQT, kWQ, kWK, PromptTab>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+      }
+      if (p.split) {
+        ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
+        SLKV_LAUNCH((join_tiles_kernel<kKind, kDim, kQT, kWQ, kWK, PromptTab>), dim3((unsigned)blocks), dim3(256), 0, stream, a, t);
+      }
+    };
+    auto with_shape = [&](auto kind, auto dim) {
+      using std::integral_constant;
+      integral_constant<int, 1> one;
+      integral_constant<int, 2> two;
+      integral_constant<int, 4> four;
+      if constexpr (decltype(kind)::value != SLKV_F32) {
+        if (p.shape == 0) return launch(kind, dim, one, one, four);
+      }
+      if (p.shape == 1) return launch(kind, dim, one, two, two);
+      launch(kind, dim, one, four, one);
+    };
+    auto with_dim = [&](auto kind) {
+      if (desc->d == 64) with_shape(kind, std::integral_constant<int, 64>{});
+      else with_shape(kind, std::integral_constant<int, 128>{});
+    };
+    switch (desc->dtype) {
+      case SLKV_F32: with_dim(std::integral_constant<int, SLKV_F32>{}); break;
+      case SLKV_BF16: with_dim(std::integral_constant<int, SLKV_BF16>{}); break;
+      case SLKV_F16: with_dim(std::integral_constant<int, SLKV_F16>{}); break;
+      default: with_dim(std::integral_constant<int, SLKV_BF16_KV_FP8>{});
+    }
+  }
+  return launch_status("attend_prompt");
+}
