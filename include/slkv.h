@@ -412,6 +412,31 @@ slkv_status slkv_attend_cache(const slkv_cache_desc* desc, const slkv_cache* cac
 slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cache, const slkv_cache_desc* out_desc, const slkv_cache* out,
                              int32_t w, const int32_t* h_budgets, int32_t* d_kept_idx, void* hip_stream);
 
+/* Attention of T drafted tokens, the nodes of a tree (or several), over the rows in use, the last T of which are theirs: row n_s - T + u is drafted token u's.  Drafted
+ * token t of sequence b sees all rows before the draft, and drafted token u's row exactly if bit u of d_sees[b][t] is set (bits from T on mean nothing); rows that are not there
+ * (n_s < T) are seen by none.  lse and out as in slkv_attend_cache, of the rows that the token sees; the rest of what is said there holds, but for weights: they enter the
+ * product with v rounded to the type of the queries as in slkv_attend_prompt, and none are added up (slkv_accept_cache does that for the tokens that turn out to be right).
+ * d_q, d_out [B][Hq][T][d];  d_sees [B][T] 64-bit numbers;  1 <= T <= 64, any Hq/Hkv;  d_lse [B][Hq][T] fp32, may be NULL
+ * Workspace: as for slkv_attend_cache, of slkv_tree_workspace_bytes.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED (T), WORKSPACE, HIP. */
+slkv_status slkv_tree_workspace_bytes(const slkv_cache_desc* desc, int32_t T, size_t* bytes);
+slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, const void* d_q, const uint64_t* d_sees,
+                             void* d_out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* What a verification leaves of a draft of T tokens whose rows stand behind the rows before it: the accepted ones move together and the others leave.
+ * d_path [B][A] int32: the accepted tokens of every sequence in their new order, up to the first number outside 0 .. T-1 (or all A); the same number twice is a row twice.  Drafted
+ *   token u's row of segment s is base_s + u, with base_s = d_at[s] if d_at is given (it may be d_lengths itself), otherwise n_s - T.  Tokens whose row is not there (below 0, or
+ *   beyond the room) are left out in that segment.
+ * The i-th accepted token's row (K, V, scales, position, weight) goes to row max(base_s, 0) + i, and d_lengths[s] becomes max(base_s, 0) + their number.  Rows behind these stay as they are.
+ * d_q [B][Hq][T][d], d_lse [B][Hq][T]: the drafted tokens' queries and what slkv_attend_tree gave for them; with them, for the new rows in use j,
+ *   weight_out[j] = weight[j] + sum over the segment's query heads and the accepted tokens i that see j (j <= max(base_s, 0) + i) of exp(q_i . k_j / sqrt(d) - lse_i)
+ *   (a token whose lse is -infinity adds nothing): the weights that slkv_attend_cache would have added, for slkv_evict_cache to rank by.
+ * d_weight_out [rows] fp32; may be cache->d_weight itself.  d_q, d_lse and d_weight_out are given together, or all NULL.  cache->d_weight NULL: sums begin at 0.
+ * 1 <= T, A <= 64.  cache->d_lengths is required.  The result has the same bits every time.
+ * Errors: NULL, BAD_ARG, UNSUPPORTED (T, A, Hq/Hkv > 2^14), HIP. */
+slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, int32_t A, const int32_t* d_path, const int32_t* d_at,
+                              const void* d_q, const float* d_lse, float* d_weight_out, void* hip_stream);
+
 /* ------------------------------------------------------------------ attention of a prompt
  * Causal attention of a ragged batch of packed prompts, or of their next pieces behind a history: what makes the outputs of the layer whose K and V
  * slkv_compress_layer then chooses from.  Sequence b has n_b = h_cu_q[b+1] - h_cu_q[b] queries, those of the last n_b of its m_b = h_cu_k[b+1] - h_cu_k[b]
@@ -475,8 +500,7 @@ typedef enum {
   SLKV_K_PROMPT = 14,       /* attention of packed prompts */
   SLKV_K_TREE = 15,         /* attention of a tree of drafted tokens over a cache */
   SLKV_K_TILES_JOIN = 16,   /* the parts of either put together */
-  SLKV_K_ACCEPT = 17,       /* accepted rows moved, lengths set */
-  SLKV_K_WEIGH = 18         /* weights of the accepted tokens' attention */
+  SLKV_K_ACCEPT = 17        /* accepted rows moved, weights of the accepted tokens' attention; lengths (a record of its own with weights) */
 } slkv_kernel_id;
 typedef struct {
   int32_t kernel; /* slkv_kernel_id */

@@ -92,6 +92,47 @@ def attend(q, k, v, offsets, lengths, Hkv, T, weight=None):
     return out, lse, weight, terms, spread
 
 
+def attend_tree(q, k, v, offsets, lengths, Hkv, sees):
+    """q [B][Hq][T][d]: drafted tokens, whose rows are the last T of every segment; sees [B][T][T] truth values: token t sees token u's row.  Returns out, lse, terms,
+    spread as attend()."""
+    q = np.asarray(q, np.float64)
+    B, Hq, T, d = q.shape
+    G = Hq // Hkv
+    out, lse = np.zeros(q.shape), np.full(q.shape[:3], -np.inf)
+    terms, spread = np.zeros(q.shape[:3]), np.zeros(q.shape)
+    with np.errstate(invalid="ignore", over="ignore"):
+        for b in range(B):
+            for hq in range(Hq):
+                s = b * Hkv + hq // G
+                a, n = int(offsets[s]), int(lengths[s])
+                for t in range(T):
+                    rows = [a + j for j in range(n) if j < n - T or sees[b][t][j - (n - T)]]
+                    if not rows:
+                        continue
+                    kk, vv = k[rows], v[rows]
+                    x = kk @ q[b, hq, t] / np.sqrt(d)
+                    top = x.max()
+                    p = np.exp(x - top)
+                    lse[b, hq, t] = top + np.log(p.sum())
+                    p = p / p.sum()
+                    out[b, hq, t] = (p[:, None] * vv).sum(0)
+                    t_all = np.abs(kk) @ np.abs(q[b, hq, t])
+                    terms[b, hq, t] = t_all[np.isfinite(t_all)].max(initial=0.0) / np.sqrt(d)
+                    spread[b, hq, t] = p @ np.abs(vv)
+    return out, lse, terms, spread
+
+
+def accept_segment(path, T, base, room):
+    """(rows that the accepted ones come from, row that the first goes to) of a draft whose token u has row base + u."""
+    rows = []
+    for p in path:
+        if not 0 <= p < T:
+            break
+        if 0 <= base + p < room:
+            rows.append(base + int(p))
+    return rows, max(base, 0)
+
+
 def evict_segment(weight, w, cap):
     """Row numbers that stay of a segment with these weights: the max(cap, w) - w largest of all but the last w (equal ones: the lower row; NaN
     above all numbers), ascending, then the last w."""

@@ -230,6 +230,20 @@ def score_heads_qk(q, k, needle_start, needle_len, topk, acc=None, stream=None):
     return acc, scores
 
 
+def tree_bits(parents):
+    """parents [.., T] whole numbers on the host: the parent of every drafted token, an earlier one, or -1 for a root.  Returns [.., T] int64 for Cache.attend_tree (to be
+    copied to the device): the bits of a token's ancestors and its own."""
+    parents = np.asarray(parents)
+    T = parents.shape[-1]
+    if T > 64 or not np.issubdtype(parents.dtype, np.integer) or (parents < -1).any() or (parents >= np.arange(T)).any():
+        raise ValueError("parents: at most 64 whole numbers, each -1 or that of an earlier token, wanted")
+    bits = np.zeros(parents.shape, dtype=np.uint64)
+    for t in range(T):
+        up = np.take_along_axis(bits, np.maximum(parents[..., t:t + 1], 0).astype(np.int64), -1)[..., 0]
+        bits[..., t] = np.where(parents[..., t] >= 0, up, np.uint64(0)) | np.uint64(1 << t)
+    return torch.from_numpy(bits.view(np.int64))
+
+
 class Cache(_OnDevice):
     """One layer's cache for decoding: packed K and V rows in a room per segment (sequence b, KV head h: b * Hkv + h), of which the first
     lengths[s] are in use.
@@ -271,7 +285,7 @@ class Cache(_OnDevice):
         self.weight = array(weight, (rows,), torch.float32, "weight", torch.zeros) if weights or weight is not None else None
         self.rows_in_all = rows
         self._arrays = B.CacheTensors(self.k, self.v, self.k_scale, self.v_scale, self.lengths, self.pos, self.weight)
-        self._attend_like = {}
+        self._attend_like, self._tree_bytes = {}, {}
 
     def _attend_buffers(self, T, weights, stream):
         """A workspace for a call on the stream of this handle, and a tensor in the shape of its lse."""
@@ -328,6 +342,48 @@ class Cache(_OnDevice):
             lse = torch.empty_like(lse_like) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
             B.slkv_attend_cache(self.layout, self._arrays, q, out, ws, lse, weight, handle)
         return out, lse
+
+    def attend_tree(self, q, sees, out=None, lse=None, stream=None):
+        """q [B, Hq, T, d]: the queries of T <= 64 drafted tokens, whose rows are the last T in the cache.  sees [B, T] int64: token t sees the rows before the draft and
+        those drafted tokens u for which bit u of sees[b, t] is set (its ancestors and itself, as tree_bits gives them).  Returns (out [B, Hq, T, d], lse [B, Hq, T] fp32)."""
+        if q.dim() != 4:
+            raise ValueError("q: four dimensions wanted, got shape %s" % (tuple(q.shape),))
+        T = q.shape[2]
+        shape = (self.B, self.Hq, T, self.d)
+        self._tensor(q, shape, self.query_dtype, "q")
+        self._tensor(sees, (self.B, T), torch.int64, "sees")
+        with self._on(stream):
+            handle = B._stream(None)
+            need = self._tree_bytes.get(T)
+            if need is None:
+                need = self._tree_bytes[T] = B.slkv_tree_workspace_bytes(self.layout, T)
+            out = torch.empty_like(q) if out is None else self._tensor(out, shape, self.query_dtype, "out")
+            lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
+            B.slkv_attend_tree(self.layout, self._arrays, q, sees, out, self._workspace(need, handle), lse, handle)
+        return out, lse
+
+    def accept(self, path, T, at=None, q=None, lse=None, weight=None, stream=None):
+        """What a verification leaves of T drafted tokens, whose rows are the last T in the cache, or those behind the first at[s] (at [B * Hkv] int32): path [B, A] int32 has the
+        accepted ones of every sequence in their new order, ending at the first number outside 0..T-1; their rows move together, the others leave.
+        q [B, Hq, T, d], lse [B, Hq, T]: the draft's queries and what attend_tree() returned for them; the accepted tokens' weights are then added up as attend() adds
+        them.  weight: where the cache's weights plus these go; None: the cache's own array."""
+        if not 1 <= T <= 64:
+            raise ValueError("T: 1 to 64 drafted tokens, got %d" % T)
+        if path.dim() != 2:
+            raise ValueError("path: two dimensions wanted, got shape %s" % (tuple(path.shape),))
+        self._tensor(path, (self.B, path.shape[1]), torch.int32, "path")
+        if at is not None:
+            self._tensor(at, (self.B * self.Hkv,), torch.int32, "at")
+        if (q is None) != (lse is None) or (q is None and weight is not None):
+            raise ValueError("q and lse are given together, and weight with them alone")
+        if q is not None:
+            self._tensor(q, (self.B, self.Hq, T, self.d), self.query_dtype, "q")
+            self._tensor(lse, (self.B, self.Hq, T), torch.float32, "lse")
+            weight = self.weight if weight is None else self._tensor(weight, (self.rows_in_all,), torch.float32, "weight")
+            if weight is None:
+                raise ValueError("the cache has no weights")
+        with self._on(stream):
+            B.slkv_accept_cache(self.layout, self._arrays, T, path, at, q, lse, weight)
 
     def rows(self, out_offsets, stream=None):
         """Every segment's latest out_offsets[s + 1] - out_offsets[s] rows as values: (k, v [rows, d], pos [rows] or None).  Output rows that have no

@@ -30,13 +30,14 @@ EXPORTS = ["slkv_status_str", "slkv_last_error", "slkv_version", "slkv_init", "s
            "slkv_recompress_sizes", "slkv_recompress_workspace_bytes", "slkv_recompress_layer",
            "slkv_fill_cache", "slkv_append_cache", "slkv_cache_rows", "slkv_attend_workspace_bytes", "slkv_attend_cache",
            "slkv_evict_cache", "slkv_prompt_workspace_bytes", "slkv_attend_prompt",
+           "slkv_tree_workspace_bytes", "slkv_attend_tree", "slkv_accept_cache",
            "slkv_profile_begin", "slkv_profile_end"]
 
 SLKV_ERR_HIP = 7
 SLKV_WORKSPACE_HEADER_BYTES = 65536
 
 KERNEL_NAMES = ["score_stats", "combine", "score_accum", "select", "gather", "row_cells", "head_reduce", "qk_cells",
-                "qk_fallback", "cache_store", "cache_rows", "attend", "attend_join", "evict", "attend_prompt", "attend_tree", "tiles_join", "accept", "weigh"]
+                "qk_fallback", "cache_store", "cache_rows", "attend", "attend_join", "evict", "attend_prompt", "attend_tree", "tiles_join", "accept"]
 
 
 class SlkvError(RuntimeError):
@@ -160,6 +161,12 @@ def lib():
         L.slkv_attend_cache.argtypes = [cd, ca, C.c_int32, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.slkv_evict_cache.restype = C.c_int
         L.slkv_evict_cache.argtypes = [cd, ca, cd, ca, C.c_int32, vp, vp, vp]
+        L.slkv_tree_workspace_bytes.restype = C.c_int
+        L.slkv_tree_workspace_bytes.argtypes = [cd, C.c_int32, vp]
+        L.slkv_attend_tree.restype = C.c_int
+        L.slkv_attend_tree.argtypes = [cd, ca, C.c_int32, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.slkv_accept_cache.restype = C.c_int
+        L.slkv_accept_cache.argtypes = [cd, ca, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp]
         L.slkv_prompt_workspace_bytes.restype = C.c_int
         L.slkv_prompt_workspace_bytes.argtypes = [cd, vp]
         L.slkv_attend_prompt.restype = C.c_int
@@ -411,6 +418,23 @@ def slkv_evict_cache(layout, cache, out_layout, out, w, budgets, kept_idx=None, 
         raise ValueError("w: %d is no 32-bit number" % w)
     _check(lib().slkv_evict_cache(layout.address, cache.address, out_layout.address, out.address, w, budgets.ctypes.data, _ptr(kept_idx),
                                   _stream(stream)))
+
+
+def slkv_tree_workspace_bytes(layout, T):
+    n = C.c_size_t(0)
+    _check(lib().slkv_tree_workspace_bytes(layout.address, T, C.addressof(n)))
+    return int(n.value)
+
+
+def slkv_attend_tree(layout, cache, q, sees, out, workspace, lse=None, stream=None):
+    """q, out: [B, Hq, T, d]; sees [B, T] int64 (64 bits); lse [B, Hq, T] fp32."""
+    _check(lib().slkv_attend_tree(layout.address, cache.address, q.shape[2], _ptr(q), _ptr(sees), _ptr(out), _ptr(lse), _ptr(workspace),
+                                  workspace.nbytes, _stream(stream)))
+
+
+def slkv_accept_cache(layout, cache, T, path, at=None, q=None, lse=None, weight_out=None, stream=None):
+    """path [B, A], at [B * Hkv] int32; q [B, Hq, T, d]; lse [B, Hq, T], weight_out [rows] fp32 device tensors or None."""
+    _check(lib().slkv_accept_cache(layout.address, cache.address, T, path.shape[1], _ptr(path), _ptr(at), _ptr(q), _ptr(lse), _ptr(weight_out), _stream(stream)))
 
 
 class PromptBatch:

@@ -13,8 +13,7 @@
 #ifndef SLKV_ATTEND_TILES_H
 #define SLKV_ATTEND_TILES_H
 
-#include "cache.h"
-#include "device_utils.h"
+#include "attend_rows.h"
 #include "launch.h"
 
 #include <cmath>
@@ -23,10 +22,7 @@ namespace slkv {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kTileLog2e = 1.4426950408889634f, kTileLn2 = 0.6931471805599453f;
 constexpr int kTileWaves = 4;
 
 // Segment and tile of a workgroup; the same in all its lanes.
@@ -53,20 +49,15 @@ struct TileArgs {
   float* part_ml;                         // [slot][tile row][2]: reference (log2), sum
 };
 
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// x / y for 0 <= x < 2^21, y > 0: (x + 1/2) / y is at least 1 / (2 y) from a whole number, and what reciprocal and product are off by, 2^-22 of it, is less.
-__device__ __forceinline__ int small_quotient(int x, int y) { return (int)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)y)); }
-
 // 16 bytes per lane from base + off into LDS at lds (the same for the whole wave) + 16 * lane.  The caller waits for it (vmcnt); the compiler does not know of it.
 __device__ __forceinline__ void stage16(const unsigned char* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 template <class T>
-__device__ __forceinline__ T lds_at(uint32_t at) { return *(const __attribute__((address_space(3))) T*)at; }
+__device__ __forceinline__ T lds_at(uint32_t at) { return *(const __attribute__((address_space(3))) T*)(uintptr_t)at; }
 template <class T>
-__device__ __forceinline__ void lds_put(uint32_t at, T v) { *(__attribute__((address_space(3))) T*)at = v; }
+__device__ __forceinline__ void lds_put(uint32_t at, T v) { *(__attribute__((address_space(3))) T*)(uintptr_t)at = v; }
 
 template <int KIND, int D, int QT, int WQ, int WK>
 struct Tiles {
@@ -181,7 +172,7 @@ struct Tiles {
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
   }
   static __device__ __forceinline__ u32x2 read_turned(uint32_t at) {
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
   }
   // element of V of a staged row
   static __device__ __forceinline__ float value(uint32_t vt, int row, int dim) {
@@ -292,13 +283,6 @@ struct Tiles {
   }
 };
 
-template <int KIND>
-__device__ __forceinline__ void store4(unsigned char* dst, f32x4 o) {   // four neighbouring outputs
-  if constexpr (KIND == SLKV_F32) *(f32x4*)dst = o;
-  else if constexpr (KIND == SLKV_F16) *(f16x4*)dst = __builtin_convertvector(o, f16x4);
-  else *(bf16x4*)dst = __builtin_convertvector(o, bf16x4);
-}
-
 // Whether nothing is seen by token t.  (A tree's token that sees nothing of the draft sees what is before it.)
 __device__ __forceinline__ uint64_t bits_of(const TileWork& w, int t, int T) {
   return w.sees ? w.sees[t] & (T < 64 ? (1ull << T) - 1 : ~0ull) : 0ull;
@@ -310,10 +294,13 @@ __device__ __forceinline__ bool sees_none(const TileWork& w, int t, uint64_t bit
   return w.hist <= -64 || (bits >> -w.hist) == 0;
 }
 
+// The lowest n bits, for any n.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // What a query gets of its reference and its sum: the log-sum-exp, and the outputs' factor.
 template <class A>
 __device__ __forceinline__ float tile_lse(float top, float total, bool none) {
-  return none ? -INFINITY : total > 0.f ? ((top + A::kBelow) + __builtin_amdgcn_logf(total * A::kBelowPower)) * kTileLn2 : NAN;
+  return none ? -INFINITY : total > 0.f ? ((top + A::kBelow) + __builtin_amdgcn_logf(total * A::kBelowPower)) * kLn2 : NAN;
 }
 __device__ __forceinline__ f32x4 tile_output(f32x4 o, float total, bool none) {
   const float inv = 1.f / total;
@@ -343,7 +330,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const int r = min(first + qt * 32 + l32, w.rows - 1 - w.r0);
-    const int dt = small_quotient(rem0 + max(r, 0), a.G), head = rem0 + max(r, 0) - dt * a.G;
+    const int dt = divide(rem0 + max(r, 0), a.G), head = rem0 + max(r, 0) - dt * a.G;
     t_of[qt] = t0 + dt;
     bits[qt] = bits_of(w, t_of[qt], a.T);
     const unsigned char* p = w.q + t_of[qt] * w.q_tok + head * w.q_head;
@@ -362,10 +349,14 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
   }
   // keys that every query of the tile sees
   const int all = w.sees ? w.hist : w.hist + t0 + 1;
-  auto sees = [&](int qt, int key) __attribute__((always_inline)) {
-    if (!w.sees) return key <= w.hist + t_of[qt];
-    const int u = key - w.hist;
-    return u < 0 || (u < 64 && (bits[qt] >> u & 1));
+  // bit j: the lane's query sees the key key0 + j, which is there
+  auto seen = [&](int qt, int key0) __attribute__((always_inline)) {
+    uint32_t m = first_bits((w.sees ? w.hist : w.hist + t_of[qt] + 1) - key0);
+    if (w.sees) {
+      const int u = key0 - w.hist;                     // the draft's first row is bit -u
+      m |= u >= 64 || u <= -32 ? 0u : u >= 0 ? (uint32_t)(bits[qt] >> u) : (uint32_t)bits[qt] << -u;
+    }
+    return m & first_bits(w.end - key0);
   };
 
   auto step = [&](int key0, uint32_t buf) __attribute__((always_inline)) {
@@ -378,12 +369,11 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
 #pragma unroll
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
+        for (int qt = 0; qt < QT; ++qt) {
+          const uint32_t m = seen(qt, mine + s * 32) >> (4 * g);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = mine + s * 32 + i / 4 * 8 + 4 * g + i % 4;
-            if (key >= w.end || !sees(qt, key)) x[s][qt][i] = -INFINITY;
-          }
+          for (int i = 0; i < 16; ++i) x[s][qt][i] = m & 1u << (i / 4 * 8 + i % 4) ? x[s][qt][i] : -INFINITY;
+        }
     }
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
@@ -396,7 +386,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
       if (__ballot(top > ref[qt] + A::kAbove)) {
         top = fmaxf(top, __shfl_xor(top, 32));
         const float now = fmaxf(ref[qt], top - A::kBelow);
-        const float f = ref[qt] == -INFINITY ? 0.f : exp2_of(ref[qt] - now);
+        const float f = ref[qt] == -INFINITY ? 0.f : exp2_fast(ref[qt] - now);
         // (sums of a NaN stay one)
         sum[qt] *= f;
 #pragma unroll
@@ -409,7 +399,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          x[s][qt][i] = exp2_of(fmaf(x[s][qt][i], a.c_log2, -from));
+          x[s][qt][i] = exp2_fast(fmaf(x[s][qt][i], a.c_log2, -from));
           sum[qt] += x[s][qt][i];
         }
     }
@@ -418,9 +408,10 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
       const uint32_t vs = vt + s * 32 * A::kRow;
       if (tail && A::any_not_finite(vs, lane)) {
         // a row at a time, to the queries that see it: an infinity or NaN reaches no other through a weight of 0
+        uint32_t m[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) m[qt] = seen(qt, mine + s * 32);
         for (int row = 0; row < 32; ++row) {
-          const int key = mine + s * 32 + row;
-          if (key >= w.end) break;
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
             float p = 0.f;
@@ -428,7 +419,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
             for (int i = 0; i < 16; ++i)
               if (i == row / 8 * 4 + row % 4) p = x[s][qt][i];
             p = __shfl(p, (row / 4 & 1) * 32 + l32);
-            if (sees(qt, key)) {
+            if (m[qt] >> row & 1) {
 #pragma unroll
               for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
@@ -491,7 +482,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
 #pragma unroll
       for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_m[i][wq * 32 + l32]);
       // (a wave that saw nothing has a sum of 0, or NaN where a product was NaN)
-      f = ref[qt] == -INFINITY ? 1.f : exp2_of(ref[qt] - top);
+      f = ref[qt] == -INFINITY ? 1.f : exp2_fast(ref[qt] - top);
     }
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt)
@@ -513,11 +504,11 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
         top = fmaxf(top, sh_m[i][row]);
       }
 #pragma unroll
-      for (int i = 0; i < WK; ++i) l += sh_l[i][row] * (WK == 1 || sh_m[i][row] == -INFINITY ? 1.f : exp2_of(sh_m[i][row] - top));
+      for (int i = 0; i < WK; ++i) l += sh_l[i][row] * (WK == 1 || sh_m[i][row] == -INFINITY ? 1.f : exp2_fast(sh_m[i][row] - top));
       if (whole) {
-        const int dt = small_quotient(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
+        const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
         const bool none = sees_none(w, t, bits_of(w, t, a.T));
-        store4<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
+        store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
         if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
       } else {
         *(f32x4*)(a.part_o + ((int64_t)slot * A::kQueries + r) * D + d0) = o;
@@ -542,13 +533,13 @@ __global__ __launch_bounds__(256) void join_tiles_kernel(const TileArgs a, const
     for (int p = 0; p < w.parts; ++p) {
       const int64_t at = (int64_t)(w.slot0 + p * w.slot_step) * A::kQueries + r;
       const f32x2 ml = *(const f32x2*)(a.part_ml + at * 2);
-      const float f = ml[0] == -INFINITY ? 1.f : exp2_of(ml[0] - top);
+      const float f = ml[0] == -INFINITY ? 1.f : exp2_fast(ml[0] - top);
       l += ml[1] * f;
       o += *(const f32x4*)(a.part_o + at * D + d0) * f;
     }
-    const int dt = small_quotient(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
+    const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
     const bool none = sees_none(w, t, bits_of(w, t, a.T));
-    store4<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
+    store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
     if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
   }
 }

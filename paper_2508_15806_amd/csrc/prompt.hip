@@ -157,7 +157,7 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
   TileArgs a;
   a.G = desc->Hq / desc->Hkv;
   a.T = 0;
-  a.c_log2 = kTileLog2e / std::sqrt((float)desc->d);
+  a.c_log2 = kLog2e / std::sqrt((float)desc->d);
   a.part_o = (float*)d_workspace;
   a.part_ml = (float*)((unsigned char*)d_workspace + p.off_ml);
   hipStream_t const stream = (hipStream_t)hip_stream;

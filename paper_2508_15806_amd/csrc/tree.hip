@@ -1,0 +1,182 @@
+// Attention of a tree of drafted tokens over a cache (slkv_attend_tree), and what becomes of the draft (slkv_accept_cache).
+#include "attend_tiles.h"
+
+#include <algorithm>
+#include <limits>
+
+namespace slkv {
+
+// ------------------------------------------------------------------ attention
+
+// Segments of a launch: first rows of their rooms, workgroups before them.  Workgroups of a segment: parts of its rows, in each of them the tiles of queries.
+template <int N>
+struct TreeTab {
+  static constexpr int kSegs = N;
+  const unsigned char *k, *v, *k_scale, *v_scale, *q;
+  unsigned char* out;
+  float* lse;
+  const uint64_t* sees;
+  const int32_t* lengths;
+  int32_t nseg, seg0, hkv;
+  int32_t start[N + 1], first[N + 1];
+
+  template <int QUERIES, int KEYS, int D, int KIND>
+  __device__ __forceinline__ TileWork find(const TileArgs& a, int block) const {
+    const int s = find_segment_wave(nseg, block, [&](int i) { return first[i]; });
+    const int seg = seg0 + s, b = seg / hkv, h = seg % hkv, at = start[s], room = start[s + 1] - at;
+    const int tiles = (a.G * a.T + QUERIES - 1) / QUERIES, i = block - first[s], parts = (first[s + 1] - first[s]) / tiles;
+    constexpr int kRow = D * Kind<KIND>::kBits / 8, kWide = D * (int)sizeof(typename Kind<KIND>::wide), kScales = D / kScaleBlock;
+    TileWork w;
+    w.part = i / tiles;
+    w.rows = a.G * a.T;
+    w.r0 = i % tiles * QUERIES;
+    w.n = __builtin_amdgcn_readfirstlane(rows_in_use(lengths, seg, room));
+    w.hist = w.n - a.T;
+    // the rows in use are spread over the parts of the room
+    const int steps = (w.n + KEYS - 1) / KEYS, each = (steps + parts - 1) / parts * KEYS;
+    w.parts = each ? (w.n + each - 1) / each : 1;
+    w.begin = w.part * each;
+    w.end = min(w.n, w.begin + each);
+    w.k = k + (int64_t)at * kRow;
+    w.v = v + (int64_t)at * kRow;
+    w.ks = KIND == SLKV_BF16_KV_MXFP4 ? k_scale + (int64_t)at * kScales : nullptr;
+    w.vs = KIND == SLKV_BF16_KV_MXFP4 ? v_scale + (int64_t)at * kScales : nullptr;
+    const int64_t head = ((int64_t)b * hkv + h) * a.G;
+    w.q = q + head * a.T * kWide;
+    w.out = out + head * a.T * kWide;
+    w.lse = lse ? lse + head * a.T : nullptr;
+    w.sees = sees + (int64_t)b * a.T;
+    w.q_tok = w.o_tok = kWide;
+    w.q_head = w.o_head = (int64_t)a.T * kWide;
+    w.lse_head = a.T;
+    w.k_row = w.v_row = kRow;
+    w.slot0 = first[s] + i % tiles;
+    w.slot_step = tiles;
+    return w;
+  }
+};
+constexpr int kTreeSegs = 480;
+
+struct TreePlan {
+  int shape, queries;
+  int64_t each;                      // room rows of a part, at most
+  int64_t slots;
+  bool split;
+  size_t off_ml, bytes;
+};
+
+static int64_t tree_parts(const slkv_cache_desc* d, int64_t s, int64_t each) {
+  return std::max<int64_t>(1, (d->h_offsets[s + 1] - d->h_offsets[s] + each - 1) / each);
+}
+
+static TreePlan plan_tree(const slkv_cache_desc* d, int T) {
+  TreePlan p;
+  const int64_t S = (int64_t)d->B * d->Hkv, R = (int64_t)(d->Hq / d->Hkv) * T, rows = d->h_offsets[S] - d->h_offsets[0];
+  p.shape = R <= 32 && d->dtype != SLKV_F32 ? 0 : R <= 64 ? 1 : 2;
+  p.queries = 32 << p.shape;
+  const int64_t tiles = (R + p.queries - 1) / p.queries, places = 256 * (p.shape == 0 || d->dtype == SLKV_F32 ? 1 : 2);
+  int64_t most = 1;
+  for (int64_t s = 0; s < S; ++s) most = std::max(most, d->h_offsets[s + 1] - d->h_offsets[s]);
+  p.each = most;
+  if (S * tiles < 2 * places) p.each = std::max<int64_t>(256, (rows * tiles + places - 1) / places);
+  p.split = most > p.each;
+  p.slots = 0;
+  for (int64_t s0 = 0; s0 < S; s0 += kTreeSegs) {
+    int64_t here = 0;
+    for (int64_t s = s0; s < std::min<int64_t>(S, s0 + kTreeSegs); ++s) here += tree_parts(d, s, p.each) * tiles;
+    p.slots = std::max(p.slots, here);
+  }
+  const size_t o = p.split ? (size_t)p.slots * p.queries * d->d * sizeof(float) : 0;
+  p.off_ml = o;
+  p.bytes = std::max<size_t>(16, o + (p.split ? (size_t)p.slots * p.queries * 2 * sizeof(float) : 0));
+  return p;
+}
+
+static slkv_status tree_checks(const slkv_cache_desc* desc, int32_t T) {
+  slkv_status st = validate_cache_desc(desc);
+  if (st != SLKV_OK) return st;
+  if (T < 1) return fail(SLKV_ERR_BAD_ARG, "T must be >= 1");
+  if (T > 64) return fail(SLKV_ERR_UNSUPPORTED, "T = %d > 64", T);
+  if (plan_tree(desc, T).slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
+  return SLKV_OK;
+}
+
+}  // namespace slkv
+
+using namespace slkv;
+
+extern "C" slkv_status slkv_tree_workspace_bytes(const slkv_cache_desc* desc, int32_t T, size_t* bytes) {
+  clear_error();
+  if (!bytes) return fail(SLKV_ERR_NULL, "bytes is NULL");
+  const slkv_status st = tree_checks(desc, T);
+  if (st != SLKV_OK) return st;
+  *bytes = plan_tree(desc, T).bytes;
+  return SLKV_OK;
+}
+
+extern "C" slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, const void* d_q, const uint64_t* d_sees, void* d_out,
+                                        float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  clear_error();
+  slkv_status st = tree_checks(desc, T);
+  if (st != SLKV_OK) return st;
+  if ((st = validate_cache(desc, cache)) != SLKV_OK) return st;
+  if (!d_q || !d_sees || !d_out || !d_workspace) return fail(SLKV_ERR_NULL, "a required device pointer is NULL");
+  const void* ptrs[] = {d_q, d_sees, d_out, d_lse, d_workspace};
+  for (const void* ptr : ptrs)
+    if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);
+  const TreePlan p = plan_tree(desc, T);
+  if (workspace_bytes < p.bytes) return fail(SLKV_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, p.bytes);
+  const int64_t S = (int64_t)desc->B * desc->Hkv;
+  TileArgs a;
+  a.G = desc->Hq / desc->Hkv;
+  a.T = T;
+  a.c_log2 = kLog2e / std::sqrt((float)desc->d);
+  a.part_o = (float*)d_workspace;
+  a.part_ml = (float*)((unsigned char*)d_workspace + p.off_ml);
+  hipStream_t const stream = (hipStream_t)hip_stream;
+  const int64_t tiles = ((int64_t)a.G * T + p.queries - 1) / p.queries;
+  auto launch_table = [&](auto t, int64_t s0, int64_t ns) {
+    using TAB = decltype(t);
+    t.k = (const unsigned char*)cache->d_k, t.v = (const unsigned char*)cache->d_v;
+    t.k_scale = (const unsigned char*)cache->d_k_scale, t.v_scale = (const unsigned char*)cache->d_v_scale;
+    t.q = (const unsigned char*)d_q, t.out = (unsigned char*)d_out;
+    t.lse = d_lse, t.sees = d_sees, t.lengths = cache->d_lengths;
+    t.nseg = (int32_t)ns, t.seg0 = (int32_t)s0, t.hkv = desc->Hkv;
+    int64_t blocks = 0;
+    for (int64_t i = 0; i <= ns; ++i) {
+      t.start[i] = (int32_t)desc->h_offsets[s0 + i];
+      t.first[i] = (int32_t)blocks;
+      if (i < ns) blocks += tree_parts(desc, s0 + i, p.each) * tiles;
+    }
+    auto launch = [&](auto kind, auto dim, auto wq, auto wk) {
+      constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value, kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
+      {
+        ScopedKernelTimer timer(SLKV_K_TREE);
+        SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, 1, kWQ, kWK, TAB>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+      }
+      if (p.split) {
+        ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
+        SLKV_LAUNCH((join_tiles_kernel<kKind, kDim, 1, kWQ, kWK, TAB>), dim3((unsigned)blocks), dim3(256), 0, stream, a, t);
+      }
+    };
+    with_kind(desc->dtype, [&](auto kind) {
+      auto with_shape = [&](auto dim) {
+        using std::integral_constant;
+        integral_constant<int, 1> one;
+        integral_constant<int, 2> two;
+        integral_constant<int, 4> four;
+        if constexpr (decltype(kind)::value != SLKV_F32) {
+          if (p.shape == 0) return launch(kind, dim, one, four);
+        }
+        if (p.shape == 1) return launch(kind, dim, two, two);
+        launch(kind, dim, four, one);
+      };
+      if (desc->d == 64) with_shape(std::integral_constant<int, 64>{});
+      else with_shape(std::integral_constant<int, 128>{});
+    });
+  };
+  if (S <= kFewSegs) launch_table(TreeTab<kFewSegs>{}, 0, S);
+  else
+    for (int64_t s0 = 0; s0 < S; s0 += kTreeSegs) launch_table(TreeTab<kTreeSegs>{}, s0, std::min<int64_t>(kTreeSegs, S - s0));
+  return launch_status("attend_tree");
+}

@@ -1,0 +1,223 @@
+"""slkv_accept_cache against the float64 oracle: rows that move, paths in any order, rooms that are full, weights of the accepted tokens."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode
+from paper_2508_15806_amd import api
+from decode_parity import DTYPES, cache_values, close, f64, normal, random_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def everything(cache):
+    return {n: getattr(cache, n).clone() for n in ("k", "v", "k_scale", "v_scale", "pos", "weight", "lengths") if getattr(cache, n) is not None}
+
+
+def check(cache, path, T, at=None, weights=True, apart=False, rng=None):
+    """One call, compared row by row with what was there; weights with the oracle's."""
+    rng = rng or np.random.default_rng(1)
+    B, Hq, Hkv, d = cache.B, cache.Hq, cache.Hkv, cache.d
+    before = everything(cache)
+    q = lse = out = None
+    if weights:
+        q = normal(rng, (B, Hq, T, d), cache.dtype)
+        lse = torch.from_numpy(rng.uniform(3, 8, (B, Hq, T)).astype(np.float32)).cuda()
+        out = torch.full_like(cache.weight, -1.0) if apart else None
+    p = torch.tensor(path, dtype=torch.int32).cuda()
+    cache.accept(p, T, at=at, q=q, lse=lse, weight=out)
+    torch.cuda.synchronize()
+    after = everything(cache)
+    if out is not None:
+        after["sums"] = out
+    offsets = cache.layout.offsets
+    rooms = np.diff(offsets)
+    n0 = before["lengths"].cpu().numpy().clip(0, rooms)
+    base = n0 - T if at is None else (n0 if at is cache.lengths else at.cpu().numpy().clip(0, rooms))
+    src, dst, used = [], [], []
+    for s in range(B * Hkv):
+        rows, to = decode.accept_segment(path[s // Hkv], T, int(base[s]), int(rooms[s]))
+        src += [int(offsets[s]) + r for r in rows]
+        dst += [int(offsets[s]) + to + i for i in range(len(rows))]
+        used.append(to + len(rows))
+    assert after["lengths"].tolist() == used
+    for name in ("k", "v", "k_scale", "v_scale", "pos", "weight"):
+        if name not in before:
+            continue
+        want = before[name].clone()
+        want[dst] = before[name][src]
+        if name == "weight":
+            moved = want.double().cpu().numpy()
+            if weights and not apart:
+                continue
+        # (bit for bit: rows may hold NaN)
+        size = want.element_size()
+        as_whole = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[size]
+        assert torch.equal(after[name].view(as_whole), want.view(as_whole)), name
+    if not weights:
+        return
+    k, _ = cache_values(cache)
+    want, tol, there = moved.copy(), np.zeros(moved.shape), np.zeros(moved.shape, bool)
+    u, G = 2.0 ** -24, Hq // Hkv
+    qq, ll = f64(q), f64(lse)
+    for s in range(B * Hkv):
+        a, n, b, h = int(offsets[s]), used[s], s // Hkv, s % Hkv
+        there[a:a + n] = True
+        rows, to = decode.accept_segment(path[b], T, int(base[s]), int(rooms[s]))
+        tokens = [r - int(base[s]) for r in rows]
+        for i, t in enumerate(tokens):
+            for g in range(G):
+                m = to + i + 1
+                with np.errstate(invalid="ignore", over="ignore"):
+                    x = k[a:a + m] @ qq[b, h * G + g, t] / np.sqrt(d)
+                    e = np.exp(x - ll[b, h * G + g, t])
+                    off = (2 * d + 8) * u * (np.abs(k[a:a + m]) @ np.abs(qq[b, h * G + g, t])) / np.sqrt(d) + 2.0 ** -21 + 4 * u * abs(ll[b, h * G + g, t])
+                want[a:a + m] += e
+                tol[a:a + m] += 2 * off * e
+        added = len(tokens) * G
+        tol[a:a + n] += (added + 2) * u * np.abs(want[a:a + n])
+    got = f64(out if apart else cache.weight)
+    close(np.where(there, got, 0), np.where(there, want, 0), np.where(np.isfinite(tol), tol, 0), "weight")
+    rest = got[~there]
+    assert (rest == (-1.0 if apart else moved[~there])).all(), "weights of rows that are not in use were written"
+
+
+PATHS = [[0, 3, 4, -1, 0], [2, 1, 0, 5, 9], [-1, 0, 0, 0, 0], [9, 9, 0, 9, 1], [0, 1, 2, 3, 4], [1, 2, 3, 10, 4]]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("weights", [False, True])
+def test_types(dtype, d, weights):
+    rng = np.random.default_rng([d, DTYPES.index(dtype)])
+    lens = [10, 11, 74, 75, 300, 266, 267, 1000, 12, 40, 523, 330]
+    cache = random_cache(rng, dtype, 6, 2, 3, d, lens, rooms=[n + (i * 7) % 11 for i, n in enumerate(lens)], before=3)
+    check(cache, PATHS, 10, weights=weights, apart=d == 64, rng=rng)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_the_largest_draft(dtype):
+    rng = np.random.default_rng(2)
+    cache = random_cache(rng, dtype, 2, 2, 8, 128, [64, 700, 65, 1300], rooms=[70, 700, 80, 1400])
+    path = [rng.permutation(64).tolist(), rng.integers(0, 64, 64).tolist()]
+    check(cache, path, 64, rng=rng)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("own_lengths", [False, True])
+def test_rows_behind_a_number_of_them(weights, own_lengths):
+    """at: given, or the lengths themselves; drafts that the room does not hold whole."""
+    rng = np.random.default_rng(3)
+    lens = [10, 0, 95, 300]
+    cache = random_cache(rng, "bf16", 2, 2, 2, 64, lens, rooms=[20, 3, 100, 310])
+    at = cache.lengths if own_lengths else torch.tensor([4, 0, 95, 900], dtype=torch.int32).cuda()
+    check(cache, [[0, 2, 5, 7], [0, 4, 6, 1]], 8, at=at, weights=weights, rng=rng)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+def test_fewer_rows_than_drafted_tokens(weights):
+    rng = np.random.default_rng(4)
+    cache = random_cache(rng, "bf16_kv8", 2, 2, 2, 64, [3, 0, 8, 7], rooms=[5, 0, 9, 7])
+    check(cache, [[7, 5, 6], [0, 1, 7]], 8, weights=weights, rng=rng)
+
+
+@pytest.mark.parametrize("S", [90, 1000])
+def test_many_segments(S):
+    rng = np.random.default_rng(S)
+    lens = rng.integers(4, 300, S)
+    cache = random_cache(rng, "bf16_kv4", S, 1, 2, 64, lens.tolist(), rooms=(lens + 5).tolist())
+    check(cache, rng.integers(-1, 4, (S, 3)).tolist(), 4, rng=rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_keys_that_are_not_finite(dtype):
+    """A NaN in an accepted key reaches its row's weight alone, one in a row that was not accepted none."""
+    rng = np.random.default_rng(5)
+    cache = random_cache(rng, dtype, 1, 1, 4, 64, [100], rooms=[110])
+    cache.k[100 - 6 + 3] = float("nan")       # accepted second
+    cache.k[100 - 6 + 1] = float("inf")       # not accepted
+    check(cache, [[0, 3, 5]], 6, rng=rng)
+    assert torch.isnan(cache.weight).nonzero().flatten().tolist() == [95]
+
+
+def test_a_token_that_saw_nothing_adds_nothing():
+    rng = np.random.default_rng(6)
+    cache = random_cache(rng, "bf16", 1, 1, 2, 64, [50], rooms=[60])
+    before = cache.weight.clone()
+    q = normal(rng, (1, 2, 4, 64), "bf16")
+    lse = torch.full((1, 2, 4), -float("inf"), device="cuda")
+    cache.accept(torch.tensor([[0]], dtype=torch.int32).cuda(), 4, q=q, lse=lse)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.weight, before) and cache.lengths.tolist() == [47]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_weights_are_those_of_one_token_after_the_other(dtype):
+    """A draft that is accepted leaves the cache that attending to its tokens one at a time leaves."""
+    rng = np.random.default_rng(7)
+    lens, T = [40, 7, 300, 130], 6
+    tree = random_cache(rng, dtype, 2, 2, 4, 128, lens, rooms=[n + 20 for n in lens])
+    chain = api.Cache(dtype, 2, 8, 2, 128, tree.layout.offsets, k=tree.k.clone(), v=tree.v.clone(), k_scale=None if tree.k_scale is None else tree.k_scale.clone(),
+                      v_scale=None if tree.v_scale is None else tree.v_scale.clone(), lengths=tree.lengths.clone(), pos=tree.pos.clone(), weight=tree.weight.clone())
+    k, v, q = normal(rng, (2, 2, T, 128), dtype), normal(rng, (2, 2, T, 128), dtype), normal(rng, (2, 8, T, 128), dtype)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")[None].repeat(2, 1) + 500
+    path = [[0, 2, 5], [0, 1, -1]]
+    parents = np.array([[-1, 0, 0, 1, 1, 2], [-1, 0, 0, 1, 2, 2]])
+    tree.append(k, v, pos)
+    out, lse = tree.attend_tree(q, api.tree_bits(parents).cuda())
+    tree.accept(torch.tensor(path, dtype=torch.int32).cuda(), T, q=q, lse=lse)
+    for i in range(3):
+        was = everything(chain)
+        t = [max(p[i], 0) for p in path]
+        pick = lambda x: torch.stack([x[b, :, t[b]] for b in range(2)])[:, :, None].contiguous()
+        chain.append(pick(k), pick(v), pos[:, :1] + torch.tensor(t, dtype=torch.int32, device="cuda")[:, None])
+        o, l = chain.attend(pick(q))
+        torch.cuda.synchronize()
+        for b in range(2):
+            if path[b][i] >= 0:
+                np.testing.assert_allclose(f64(out[b, :, t[b]]), f64(o[b, :, 0]), rtol=2.0 ** -6, atol=0.02)
+                np.testing.assert_allclose(f64(lse[b, :, t[b]]), f64(l[b, :, 0]), rtol=1e-5, atol=1e-5)
+        if i == 2:                              # the second sequence has no third token
+            a = int(chain.layout.offsets[2])
+            for name, x in was.items():
+                getattr(chain, name)[2 if name == "lengths" else a:] = x[2 if name == "lengths" else a:]
+    assert tree.lengths.tolist() == chain.lengths.tolist() == [43, 10, 302, 132]
+    for s, n in enumerate(tree.lengths.tolist()):
+        rows = slice(int(tree.layout.offsets[s]), int(tree.layout.offsets[s]) + n)
+        for name in ("k", "v", "pos"):
+            assert torch.equal(getattr(tree, name)[rows], getattr(chain, name)[rows])
+        np.testing.assert_allclose(f64(tree.weight[rows]), f64(chain.weight[rows]), rtol=2e-5, atol=1e-6)
+
+
+def test_graph():
+    """Draft, verification and acceptance, captured and replayed: the cache grows as it does without a graph."""
+    rng = np.random.default_rng(8)
+    T = 5
+    made = [random_cache(np.random.default_rng(9), "bf16_kv4", 2, 2, 4, 64, [30, 200, 75, 400], rooms=[80, 250, 125, 450]) for _ in range(2)]
+    k, v, q = normal(rng, (2, 2, T, 64), "bf16"), normal(rng, (2, 2, T, 64), "bf16"), normal(rng, (2, 8, T, 64), "bf16")
+    bits = api.tree_bits(np.array([[-1, 0, 0, 1, 3], [-1, 0, 1, 2, 3]])).cuda()
+    path = torch.tensor([[0, 1, 3, 4], [0, 1, -1, -1]], dtype=torch.int32).cuda()
+
+    def turn(cache):
+        cache.append(k, v)
+        out, lse = cache.attend_tree(q, bits)
+        cache.accept(path, T, q=q, lse=lse)
+        return out, lse
+    g = torch.cuda.CUDAGraph()
+    turn(made[0])
+    turn(made[1])
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        got = turn(made[1])
+    for i in range(5):
+        want = turn(made[0])
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        a, b = everything(made[0]), everything(made[1])
+        assert a["lengths"].tolist() == b["lengths"].tolist() == [30 + 4 * (i + 2), 200 + 4 * (i + 2), 75 + 2 * (i + 2), 400 + 2 * (i + 2)]
+        for s, n in enumerate(a["lengths"].tolist()):
+            rows = slice(int(made[0].layout.offsets[s]), int(made[0].layout.offsets[s]) + n)
+            assert all(torch.equal(a[x][rows], b[x][rows]) for x in ("k", "v", "k_scale", "v_scale", "weight")), (i, s)
+        torch.zeros(1000, device="cuda").sum().item()
