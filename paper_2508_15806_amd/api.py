@@ -169,6 +169,7 @@ class PromptCall(_OnDevice):
         self.keys = self.queries if cu_k is None else int(self.batch.cu_k[-1])
         self.workspace_bytes = B.slkv_prompt_workspace_bytes(self.batch)
         self._set_device(device)
+        self._lse_like = None
 
     def _rows(self, t, heads, tokens, tdt, name):
         if self._tensor(t, (heads, tokens, self.d), tdt, name, contiguous=False).stride(2) != 1:
@@ -184,10 +185,12 @@ class PromptCall(_OnDevice):
         with self._on(stream):
             handle = B._stream(None)
             out = torch.empty_like(q) if out is None else self._rows(out, self.Hq, self.queries, self.query_dtype, "out")
-            if lse is None:
-                lse = torch.empty((self.Hq, self.queries), dtype=torch.float32, device=self.device)
-            else:
+            if lse is not None:
                 self._tensor(lse, (self.Hq, self.queries), torch.float32, "lse")
+            elif self._lse_like is None:
+                lse = self._lse_like = torch.empty((self.Hq, self.queries), dtype=torch.float32, device=self.device)
+            else:
+                lse = torch.empty_like(self._lse_like)
             B.slkv_attend_prompt(self.batch, q, k, v, out, self._workspace(self.workspace_bytes, handle), lse, handle)
         return out, lse
 

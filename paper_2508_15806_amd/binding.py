@@ -450,12 +450,18 @@ class PromptBatch:
                                None if cu_k is None else self.cu_k.ctypes.data, (C.c_int64 * 8)(0, 0, 0, 0, 0, 0, d, 0))
         self.desc.strides[7] = d * max(int(self.cu_q[-1]), 1)      # (of out: [Hq][tokens][d] until a call says otherwise)
         self.address = C.addressof(self.desc)
+        self._strided = {}
 
     def with_strides(self, *tensors):
-        """This batch with the token and head strides of q, k, v and out [heads, tokens, d]."""
-        desc = PromptDesc.from_buffer_copy(self.desc)
-        desc.strides[:] = [t.stride(i) if t.shape[i] > 1 else 0 for t in tensors for i in (1, 0)]    # (torch leaves anything as the stride of one)
-        return desc
+        """The descriptor with the token and head strides of q, k, v and out [heads, tokens, d], by address; kept, for a program calls with few of them."""
+        strides = tuple(t.stride() for t in tensors)
+        desc = self._strided.get(strides)
+        if desc is None:
+            if len(self._strided) >= 64:
+                self._strided.clear()
+            desc = self._strided[strides] = PromptDesc.from_buffer_copy(self.desc)
+            desc.strides[:] = [t.stride(i) if t.shape[i] > 1 else 0 for t in tensors for i in (1, 0)]    # (torch leaves anything as the stride of one)
+        return C.addressof(desc), desc
 
 
 def slkv_prompt_workspace_bytes(batch):
@@ -466,8 +472,8 @@ def slkv_prompt_workspace_bytes(batch):
 
 def slkv_attend_prompt(batch, q, k, v, out, workspace, lse=None, stream=None):
     """q, out: [Hq, queries, d]; k, v: [Hkv, tokens, d], of any strides with contiguous rows; lse [Hq, queries] fp32."""
-    desc = batch.with_strides(q, k, v, out)
-    _check(lib().slkv_attend_prompt(C.addressof(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(workspace), workspace.nbytes,
+    address, _kept = batch.with_strides(q, k, v, out)
+    _check(lib().slkv_attend_prompt(address, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(workspace), workspace.nbytes,
                                     _stream(stream)))
 
 

@@ -1,7 +1,7 @@
 // Attention of tiles of queries over tiles of rows that are staged in LDS: what slkv_attend_prompt and slkv_attend_tree share.
 //
 // The G = Hq/Hkv heads that share a KV head's rows are put together: query row r of a segment (sequence, KV head) is token r / G, head r % G, so that a tile of
-// 32 rows covers 32/G neighbouring tokens and the mask cuts few of its keys.  A workgroup is WQ x WK waves; a wave holds QT tiles of 32 query rows in
+// 32 rows covers 32/G neighbouring tokens and the mask cuts few of its keys.  A workgroup is WQ x WK waves; a wave holds 32 query rows in
 // registers, and takes every WK'th 32 rows of a staged tile of keys.
 //
 // x = K q with MFMA operands of 32 keys by 16 dims comes out as D[key][query]: lane l holds query l % 32 and, of 32 keys, 8 (i / 4) + 4 (l / 32) + i % 4 for
@@ -16,6 +16,7 @@
 #include "attend_rows.h"
 #include "launch.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace slkv {
@@ -23,7 +24,6 @@ namespace slkv {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTileWaves = 4;
 
 // Segment and tile of a workgroup; the same in all its lanes.
 struct TileWork {
@@ -59,13 +59,13 @@ __device__ __forceinline__ T lds_at(uint32_t at) { return *(const __attribute__(
 template <class T>
 __device__ __forceinline__ void lds_put(uint32_t at, T v) { *(__attribute__((address_space(3))) T*)(uintptr_t)at = v; }
 
-template <int KIND, int D, int QT, int WQ, int WK>
+template <int KIND, int D, int WQ, int WK>
 struct Tiles {
   typedef typename Kind<KIND>::wide wide;
   static constexpr bool kF32 = KIND == SLKV_F32;
   static constexpr bool kNarrow = Kind<KIND>::kBits < 16;
-  static constexpr int kThreads = WQ * WK * kWave;
-  static constexpr int kQueries = 32 * QT * WQ;        // query rows of a workgroup
+  static constexpr int kWaves = WQ * WK, kThreads = kWaves * kWave;
+  static constexpr int kQueries = 32 * WQ;        // query rows of a workgroup
   static constexpr int kSub = WK == 1 ? 2 : 1;         // subtiles of 32 keys that a wave takes of a staged tile
   static constexpr int kKeys = 32 * kSub * WK;         // rows of a staged tile
   static constexpr int kRow = D * (int)sizeof(wide);   // bytes of a row in LDS
@@ -75,7 +75,11 @@ struct Tiles {
   static constexpr int kScales = D / kScaleBlock;
   static constexpr int kDT = D / 32;                   // tiles of 32 dims
   static constexpr int kOutRow = D + 4;                // floats of a row of sums in LDS
-  static constexpr int kLds = 4 * kTileBytes > kTileWaves * 32 * kOutRow * 4 ? 4 * kTileBytes : kTileWaves * 32 * kOutRow * 4;
+  // Narrow rows of four subtiles a step: one tile in LDS, the next one in registers, so that two workgroups share a CU.
+  static constexpr bool kSingle = kNarrow && WK == 4 && WQ == 1;
+  static constexpr int kTilesBytes = (kSingle ? 2 : 4) * kTileBytes;
+  static constexpr int kLds = kTilesBytes > kWaves * 32 * kOutRow * 4 ? kTilesBytes : kWaves * 32 * kOutRow * 4;
+  static constexpr int kPerSimd = KIND == SLKV_F32 || (WQ == 1 && WK == 4 && !kSingle) ? 1 : 2;   // waves of a SIMD, at least
   // Reference of fp16 weights: they reach 2^15, so that those down to 2^-26 of the largest keep all their bits.
   static constexpr float kBelow = KIND == SLKV_F16 ? 12.f : 0.f, kBelowPower = KIND == SLKV_F16 ? 0x1p-12f : 1.f;
   static constexpr float kAbove = KIND == SLKV_F16 ? 15.f : 8.f;   // a product this far above the reference moves it
@@ -123,11 +127,15 @@ struct Tiles {
   static constexpr int kSrcChunks = kNarrow ? kSrcRow / 16 : 1;
   static constexpr int kUnits = kKeys * kSrcChunks, kFetch = (kUnits + kThreads - 1) / kThreads;
   struct Fetched { u32x4 k[kFetch], v[kFetch]; uint32_t ks[kFetch], vs[kFetch]; };
+  // a wave takes whole rows, its neighbouring lanes a piece of one after the other, so that what they write finds all banks
+  static constexpr int kUnitRows = kWave / kSrcChunks;
+  static __device__ __forceinline__ int row_of_unit(int u) { return u / kWave * kUnitRows + u % kUnitRows; }
+  static __device__ __forceinline__ int chunk_of_unit(int u) { return u % kWave / kUnitRows; }
   static __device__ __forceinline__ void fetch(Fetched& f, const TileWork& w, int first, int end) {
 #pragma unroll
     for (int i = 0; i < kFetch; ++i) {
-      const int u = min((int)threadIdx.x + i * kThreads, kUnits - 1), c = u % kSrcChunks;
-      const int64_t row = min(first + u / kSrcChunks, end - 1);
+      const int u = min((int)threadIdx.x + i * kThreads, kUnits - 1), c = chunk_of_unit(u);
+      const int64_t row = min(first + row_of_unit(u), end - 1);
       f.k[i] = *(const u32x4*)(w.k + row * w.k_row + c * 16);
       f.v[i] = *(const u32x4*)(w.v + row * w.v_row + c * 16);
       if constexpr (KIND == SLKV_BF16_KV_MXFP4) {
@@ -154,8 +162,8 @@ struct Tiles {
     for (int i = 0; i < kFetch; ++i) {
       const int u = (int)threadIdx.x + i * kThreads;
       if (kUnits % kThreads && u >= kUnits) break;
-      one(f.k[i], f.ks[i], u / kSrcChunks, u % kSrcChunks, lds);
-      one(f.v[i], f.vs[i], u / kSrcChunks, u % kSrcChunks, lds + kTileBytes);
+      one(f.k[i], f.ks[i], row_of_unit(u), chunk_of_unit(u), lds);
+      one(f.v[i], f.vs[i], row_of_unit(u), chunk_of_unit(u), lds + kTileBytes);
     }
   }
 
@@ -183,46 +191,38 @@ struct Tiles {
   }
 
   // queries of the lane: 16-bit: product u takes the dims 16 u + 8 g .. + 7 of lane group g = lane / 32; fp32: 8 u + 4 g + j
-  struct Queries { u32x4 w[QT][kF32 ? D / 8 : D / 16]; };
+  struct Queries { u32x4 w[kF32 ? D / 8 : D / 16]; };
 
-  // x[sub][qt] of the wave's subtiles; kt: K in LDS, at the wave's first subtile
-  static __device__ __forceinline__ void logits(f32x16 (&x)[kSub][QT], const Queries& q, uint32_t kt, int l32, int g) {
+  // x[sub] of the wave's subtiles; kt: K in LDS, at the wave's first subtile
+  static __device__ __forceinline__ void logits(f32x16 (&x)[kSub], const Queries& q, uint32_t kt, int l32, int g) {
     const uint32_t at = kt + l32 * kRow + (uint32_t)((g ^ swizzle(l32)) * 16);      // (chunk 2 u + g) ^ swizzle = (2 u) ^ (g ^ swizzle)
 #pragma unroll
     for (int s = 0; s < kSub; ++s) {
       if constexpr (kF32) {
         // four sums side by side: one chain of D additions is what the result's error comes from
-        f32x16 y[QT][4];
+        f32x16 y[4];
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[qt][j] = f32x16{};
+        for (int j = 0; j < 4; ++j) y[j] = f32x16{};
 #pragma unroll
         for (int u = 0; u < D / 8; ++u) {
           const f32x4 ko = lds_at<f32x4>((at ^ (u * 32)) + s * 32 * kRow);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt)
-              y[qt][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(ko[j], __uint_as_float(q.w[qt][u][j]), y[qt][j], 0, 0, 0);
+          for (int j = 0; j < 4; ++j) y[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(ko[j], __uint_as_float(q.w[u][j]), y[j], 0, 0, 0);
         }
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) x[s][qt] = (y[qt][0] + y[qt][1]) + (y[qt][2] + y[qt][3]);
+        x[s] = (y[0] + y[1]) + (y[2] + y[3]);
       } else {
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) x[s][qt] = f32x16{};
+        x[s] = f32x16{};
 #pragma unroll
         for (int u = 0; u < D / 16; ++u) {
           const u32x4 ko = lds_at<u32x4>((at ^ (u * 32)) + s * 32 * kRow);
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt) x[s][qt] = mfma(ko, q.w[qt][u], x[s][qt]);
+          x[s] = mfma(ko, q.w[u], x[s]);
         }
       }
     }
   }
 
-  // acc[qt] += p V of one subtile; vt: V in LDS, at the subtile
-  static __device__ __forceinline__ void add_values(f32x16 (&acc)[QT][kDT], const f32x16 (&p)[QT], uint32_t vt, int lane) {
+  // acc += p V of one subtile; vt: V in LDS, at the subtile
+  static __device__ __forceinline__ void add_values(f32x16 (&acc)[kDT], const f32x16& p, uint32_t vt, int lane) {
     if constexpr (kF32) {
       const int g = lane >> 5, l32 = lane & 31;
       const uint32_t at = vt + 4 * g * kRow + (uint32_t)((l32 / 4) ^ (g << 3)) * 16 + l32 % 4 * 4;
@@ -231,8 +231,7 @@ struct Tiles {
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt) {
           const float v = lds_at<float>((at ^ (uint32_t)((i & 3 | (i >> 2 & 1) << 2 | dt << 3) * 16)) + (i / 4 * 8 + i % 4) * kRow);
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[qt][i], acc[qt][dt], 0, 0, 0);
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], acc[dt], 0, 0, 0);
         }
     } else {
       // lane i of 16 reads the piece i % 4, of 8 bytes, of row i / 4: of the rows 4 g .. 4 g + 3 and, with j2, 8 rows on; 16 dims to 16 lanes
@@ -241,11 +240,9 @@ struct Tiles {
       const uint32_t at = vt + row * kRow + (uint32_t)((2 * h + i1) ^ swizzle(row)) * 16 + (lane & 1) * 8;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        u32x4 po[QT];
+        u32x4 po;
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) po[qt][j] = pair(p[qt][c * 8 + j * 2], p[qt][c * 8 + j * 2 + 1]);
+        for (int j = 0; j < 4; ++j) po[j] = pair(p[c * 8 + j * 2], p[c * 8 + j * 2 + 1]);
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt) {
           u32x4 vo;
@@ -256,8 +253,7 @@ struct Tiles {
             vo[j2 * 2] = t[0];
             vo[j2 * 2 + 1] = t[1];
           }
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = mfma(vo, po[qt], acc[qt][dt]);
+          acc[dt] = mfma(vo, po, acc[dt]);
         }
       }
     }
@@ -265,20 +261,16 @@ struct Tiles {
 
   // whether some value of the subtile's 32 rows is not finite
   static __device__ __forceinline__ bool any_not_finite(uint32_t vt, int lane) {
-    bool bad = false;
+    // an exponent of all ones carries into the sign's place
+    constexpr uint32_t kExp = kF32 ? 0x7f800000u : KIND == SLKV_F16 ? 0x7c007c00u : 0x7f807f80u, kOne = kF32 ? 0x00800000u : KIND == SLKV_F16 ? 0x04000400u : 0x00800080u;
+    uint32_t carries = 0;
 #pragma unroll
     for (int i = 0; i < 32 * kChunks / kWave; ++i) {
       const u32x4 x = lds_at<u32x4>(vt + (i * kWave + lane) * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (kF32) {
-          bad |= (x[j] & 0x7f800000u) == 0x7f800000u;
-        } else {
-          constexpr uint32_t kExp = KIND == SLKV_F16 ? 0x7c00u : 0x7f80u;
-          bad |= (x[j] & kExp) == kExp || (x[j] >> 16 & kExp) == kExp;
-        }
-      }
+      for (int j = 0; j < 4; ++j) carries |= (x[j] & kExp) + kOne;
     }
+    const bool bad = (carries & (kF32 ? 0x80000000u : 0x80008000u)) != 0;
     return __ballot(bad) != 0;
   }
 };
@@ -309,9 +301,9 @@ __device__ __forceinline__ f32x4 tile_output(f32x4 o, float total, bool none) {
   return o;
 }
 
-template <int KIND, int D, int QT, int WQ, int WK, class TAB>
-__global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F32 ? 2 : 1) void attend_tiles_kernel(const TileArgs a, const TAB tab) {
-  using A = Tiles<KIND, D, QT, WQ, WK>;
+template <int KIND, int D, int WQ, int WK, class TAB>
+__global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) void attend_tiles_kernel(const TileArgs a, const TAB tab) {
+  using A = Tiles<KIND, D, WQ, WK>;
   constexpr int kSub = A::kSub, kDT = A::kDT;
   __shared__ __align__(1024) unsigned char sh[A::kLds];
   __shared__ float sh_m[WK][32 * WQ], sh_l[WK][32 * WQ];
@@ -321,110 +313,88 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int l32 = lane & 31, g = lane >> 5, wq = wave % WQ, wk = wave / WQ;
   const int t0 = w.r0 / a.G, rem0 = w.r0 % a.G;        // token and head of the tile's first row
-  const int first = wq * 32 * QT;                      // the wave's first row of the tile
+  const int first = wq * 32;                           // the wave's first row of the tile
   const bool busy = w.r0 + first < w.rows;             // (waves without queries only stage)
 
   typename A::Queries q;
-  int t_of[QT];
-  uint64_t bits[QT];
+  const int r_of = max(min(first + l32, w.rows - 1 - w.r0), 0), dt_of = divide(rem0 + r_of, a.G), t_of = t0 + dt_of;   // the lane's row of the tile, its token
+  const uint64_t bits = bits_of(w, t_of, a.T);
+  const unsigned char* const q_at = w.q + t_of * w.q_tok + (rem0 + r_of - dt_of * a.G) * w.q_head;
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const int r = min(first + qt * 32 + l32, w.rows - 1 - w.r0);
-    const int dt = divide(rem0 + max(r, 0), a.G), head = rem0 + max(r, 0) - dt * a.G;
-    t_of[qt] = t0 + dt;
-    bits[qt] = bits_of(w, t_of[qt], a.T);
-    const unsigned char* p = w.q + t_of[qt] * w.q_tok + head * w.q_head;
-#pragma unroll
-    for (int u = 0; u < (A::kF32 ? D / 8 : D / 16); ++u) q.w[qt][u] = *(const u32x4*)(p + u * 32 + g * 16);
-  }
+  for (int u = 0; u < (A::kF32 ? D / 8 : D / 16); ++u) q.w[u] = *(const u32x4*)(q_at + u * 32 + g * 16);
 
-  float ref[QT], sum[QT];
-  f32x16 acc[QT][kDT];
+  float ref = -INFINITY, sum = 0.f;
+  f32x16 acc[kDT];
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    ref[qt] = -INFINITY;
-    sum[qt] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < kDT; ++dt) acc[qt][dt] = f32x16{};
-  }
+  for (int dt = 0; dt < kDT; ++dt) acc[dt] = f32x16{};
   // keys that every query of the tile sees
   const int all = w.sees ? w.hist : w.hist + t0 + 1;
   // bit j: the lane's query sees the key key0 + j, which is there
-  auto seen = [&](int qt, int key0) __attribute__((always_inline)) {
-    uint32_t m = first_bits((w.sees ? w.hist : w.hist + t_of[qt] + 1) - key0);
+  auto seen = [&](int key0) __attribute__((always_inline)) {
+    uint32_t m = first_bits((w.sees ? w.hist : w.hist + t_of + 1) - key0);
     if (w.sees) {
       const int u = key0 - w.hist;                     // the draft's first row is bit -u
-      m |= u >= 64 || u <= -32 ? 0u : u >= 0 ? (uint32_t)(bits[qt] >> u) : (uint32_t)bits[qt] << -u;
+      m |= u >= 64 || u <= -32 ? 0u : u >= 0 ? (uint32_t)(bits >> u) : (uint32_t)bits << -u;
     }
     return m & first_bits(w.end - key0);
   };
 
-  auto step = [&](int key0, uint32_t buf) __attribute__((always_inline)) {
+  auto step = [&](auto tail_c, int key0, uint32_t buf) __attribute__((always_inline)) {
+    constexpr bool tail = decltype(tail_c)::value;
     const uint32_t kt = buf + wk * 32 * kSub * A::kRow, vt = kt + A::kTileBytes;
     const int mine = key0 + wk * 32 * kSub;
-    f32x16 x[kSub][QT];
+    f32x16 x[kSub];
     A::logits(x, q, kt, l32, g);
-    const bool tail = key0 + A::kKeys > all;
-    if (tail) {
+    if constexpr (tail) {
 #pragma unroll
-      for (int s = 0; s < kSub; ++s)
+      for (int s = 0; s < kSub; ++s) {
+        const uint32_t m = seen(mine + s * 32) >> (4 * g);
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          const uint32_t m = seen(qt, mine + s * 32) >> (4 * g);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[s][qt][i] = m & 1u << (i / 4 * 8 + i % 4) ? x[s][qt][i] : -INFINITY;
-        }
-    }
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int s = 0; s < kSub; ++s)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[s][qt][i]);
-      top *= a.c_log2;
-      if (__ballot(top > ref[qt] + A::kAbove)) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = fmaxf(ref[qt], top - A::kBelow);
-        const float f = ref[qt] == -INFINITY ? 0.f : exp2_fast(ref[qt] - now);
-        // (sums of a NaN stay one)
-        sum[qt] *= f;
-#pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) acc[qt][dt] *= f;
-        ref[qt] = now;
+        for (int i = 0; i < 16; ++i) x[s][i] = m & 1u << (i / 4 * 8 + i % 4) ? x[s][i] : -INFINITY;
       }
-      // (one rounding, of the difference: a large product's own would be an error of the weight)
-      const float from = ref[qt] == -INFINITY ? 0.f : ref[qt];
-#pragma unroll
-      for (int s = 0; s < kSub; ++s)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          x[s][qt][i] = exp2_fast(fmaf(x[s][qt][i], a.c_log2, -from));
-          sum[qt] += x[s][qt][i];
-        }
     }
+    float top = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < kSub; ++s)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[s][i]);
+    top *= a.c_log2;
+    if (__ballot(top > ref + A::kAbove)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float now = fmaxf(ref, top - A::kBelow);
+      const float f = ref == -INFINITY ? 0.f : exp2_fast(ref - now);
+      // (sums of a NaN stay one)
+      sum *= f;
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) acc[dt] *= f;
+      ref = now;
+    }
+    // (one rounding, of the difference: a large product's own would be an error of the weight)
+    const float from = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+    for (int s = 0; s < kSub; ++s)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[s][i] = exp2_fast(fmaf(x[s][i], a.c_log2, -from));
+        sum += x[s][i];
+      }
 #pragma unroll
     for (int s = 0; s < kSub; ++s) {
       const uint32_t vs = vt + s * 32 * A::kRow;
       if (tail && A::any_not_finite(vs, lane)) {
         // a row at a time, to the queries that see it: an infinity or NaN reaches no other through a weight of 0
-        uint32_t m[QT];
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) m[qt] = seen(qt, mine + s * 32);
+        const uint32_t m = seen(mine + s * 32);
         for (int row = 0; row < 32; ++row) {
+          float p = 0.f;
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) {
-            float p = 0.f;
+          for (int i = 0; i < 16; ++i)
+            if (i == row / 8 * 4 + row % 4) p = x[s][i];
+          p = __shfl(p, (row / 4 & 1) * 32 + l32);
+          if (m >> row & 1) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (i == row / 8 * 4 + row % 4) p = x[s][qt][i];
-            p = __shfl(p, (row / 4 & 1) * 32 + l32);
-            if (m[qt] >> row & 1) {
+            for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-              for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[qt][dt][i] += p * A::value(vs, row, dt * 32 + i / 4 * 8 + 4 * g + i % 4);
-            }
+              for (int i = 0; i < 16; ++i) acc[dt][i] += p * A::value(vs, row, dt * 32 + i / 4 * 8 + 4 * g + i % 4);
           }
         }
       } else {
@@ -433,116 +403,213 @@ __global__ __launch_bounds__(WQ* WK* kWave, QT == 1 && WK < 4 && KIND != SLKV_F3
     }
   };
 
+  // Tiles that every query sees whole, then the others: the steps are two programs, so that the first has no branches for what the second has to look after (in one, with copies of
+  // the sums where its ways met, 32768 tokens took 8.90 ms).
   uint32_t buf = lds, other = lds + 2 * A::kTileBytes;
-  if constexpr (A::kNarrow) {
-    typename A::Fetched f;
-    if (w.begin < w.end) {
-      A::fetch(f, w, w.begin, w.end);
-      A::put(f, buf);
-    }
-    for (int key0 = w.begin; key0 < w.end; key0 += A::kKeys) {
-      const bool more = key0 + A::kKeys < w.end;
-      if (more) A::fetch(f, w, key0 + A::kKeys, w.end);
-      __syncthreads();
-      if (busy) step(key0, buf);
-      if (more) A::put(f, other);
-      const uint32_t t = buf;
-      buf = other;
-      other = t;
-    }
-  } else {
-    if (w.begin < w.end) A::stage(w, w.begin, w.end, buf);
-    for (int key0 = w.begin; key0 < w.end; key0 += A::kKeys) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (key0 + A::kKeys < w.end) A::stage(w, key0 + A::kKeys, w.end, other);
-      if (busy) step(key0, buf);
-      const uint32_t t = buf;
-      buf = other;
-      other = t;
+  int key0 = w.begin;
+  const int whole_end = w.begin + max(min(all, w.end) - w.begin, 0) / A::kKeys * A::kKeys;
+  typename A::Fetched raw;
+  if (w.begin < w.end) {
+    if constexpr (A::kNarrow) {
+      A::fetch(raw, w, w.begin, w.end);
+      A::put(raw, buf);
+    } else {
+      A::stage(w, w.begin, w.end, buf);
     }
   }
+  auto run = [&](auto tail_c, int until) __attribute__((always_inline)) {
+    for (; key0 < until; key0 += A::kKeys) {
+      const bool more = key0 + A::kKeys < w.end;
+      if constexpr (A::kNarrow) {
+        if (more) A::fetch(raw, w, key0 + A::kKeys, w.end);
+        __syncthreads();
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (more) A::stage(w, key0 + A::kKeys, w.end, other);
+      }
+      if (busy) step(tail_c, key0, buf);
+      if constexpr (A::kSingle) {
+        __syncthreads();
+        if (more) A::put(raw, buf);
+        continue;
+      }
+      if constexpr (A::kNarrow) {
+        if (more) A::put(raw, other);
+      }
+      const uint32_t t = buf;
+      buf = other;
+      other = t;
+    }
+  };
+  run(std::integral_constant<bool, false>{}, whole_end);
+  run(std::integral_constant<bool, true>{}, w.end);
 
   // The waves that share queries are put together, and the outputs turned round, through LDS.
   const bool whole = w.parts == 1;
   const int slot = w.slot0 + w.part * w.slot_step;
   float* const sh_o = (float*)sh;
+  const float total = sum + __shfl_xor(sum, 32);
+  __syncthreads();                                   // (the last tile has been read)
+  if (g == 0) {
+    sh_m[wk][wq * 32 + l32] = ref;
+    sh_l[wk][wq * 32 + l32] = total;
+  }
+  if constexpr (WK > 1) __syncthreads();
+  float f = 1.f;
+  if constexpr (WK > 1) {
+    float top = -INFINITY;
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const float total = sum[qt] + __shfl_xor(sum[qt], 32);
-    __syncthreads();                                   // (the last tile, or the tile of queries before, has been read)
-    if (g == 0) {
-      sh_m[wk][wq * 32 + l32] = ref[qt];
-      sh_l[wk][wq * 32 + l32] = total;
+    for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_m[i][wq * 32 + l32]);
+    // (a wave that saw nothing has a sum of 0, or NaN where a product was NaN)
+    f = ref == -INFINITY ? 1.f : exp2_fast(ref - top);
+  }
+#pragma unroll
+  for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(f32x4*)&sh_o[((wk * WQ + wq) * 32 + l32) * A::kOutRow + dt * 32 + i * 8 + 4 * g] =
+          f32x4{acc[dt][i * 4], acc[dt][i * 4 + 1], acc[dt][i * 4 + 2], acc[dt][i * 4 + 3]} * f;
+  __syncthreads();
+  constexpr int kLanes = D / 4;                      // threads of a row of outputs
+  for (int idx = threadIdx.x; idx < 32 * WQ * kLanes; idx += A::kThreads) {
+    const int r = idx / kLanes, d0 = idx % kLanes * 4;    // row of the tile, dims
+    if (w.r0 + r >= w.rows) continue;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < WK; ++i) {
+      o += *(const f32x4*)&sh_o[(i * WQ * 32 + r) * A::kOutRow + d0];
+      top = fmaxf(top, sh_m[i][r]);
     }
-    if constexpr (WK > 1) __syncthreads();
-    float f = 1.f;
-    if constexpr (WK > 1) {
-      float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_m[i][wq * 32 + l32]);
-      // (a wave that saw nothing has a sum of 0, or NaN where a product was NaN)
-      f = ref[qt] == -INFINITY ? 1.f : exp2_fast(ref[qt] - top);
-    }
-#pragma unroll
-    for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *(f32x4*)&sh_o[((wk * WQ + wq) * 32 + l32) * A::kOutRow + dt * 32 + i * 8 + 4 * g] =
-            f32x4{acc[qt][dt][i * 4], acc[qt][dt][i * 4 + 1], acc[qt][dt][i * 4 + 2], acc[qt][dt][i * 4 + 3]} * f;
-    __syncthreads();
-    constexpr int kLanes = D / 4;                      // threads of a row of outputs
-    for (int idx = threadIdx.x; idx < 32 * WQ * kLanes; idx += A::kThreads) {
-      const int row = idx / kLanes, d0 = idx % kLanes * 4;
-      const int r = row / 32 * 32 * QT + qt * 32 + row % 32;          // row of the tile
-      if (w.r0 + r >= w.rows) continue;
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-      float top = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int i = 0; i < WK; ++i) {
-        o += *(const f32x4*)&sh_o[(i * WQ * 32 + row) * A::kOutRow + d0];
-        top = fmaxf(top, sh_m[i][row]);
-      }
-#pragma unroll
-      for (int i = 0; i < WK; ++i) l += sh_l[i][row] * (WK == 1 || sh_m[i][row] == -INFINITY ? 1.f : exp2_fast(sh_m[i][row] - top));
-      if (whole) {
-        const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
-        const bool none = sees_none(w, t, bits_of(w, t, a.T));
-        store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
-        if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
-      } else {
-        *(f32x4*)(a.part_o + ((int64_t)slot * A::kQueries + r) * D + d0) = o;
-        if (d0 == 0) *(f32x2*)(a.part_ml + ((int64_t)slot * A::kQueries + r) * 2) = f32x2{top, l};
-      }
+    for (int i = 0; i < WK; ++i) l += sh_l[i][r] * (WK == 1 || sh_m[i][r] == -INFINITY ? 1.f : exp2_fast(sh_m[i][r] - top));
+    if (whole) {
+      const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
+      const bool none = sees_none(w, t, bits_of(w, t, a.T));
+      store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
+      if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
+    } else {
+      *(f32x4*)(a.part_o + ((int64_t)slot * A::kQueries + r) * D + d0) = o;
+      if (d0 == 0) *(f32x2*)(a.part_ml + ((int64_t)slot * A::kQueries + r) * 2) = f32x2{top, l};
     }
   }
 }
 
-// The parts of a tile put together, in their order.  The workgroup of part p takes every parts'th group of rows.
-template <int KIND, int D, int QT, int WQ, int WK, class TAB>
+// The parts of a tile put together, in their order.  The workgroups of a part (join_slices() of them) take every so many'th group of rows.  Bound by latency: all references and sums of a row are asked for at once,
+// by the lanes that share the row, and of the outputs eight parts at a time.
+template <int KIND, int D, int WQ, int WK, class TAB>
 __global__ __launch_bounds__(256) void join_tiles_kernel(const TileArgs a, const TAB tab) {
-  using A = Tiles<KIND, D, QT, WQ, WK>;
+  using A = Tiles<KIND, D, WQ, WK>;
   const TileWork w = tab.template find<A::kQueries, A::kKeys, D, KIND>(a, (int)blockIdx.x);
   if (w.parts == 1 || w.part >= w.parts) return;
-  constexpr int kLanes = D / 4, kRows = 256 / kLanes;
-  const int t0 = w.r0 / a.G, rem0 = w.r0 % a.G, d0 = threadIdx.x % kLanes * 4;
-  for (int r = w.part * kRows + threadIdx.x / kLanes; r < A::kQueries && w.r0 + r < w.rows; r += w.parts * kRows) {
-    float top = -INFINITY, l = 0.f;
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes, kAtOnce = 8;
+  const int t0 = w.r0 / a.G, rem0 = w.r0 % a.G, lane = threadIdx.x % kLanes, d0 = lane * 4;
+  const int turn = w.parts * (int)gridDim.y * kRows;
+  for (int r = (w.part * (int)gridDim.y + (int)blockIdx.y) * kRows + threadIdx.x / kLanes; r < A::kQueries && w.r0 + r < w.rows; r += turn) {
+    auto at = [&](int p) __attribute__((always_inline)) { return (int64_t)(w.slot0 + p * w.slot_step) * A::kQueries + r; };
+    f32x4 x[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) x[i] = *(const f32x4*)(a.part_o + at(min(i, w.parts - 1)) * D + d0);
+    // the lane's parts: lane, lane + kLanes, ..
+    f32x2 ml = f32x2{-INFINITY, 0.f};
+    if (lane < w.parts) ml = *(const f32x2*)(a.part_ml + at(lane) * 2);
+    float top = ml[0];
+    for (int p = lane + kLanes; p < w.parts; p += kLanes) top = fmaxf(top, a.part_ml[at(p) * 2]);
+    top = reduce_lanes(top, kLanes, [](float u, float v) { return fmaxf(u, v); });
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < w.parts; ++p) top = fmaxf(top, a.part_ml[((int64_t)(w.slot0 + p * w.slot_step) * A::kQueries + r) * 2]);
-    for (int p = 0; p < w.parts; ++p) {
-      const int64_t at = (int64_t)(w.slot0 + p * w.slot_step) * A::kQueries + r;
-      const f32x2 ml = *(const f32x2*)(a.part_ml + at * 2);
+    float l = 0.f;
+    for (int p0 = 0; p0 < w.parts; p0 += kLanes) {     // (kLanes is a multiple of kAtOnce)
+      if (p0 && p0 + lane < w.parts) ml = *(const f32x2*)(a.part_ml + at(p0 + lane) * 2);
       const float f = ml[0] == -INFINITY ? 1.f : exp2_fast(ml[0] - top);
-      l += ml[1] * f;
-      o += *(const f32x4*)(a.part_o + at * D + d0) * f;
+      if (p0 + lane < w.parts) l += ml[1] * f;
+      for (int q0 = p0; q0 < min(w.parts, p0 + kLanes); q0 += kAtOnce) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const float fi = __shfl(f, ((int)threadIdx.x & ~(kLanes - 1)) + q0 - p0 + i);
+          if (q0 + i < w.parts) o += x[i] * fi;
+        }
+        if (q0 + kAtOnce < w.parts) {
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) x[i] = *(const f32x4*)(a.part_o + at(min(q0 + kAtOnce + i, w.parts - 1)) * D + d0);
+        }
+      }
     }
+    l = reduce_lanes(l, kLanes, [](float u, float v) { return u + v; });
     const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
     const bool none = sees_none(w, t, bits_of(w, t, a.T));
     store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
     if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
   }
 }
+
+// ------------------------------------------------------------------ host
+
+// Waves of a workgroup: along the queries, along the keys of a staged tile.
+struct TileShape { int wq, wk; };
+constexpr TileShape kTileShapes[] = {{1, 4}, {2, 2}, {4, 1}, {4, 2}, {8, 1}};
+constexpr int kTileShapeCount = 5;
+inline int tile_queries(int shape) { return 32 * kTileShapes[shape].wq; }
+
+// f with the waves of a shape as compile-time constants.  fp32 has two shapes: others do not fit LDS or registers.
+template <int KIND, class F>
+void with_shape(int shape, F f) {
+  using std::integral_constant;
+  integral_constant<int, 1> one;
+  integral_constant<int, 2> two;
+  integral_constant<int, 4> four;
+  if constexpr (KIND != SLKV_F32) {
+    if (shape == 0) return f(one, four);
+    if (shape == 3) return f(four, two);
+    if (shape == 4) return f(integral_constant<int, 8>{}, one);
+  }
+  if (shape == 1) return f(two, two);
+  f(four, one);
+}
+
+// What a call consists of in a shape: workgroups without parts, keys of all and of the longest.
+struct TileLoad { double tiles, keys, longest; };
+struct TileChoice { int shape; int64_t each; };        // each: keys of a part, at most
+
+// The shape and the parts that should be done first.  A workgroup takes kBegin us and, for every 64 keys (128: shape 0), alone[shape] us on a CU that it has to itself, loaded[shape] where all places are
+// taken; longer where nobody else reads the same rows.  The keys and values of all segments (bytes) come at 4.8 TB/s at best; parts cost a second launch, and their sums are written and read.
+// (us, bf16, d = 128, 32 heads, 8 KV heads: 32768 tokens in shape 4 7800, in 2 7900; 4096: 143, 152, in shape 1 169; 1024: 28 in shape 2, 22 in shape 1, 44 in shape 0; 130: 11.6, 9.2, 8.0;
+// 128 queries a segment on 128 segments of 1024 rows: 35 in shape 3 with parts of 900, 40 in shape 2, 38 in it with parts of 600, 53 of 200; 64 on 512 segments of 1024 MXFP4 rows: 55 in shape 1 whole, 102 with parts of 200.)
+template <class LOAD>
+TileChoice choose_tiles(int dtype, int d, int64_t rows, int64_t segments, double bytes, LOAD load) {
+  constexpr double kBegin = 5.5, kJoin = 6;
+  constexpr double kShared[] = {1.45, 0.85, 1.25, 1.2, 1.9}, kStreaming[] = {1.8, 1.5, 1.9, 1.4, 2.1}, kLoaded[] = {1.45, 1.24, 1.94, 1.2, 1.9};
+  constexpr int kKeys[] = {128, 64, 64, 64, 64}, kPlaces[] = {1, 2, 2, 1, 1};
+  const bool f32 = dtype == SLKV_F32, narrow = kind_bits(dtype) < 16;
+  TileChoice best{2, 1};
+  double least = 1e300;
+  for (int s = 0; s < kTileShapeCount; ++s) {
+    if (f32 && s != 1 && s != 2) continue;
+    if (s > 0 && rows <= tile_queries(s) / 2 && !(f32 && s == 1)) continue;   // (no more waves than queries)
+    if (d == 64 && s == 4) continue;                             // (8192 tokens in fp16: 354 us, 320 in shape 2)
+    const TileLoad l = load(tile_queries(s));
+    const double scale = (f32 ? (d == 64 ? 4 : 8) * (s == 1 ? 0.78 : 1) : d == 64 ? 0.55 : 1) * (narrow ? 1.2 : 1);
+    const double alone = (l.tiles < 4.0 * segments && !f32 ? kStreaming[s] : kShared[s]) * scale, loaded = f32 ? alone : std::max(kLoaded[s] * scale, alone) * (narrow && s == 0 ? 2 : 1);
+    const double places = 256.0 * (f32 ? 1 : narrow && s == 0 ? 2 : kPlaces[s]);
+    const bool even = l.keys > 0.95 * l.longest * l.tiles;
+    for (int parts = 1; parts <= 256; parts += parts < 4 ? 1 : parts / 2) {
+      const double each = std::ceil(std::ceil(l.longest / parts) / kKeys[s]) * kKeys[s];
+      const double groups = l.tiles * (parts == 1 ? 1 : even ? std::ceil(l.longest / each) : std::max(1.0, l.keys / l.tiles / each + 0.4));
+      const double steps = l.keys / kKeys[s] + 0.5 * groups, mean = std::min(1.0, steps / groups / (each / kKeys[s]));
+      const double one = each / kKeys[s] * (groups <= 256 ? alone : alone + (loaded - alone) * mean);
+      // (more workgroups than places: the last ones begin late; parts are about equal, whole tiles the longest first)
+      const double all = steps * loaded / places + (groups <= places ? 0 : parts > 1 ? 0.5 * one : 0.1 * one);
+      double us = kBegin + std::max(std::max(one, all), bytes / 4.8e6 + (parts > 1 || l.tiles < places ? 0.2 * one : 0));
+      if (parts > 1) us += kJoin + groups * tile_queries(s) * d * 8 / 6e6;
+      if (us < least) least = us, best = TileChoice{s, (int64_t)std::max(each, 1.0)};
+      if (each <= kKeys[s]) break;
+    }
+  }
+  return best;
+}
+
+// Workgroups of a part that join tiles.
+inline unsigned join_slices(int queries) { return (unsigned)std::max(1, queries / 32); }
 
 }  // namespace slkv
 #endif

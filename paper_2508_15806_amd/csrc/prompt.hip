@@ -69,21 +69,25 @@ static PromptPlan plan_prompt(const slkv_prompt_desc* d) {
   PromptPlan p;
   const int64_t G = d->Hq / d->Hkv;
   const int64_t* ck = cu_k_of(d);
-  int64_t rows = 0;
-  for (int64_t b = 0; b < d->B; ++b) rows = std::max(rows, (d->h_cu_q[b + 1] - d->h_cu_q[b]) * G);
-  p.shape = rows <= 32 && d->dtype != SLKV_F32 ? 0 : rows <= 64 ? 1 : 2;
-  p.queries = 32 << p.shape;
-  const int64_t places = 256 * (p.shape == 0 || d->dtype == SLKV_F32 ? 1 : 2);
-  int64_t tiles = 0, keys = 0, most = 0;
-  for (int64_t b = 0; b < d->B; ++b) {
-    const int64_t t = seq_tiles(d, b, p.queries) * d->Hkv, n = d->h_cu_q[b + 1] - d->h_cu_q[b], m = ck[b + 1] - ck[b];
-    tiles += t;
-    keys += t * std::max<int64_t>(1, m - n / 2);
-    if (t) most = std::max(most, m);
-  }
-  p.each = std::max<int64_t>(1, most);
-  if (tiles < places) p.each = std::max<int64_t>(256, (keys + places - 1) / places);
-  p.split = most > p.each;
+  int64_t rows = 0, kv = 0;
+  for (int64_t b = 0; b < d->B; ++b) rows = std::max(rows, (d->h_cu_q[b + 1] - d->h_cu_q[b]) * G), kv += ck[b + 1] - ck[b];
+  const TileChoice c = choose_tiles(d->dtype, d->d, rows, (int64_t)d->B * d->Hkv, (double)kv * d->Hkv * d->d * kind_bits(d->dtype) / 4, [&](int queries) {
+    TileLoad l{0, 0, 1};
+    for (int64_t b = 0; b < d->B; ++b) {
+      const int64_t t = seq_tiles(d, b, queries) * d->Hkv, n = d->h_cu_q[b + 1] - d->h_cu_q[b], m = ck[b + 1] - ck[b];
+      if (!t) continue;
+      l.tiles += t;
+      l.keys += (double)t * std::max<int64_t>(1, m - n / 2);
+      l.longest = std::max(l.longest, (double)m);
+    }
+    l.tiles = std::max(l.tiles, 1.0);
+    return l;
+  });
+  p.shape = c.shape;
+  p.each = c.each;
+  p.queries = tile_queries(p.shape);
+  p.split = false;
+  for (int64_t b = 0; b < d->B; ++b) p.split |= seq_tiles(d, b, p.queries) && seq_parts(d, b, p.each) > 1;
   p.slots = 0;
   for (int64_t b0 = 0; b0 < d->B; b0 += PromptTab::kSeqs) {
     int64_t here = 0;
@@ -96,7 +100,8 @@ static PromptPlan plan_prompt(const slkv_prompt_desc* d) {
   return p;
 }
 
-static slkv_status prompt_checks(const slkv_prompt_desc* d) {
+// Everything that can be checked without the arrays; the plan of a descriptor that passes.
+static slkv_status prompt_checks(const slkv_prompt_desc* d, PromptPlan& plan) {
   if (!d) return fail(SLKV_ERR_NULL, "desc is NULL");
   if (d->struct_size != sizeof(slkv_prompt_desc)) return fail(SLKV_ERR_BAD_ARG, "desc.struct_size %u != %zu", d->struct_size, sizeof(slkv_prompt_desc));
   if (d->dtype < SLKV_F32 || d->dtype > SLKV_BF16_KV_MXFP4) return fail(SLKV_ERR_BAD_ARG, "unknown dtype %d", d->dtype);
@@ -123,7 +128,8 @@ static slkv_status prompt_checks(const slkv_prompt_desc* d) {
   const int64_t G = d->Hq / d->Hkv;
   for (int64_t b = 0; b < d->B; ++b)
     if ((d->h_cu_q[b + 1] - d->h_cu_q[b]) * G >= (int64_t(1) << 31) - 512) return fail(SLKV_ERR_UNSUPPORTED, "sequence %lld: 2^31 - 512 query rows of a KV head and more", (long long)b);
-  if (plan_prompt(d).slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
+  plan = plan_prompt(d);
+  if (plan.slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
   return SLKV_OK;
 }
 
@@ -134,16 +140,18 @@ using namespace slkv;
 extern "C" slkv_status slkv_prompt_workspace_bytes(const slkv_prompt_desc* desc, size_t* bytes) {
   clear_error();
   if (!bytes) return fail(SLKV_ERR_NULL, "bytes is NULL");
-  const slkv_status st = prompt_checks(desc);
+  PromptPlan p;
+  const slkv_status st = prompt_checks(desc, p);
   if (st != SLKV_OK) return st;
-  *bytes = plan_prompt(desc).bytes;
+  *bytes = p.bytes;
   return SLKV_OK;
 }
 
 extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const void* d_q, const void* d_k, const void* d_v, void* d_out, float* d_lse,
                                           void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   clear_error();
-  const slkv_status st = prompt_checks(desc);
+  PromptPlan p;
+  const slkv_status st = prompt_checks(desc, p);
   if (st != SLKV_OK) return st;
   const int64_t* ck = cu_k_of(desc);
   const int64_t queries = desc->h_cu_q[desc->B] - desc->h_cu_q[0], keys = ck[desc->B] - ck[0];
@@ -151,7 +159,6 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
   const void* ptrs[] = {d_q, d_k, d_v, d_out, d_lse, d_workspace};
   for (const void* ptr : ptrs)
     if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);
-  const PromptPlan p = plan_prompt(desc);
   if (workspace_bytes < p.bytes) return fail(SLKV_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, p.bytes);
   const int wide = wide_bytes(desc->dtype), narrow = desc->dtype == SLKV_BF16_KV_FP8 ? 1 : wide;
   TileArgs a;
@@ -190,31 +197,23 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
     }
     t.first[t.nseq] = (int32_t)blocks;
     if (!blocks) continue;
-    auto launch = [&](auto kind, auto dim, auto qt, auto wq, auto wk) {
-      constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value, kQT = decltype(qt)::value, kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
-      {
-        ScopedKernelTimer timer(SLKV_K_PROMPT);
-        SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kQT, kWQ, kWK, PromptTab>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
-      }
-      if (p.split) {
-        ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
-        SLKV_LAUNCH((join_tiles_kernel<kKind, kDim, kQT, kWQ, kWK, PromptTab>), dim3((unsigned)blocks), dim3(256), 0, stream, a, t);
-      }
-    };
-    auto with_shape = [&](auto kind, auto dim) {
-      using std::integral_constant;
-      integral_constant<int, 1> one;
-      integral_constant<int, 2> two;
-      integral_constant<int, 4> four;
-      if constexpr (decltype(kind)::value != SLKV_F32) {
-        if (p.shape == 0) return launch(kind, dim, one, one, four);
-      }
-      if (p.shape == 1) return launch(kind, dim, one, two, two);
-      launch(kind, dim, one, four, one);
+    auto launch = [&](auto kind, auto dim) {
+      constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
+      with_shape<kKind>(p.shape, [&](auto wq, auto wk) {
+        constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
+        {
+          ScopedKernelTimer timer(SLKV_K_PROMPT);
+          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTab>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+        }
+        if (p.split) {
+          ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
+          SLKV_LAUNCH((join_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTab>), dim3((unsigned)blocks, join_slices(p.queries)), dim3(256), 0, stream, a, t);
+        }
+      });
     };
     auto with_dim = [&](auto kind) {
-      if (desc->d == 64) with_shape(kind, std::integral_constant<int, 64>{});
-      else with_shape(kind, std::integral_constant<int, 128>{});
+      if (desc->d == 64) launch(kind, std::integral_constant<int, 64>{});
+      else launch(kind, std::integral_constant<int, 128>{});
     };
     switch (desc->dtype) {
       case SLKV_F32: with_dim(std::integral_constant<int, SLKV_F32>{}); break;

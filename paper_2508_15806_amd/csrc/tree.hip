@@ -8,28 +8,41 @@ namespace slkv {
 
 // ------------------------------------------------------------------ attention
 
-// Segments of a launch: first rows of their rooms, workgroups before them.  Workgroups of a segment: parts of its rows, in each of them the tiles of queries.
+// Segments of a launch: first rows of their rooms, the order in which they are launched, and how many parts come before every 16th of it; a segment has
+// max(1, ceil(room / each)).  Workgroups: parts, in each of them the tiles of queries.
 template <int N>
 struct TreeTab {
-  static constexpr int kSegs = N;
+  static constexpr int kSegs = N, kGroup = 16, kGroups = (N + kGroup - 1) / kGroup;
+  static_assert(kGroups <= kWave, "a lane for every group");
   const unsigned char *k, *v, *k_scale, *v_scale, *q;
   unsigned char* out;
   float* lse;
   const uint64_t* sees;
   const int32_t* lengths;
-  int32_t nseg, seg0, hkv;
-  int32_t start[N + 1], first[N + 1];
+  int32_t nseg, seg0, hkv, each;
+  int32_t start[N + 1], before[kGroups];
+  uint16_t order[N];
 
   template <int QUERIES, int KEYS, int D, int KIND>
   __device__ __forceinline__ TileWork find(const TileArgs& a, int block) const {
-    const int s = find_segment_wave(nseg, block, [&](int i) { return first[i]; });
-    const int seg = seg0 + s, b = seg / hkv, h = seg % hkv, at = start[s], room = start[s + 1] - at;
-    const int tiles = (a.G * a.T + QUERIES - 1) / QUERIES, i = block - first[s], parts = (first[s + 1] - first[s]) / tiles;
+    const int tiles = (a.G * a.T + QUERIES - 1) / QUERIES, part_id = block / tiles, lane = threadIdx.x % kWave;
+    const int groups = (nseg + kGroup - 1) / kGroup;
+    const int b0 = before[min(lane, groups - 1)];
+    const int grp = __popcll(__ballot(lane < groups && b0 <= part_id)) - 1;
+    const int in_group = order[min(grp * kGroup + min(lane, kGroup - 1), nseg - 1)];
+    const int at_lane = start[in_group], room_lane = start[in_group + 1] - at_lane;
+    const bool in = lane < kGroup && grp * kGroup + lane < nseg;
+    const int parts_lane = in ? max(1, (room_lane + each - 1) / each) : 0;
+    const int first_lane = __builtin_amdgcn_readlane(b0, grp) + (int)wave_incl_scan((uint32_t)parts_lane) - parts_lane;
+    const int which = __popcll(__ballot(in && first_lane <= part_id)) - 1;
+    const int s = __builtin_amdgcn_readlane(in_group, which), at = __builtin_amdgcn_readlane(at_lane, which), room = __builtin_amdgcn_readlane(room_lane, which);
+    const int parts = __builtin_amdgcn_readlane(parts_lane, which), first = __builtin_amdgcn_readlane(first_lane, which);
+    const int seg = seg0 + s, b = seg / hkv, h = seg % hkv, tile = block - part_id * tiles;
     constexpr int kRow = D * Kind<KIND>::kBits / 8, kWide = D * (int)sizeof(typename Kind<KIND>::wide), kScales = D / kScaleBlock;
     TileWork w;
-    w.part = i / tiles;
+    w.part = part_id - first;
     w.rows = a.G * a.T;
-    w.r0 = i % tiles * QUERIES;
+    w.r0 = tile * QUERIES;
     w.n = __builtin_amdgcn_readfirstlane(rows_in_use(lengths, seg, room));
     w.hist = w.n - a.T;
     // the rows in use are spread over the parts of the room
@@ -50,12 +63,12 @@ struct TreeTab {
     w.q_head = w.o_head = (int64_t)a.T * kWide;
     w.lse_head = a.T;
     w.k_row = w.v_row = kRow;
-    w.slot0 = first[s] + i % tiles;
+    w.slot0 = first * tiles + tile;
     w.slot_step = tiles;
     return w;
   }
 };
-constexpr int kTreeSegs = 480;
+constexpr int kTreeSegs = 600;
 
 struct TreePlan {
   int shape, queries;
@@ -72,13 +85,16 @@ static int64_t tree_parts(const slkv_cache_desc* d, int64_t s, int64_t each) {
 static TreePlan plan_tree(const slkv_cache_desc* d, int T) {
   TreePlan p;
   const int64_t S = (int64_t)d->B * d->Hkv, R = (int64_t)(d->Hq / d->Hkv) * T, rows = d->h_offsets[S] - d->h_offsets[0];
-  p.shape = R <= 32 && d->dtype != SLKV_F32 ? 0 : R <= 64 ? 1 : 2;
-  p.queries = 32 << p.shape;
-  const int64_t tiles = (R + p.queries - 1) / p.queries, places = 256 * (p.shape == 0 || d->dtype == SLKV_F32 ? 1 : 2);
   int64_t most = 1;
   for (int64_t s = 0; s < S; ++s) most = std::max(most, d->h_offsets[s + 1] - d->h_offsets[s]);
-  p.each = most;
-  if (S * tiles < 2 * places) p.each = std::max<int64_t>(256, (rows * tiles + places - 1) / places);
+  const TileChoice c = choose_tiles(d->dtype, d->d, R, S, (double)rows * d->d * kind_bits(d->dtype) / 4, [&](int queries) {
+    const double tiles = (double)((R + queries - 1) / queries);
+    return TileLoad{S * tiles, std::max<double>(1, (double)rows) * tiles, (double)most};
+  });
+  p.shape = c.shape;
+  p.each = std::min(most, c.each);
+  p.queries = tile_queries(p.shape);
+  const int64_t tiles = (R + p.queries - 1) / p.queries;
   p.split = most > p.each;
   p.slots = 0;
   for (int64_t s0 = 0; s0 < S; s0 += kTreeSegs) {
@@ -92,12 +108,30 @@ static TreePlan plan_tree(const slkv_cache_desc* d, int T) {
   return p;
 }
 
-static slkv_status tree_checks(const slkv_cache_desc* desc, int32_t T) {
+// The segments with the longest parts first, by sixteenths of the longest.
+template <class TAB>
+static void order_segments(TAB& t) {
+  constexpr int kSteps = 16;
+  int from[kSteps + 1] = {};
+  uint8_t key[TAB::kSegs];
+  auto length = [&](int i) {
+    const int64_t room = t.start[i + 1] - t.start[i], parts = std::max<int64_t>(1, (room + t.each - 1) / t.each);
+    return (room + parts - 1) / parts;
+  };
+  int64_t most = 1;
+  for (int i = 0; i < t.nseg; ++i) most = std::max(most, length(i));
+  for (int i = 0; i < t.nseg; ++i) ++from[(key[i] = (uint8_t)(kSteps - 1 - length(i) * (kSteps - 1) / most)) + 1];
+  for (int k = 0; k < kSteps; ++k) from[k + 1] += from[k];
+  for (int i = 0; i < t.nseg; ++i) t.order[from[key[i]]++] = (uint16_t)i;
+}
+
+static slkv_status tree_checks(const slkv_cache_desc* desc, int32_t T, TreePlan& plan) {
   slkv_status st = validate_cache_desc(desc);
   if (st != SLKV_OK) return st;
   if (T < 1) return fail(SLKV_ERR_BAD_ARG, "T must be >= 1");
   if (T > 64) return fail(SLKV_ERR_UNSUPPORTED, "T = %d > 64", T);
-  if (plan_tree(desc, T).slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
+  plan = plan_tree(desc, T);
+  if (plan.slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
   return SLKV_OK;
 }
 
@@ -108,23 +142,24 @@ using namespace slkv;
 extern "C" slkv_status slkv_tree_workspace_bytes(const slkv_cache_desc* desc, int32_t T, size_t* bytes) {
   clear_error();
   if (!bytes) return fail(SLKV_ERR_NULL, "bytes is NULL");
-  const slkv_status st = tree_checks(desc, T);
+  TreePlan p;
+  const slkv_status st = tree_checks(desc, T, p);
   if (st != SLKV_OK) return st;
-  *bytes = plan_tree(desc, T).bytes;
+  *bytes = p.bytes;
   return SLKV_OK;
 }
 
 extern "C" slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, const void* d_q, const uint64_t* d_sees, void* d_out,
                                         float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   clear_error();
-  slkv_status st = tree_checks(desc, T);
+  TreePlan p;
+  slkv_status st = tree_checks(desc, T, p);
   if (st != SLKV_OK) return st;
   if ((st = validate_cache(desc, cache)) != SLKV_OK) return st;
   if (!d_q || !d_sees || !d_out || !d_workspace) return fail(SLKV_ERR_NULL, "a required device pointer is NULL");
   const void* ptrs[] = {d_q, d_sees, d_out, d_lse, d_workspace};
   for (const void* ptr : ptrs)
     if ((uintptr_t)ptr % 16) return fail(SLKV_ERR_BAD_ARG, "device pointer %p not 16-byte aligned", ptr);
-  const TreePlan p = plan_tree(desc, T);
   if (workspace_bytes < p.bytes) return fail(SLKV_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, p.bytes);
   const int64_t S = (int64_t)desc->B * desc->Hkv;
   TileArgs a;
@@ -143,36 +178,31 @@ extern "C" slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_
     t.lse = d_lse, t.sees = d_sees, t.lengths = cache->d_lengths;
     t.nseg = (int32_t)ns, t.seg0 = (int32_t)s0, t.hkv = desc->Hkv;
     int64_t blocks = 0;
-    for (int64_t i = 0; i <= ns; ++i) {
-      t.start[i] = (int32_t)desc->h_offsets[s0 + i];
-      t.first[i] = (int32_t)blocks;
-      if (i < ns) blocks += tree_parts(desc, s0 + i, p.each) * tiles;
+    t.each = (int32_t)p.each;
+    for (int64_t i = 0; i <= ns; ++i) t.start[i] = (int32_t)desc->h_offsets[s0 + i];
+    order_segments(t);
+    for (int64_t i = 0; i < ns; ++i) {
+      if (i % TAB::kGroup == 0) t.before[i / TAB::kGroup] = (int32_t)blocks;
+      blocks += tree_parts(desc, s0 + t.order[i], p.each);
     }
-    auto launch = [&](auto kind, auto dim, auto wq, auto wk) {
-      constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value, kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
-      {
-        ScopedKernelTimer timer(SLKV_K_TREE);
-        SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, 1, kWQ, kWK, TAB>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
-      }
-      if (p.split) {
-        ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
-        SLKV_LAUNCH((join_tiles_kernel<kKind, kDim, 1, kWQ, kWK, TAB>), dim3((unsigned)blocks), dim3(256), 0, stream, a, t);
-      }
+    blocks *= tiles;
+    auto launch = [&](auto kind, auto dim) {
+      constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
+      with_shape<kKind>(p.shape, [&](auto wq, auto wk) {
+        constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
+        {
+          ScopedKernelTimer timer(SLKV_K_TREE);
+          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, TAB>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+        }
+        if (p.split) {
+          ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
+          SLKV_LAUNCH((join_tiles_kernel<kKind, kDim, kWQ, kWK, TAB>), dim3((unsigned)blocks, join_slices(p.queries)), dim3(256), 0, stream, a, t);
+        }
+      });
     };
     with_kind(desc->dtype, [&](auto kind) {
-      auto with_shape = [&](auto dim) {
-        using std::integral_constant;
-        integral_constant<int, 1> one;
-        integral_constant<int, 2> two;
-        integral_constant<int, 4> four;
-        if constexpr (decltype(kind)::value != SLKV_F32) {
-          if (p.shape == 0) return launch(kind, dim, one, four);
-        }
-        if (p.shape == 1) return launch(kind, dim, two, two);
-        launch(kind, dim, four, one);
-      };
-      if (desc->d == 64) with_shape(std::integral_constant<int, 64>{});
-      else with_shape(std::integral_constant<int, 128>{});
+      if (desc->d == 64) launch(kind, std::integral_constant<int, 64>{});
+      else launch(kind, std::integral_constant<int, 128>{});
     });
   };
   if (S <= kFewSegs) launch_table(TreeTab<kFewSegs>{}, 0, S);

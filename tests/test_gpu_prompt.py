@@ -95,6 +95,21 @@ def test_random_shapes(seed):
     run_and_check(rng, DTYPES[seed % 4], Hkv * G, Hkv, int(rng.choice([64, 128])), n.tolist(), m.tolist(), int(rng.integers(0, 4)), int(rng.integers(0, 4)))
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,n", [("bf16", 64, 2, [2000]), ("f16", 128, 4, [1000]), ("bf16_kv8", 128, 2, [1000, 3]), ("bf16_kv8", 128, 2, [500]), ("bf16", 64, 2, [1000]), ("f16", 128, 2, [700, 90]),
+                                            ("f32", 32, 2, [900])])
+def test_enough_queries_for_every_split_of_a_workgroup(dtype, Hq, Hkv, n):
+    """Sizes at which workgroups of 8 waves are taken, along the queries and along the keys; some of the heads are checked."""
+    rng = np.random.default_rng(Hq + n[0])
+    cu = offsets(n)
+    q, k, v = inputs(rng, dtype, Hq, Hkv, 128, cu, cu)
+    out, lse = api.PromptCall(dtype, len(n), Hq, Hkv, 128, cu).run(q, k, v)
+    torch.cuda.synchronize()
+    for h in range(Hkv):
+        G = Hq // Hkv
+        heads = [h * G, h * G + G // 2, h * G + G - 1]
+        check(dtype, 3, 1, 128, cu, cu, q[heads], k[h:h + 1], v[h:h + 1], out[heads], lse[heads])
+
+
 def test_many_sequences():
     # more than one launch holds
     rng = np.random.default_rng(3)

@@ -73,6 +73,27 @@ def test_long_segments_are_split(dtype, G, T):
     check(cache, normal(rng, (2, 2 * G, T, 128), dtype), api.tree_bits(random_parents(rng, 2, T)).cuda())
 
 
+@pytest.mark.parametrize("dtype,Hq,T,S,room", [("bf16", 32, 64, 40, 700), ("bf16_kv4", 32, 64, 40, 700), ("bf16_kv8", 64, 64, 80, 300), ("f16", 64, 50, 80, 600), ("bf16_kv4", 16, 16, 128, 900),
+                                               ("bf16", 16, 32, 200, 400), ("bf16_kv8", 8, 16, 64, 1500), ("f32", 16, 32, 40, 300)])
+def test_enough_queries_for_every_split_of_a_workgroup(dtype, Hq, T, S, room):
+    """Sizes at which workgroups of 8 waves are taken, along the queries and along the keys; the first and the last sequence are checked."""
+    rng = np.random.default_rng(Hq + T)
+    B, d = S // 2, 128
+    lens = [room - (i * 7) % 50 for i in range(S)]
+    cache = random_cache(rng, dtype, B, 2, Hq // 2, d, lens, rooms=[room] * S)
+    q, bits = normal(rng, (B, Hq, T, d), dtype), api.tree_bits(random_parents(rng, B, T)).cuda()
+    out, lse = cache.attend_tree(q, bits)
+    torch.cuda.synchronize()
+    for b in (0, B - 1):
+        rows = slice(b * 2 * room, (b + 1) * 2 * room)
+        part = api.Cache(dtype, 1, Hq, 2, d, [0, room, 2 * room], k=cache.k[rows], v=cache.v[rows], k_scale=None if cache.k_scale is None else cache.k_scale[rows],
+                         v_scale=None if cache.v_scale is None else cache.v_scale[rows], lengths=cache.lengths[2 * b:2 * b + 2])
+        k, v = cache_values(part)
+        heads = [0, Hq // 2 - 1, Hq // 2, Hq - 1]
+        o, l, terms, spread = decode.attend_tree(f64(q[b:b + 1, heads]), k, v, [0, room, 2 * room], lens[2 * b:2 * b + 2], 2, truth(bits[b:b + 1], T))
+        check_outputs(dtype, d, room, out[b:b + 1, heads], lse[b:b + 1, heads], o, l, terms, spread, np.abs(v[np.isfinite(v)]).max(initial=0.0))
+
+
 @pytest.mark.parametrize("S", [90, 700])
 def test_many_segments(S):
     rng = np.random.default_rng(S)
