@@ -2,8 +2,8 @@
 // attention are added up.
 //
 // A segment's workgroups: one for the rows of the draft, which alone reads and writes them, and one for every kWeighRows rows of its room, for the weights of the rows
-// before the draft, which every accepted token sees.  Lengths are read by all of them and set by a launch of their own; without weights there is nothing but the
-// draft, and its workgroup sets the length.
+// before the draft, which every accepted token sees.  The workgroup of the draft sets the length, unless the others read it (drafts behind the rows in use, and weights): a
+// launch of its own does so then.
 #include "attend_rows.h"
 #include "launch.h"
 
@@ -25,17 +25,31 @@ struct AcceptArgs {
   const float* lse;                  // NULL: no weights
   float* w_out;
   int32_t T, A, G, hkv;
+  int32_t lengths_later;             // a launch of their own sets the lengths
   float c_log2;                      // log2(e) / sqrt(d)
 };
 
-// Segments of a launch: first rows of their rooms.
+// Segments of a launch: first rows of their rooms, and workgroups before every 16th of them.
 template <int N>
 struct AcceptTab {
-  static constexpr int kSegs = N;
-  int32_t nseg, seg0;
-  int32_t start[N + 1], first[N + 1];          // workgroups before a segment
+  static constexpr int kSegs = N, kGroup = 16, kGroups = (N + kGroup - 1) / kGroup;
+  static_assert(kGroups <= kWave, "a lane for every group");
+  int32_t nseg, seg0, weights;
+  int32_t start[N + 1], before[kGroups];
+  struct Place { int seg, block, start, room; };
+  __host__ __device__ int blocks_of(int room) const { return 1 + (weights ? (room + kWeighRows - 1) / kWeighRows : 0); }
+  // two round trips to the arguments
+  __device__ __forceinline__ Place find(int block) const {
+    const int lane = threadIdx.x % kWave, groups = (nseg + kGroup - 1) / kGroup;
+    const int b0 = before[min(lane, groups - 1)];
+    const int grp = __popcll(__ballot(lane < groups && b0 <= block)) - 1, i = min(grp * kGroup + min(lane, kGroup - 1), nseg - 1);
+    const int at = start[i], room = start[i + 1] - at, mine = lane < kGroup && grp * kGroup + lane < nseg ? blocks_of(room) : 0;
+    const int first = __builtin_amdgcn_readlane(b0, grp) + (int)wave_incl_scan((uint32_t)mine) - mine;
+    const int which = __popcll(__ballot(mine && first <= block)) - 1;
+    return Place{seg0 + grp * kGroup + which, block - __builtin_amdgcn_readlane(first, which), __builtin_amdgcn_readlane(at, which), __builtin_amdgcn_readlane(room, which)};
+  }
 };
-constexpr int kAcceptSegs = 480;
+constexpr int kAcceptSegs = 880;
 
 // The accepted tokens of a segment whose rows are there: lane i has the i-th one's number; the row of token 0, which may be below 0; how many.
 struct Accepted { int token, base, count; };
@@ -59,93 +73,113 @@ __device__ __forceinline__ Accepted accepted_of(const AcceptArgs& a, int seg, in
   return r;
 }
 
-// Weights of kSteps x Attend::kStep rows from row j0 of the segment on, one wave; those of the draft, from row `drafted` on, are seen by the tokens that were accepted with or after
-// them.  tokens: the accepted ones, in LDS.
+// Weights of kWeighEach rows from row j0 of a segment on, up to `end`, one wave; those of the draft, from row `drafted` on, are seen by the tokens that were accepted with or
+// after them.  tokens: the accepted ones, in LDS.  Bound by latency and by memory: the rows' keys, what they have so far and the first queries are asked for at once, the next queries a tile
+// ahead.  (256 segments of 2048 E4M3 rows, 8 tokens: 27 us, 3.2 TB/s.  A wave that goes through several times as many rows, the next ones on their way in registers: 31 to 44.)
 template <int KIND, int D>
-__device__ __forceinline__ void weigh_rows(const AcceptArgs& a, int seg, int64_t start, int j0, int end, int drafted, int count, const int* tokens) {
+struct Weigh {
   using A = Attend<KIND, D>;
-  constexpr int kSteps = kWeighEach / A::kStep, kProducts = A::kF32 ? D / 4 : D / 32, kEach = A::kEach;
-  if (j0 >= end) return;
-  const int lane = threadIdx.x % kWave, rq = lane & 15, g = lane >> 4, R = count * a.G;
-  typename A::Rows rows;
-  rows.k = A::buffer(a.k, start + j0, end - j0, A::kRowBytes);
-  if constexpr (KIND == SLKV_BF16_KV_MXFP4) rows.ks = A::buffer(a.k_scale, start + j0, end - j0, A::kScales);
-  typename A::KRegs kr[kSteps];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    const typename A::Place place = A::place_of(s, lane);
-    A::load_k(kr[s], rows, place);
-  }
-  float w[kSteps][kEach];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) w[s][j] = 0.f;
-  const bool tail = j0 + kWeighEach > drafted;
-  for (int r0 = 0; r0 < R; r0 += 16) {
-    const int r = min(r0 + rq, R - 1), i = divide(r, a.G), token = tokens[i];
-    const int64_t query = ((int64_t)seg * a.G + (r - i * a.G)) * a.T + token;
-    const unsigned char* p = a.q + query * (D * (int)sizeof(typename A::wide));
-    const float lse = a.lse[query];
-    // (a query that saw nothing has no weights; nor has one that is not there)
-    const float l2 = lse == -INFINITY || r0 + rq >= R ? INFINITY : lse * kLog2e;
-    u32x4 q[A::kF32 ? 1 : kProducts];
-    float qf[A::kF32 ? kProducts : 1];
-    if constexpr (A::kF32) {
-#pragma unroll
-      for (int u = 0; u < kProducts / 4; ++u) *(f32x4*)&qf[u * 4] = *(const f32x4*)(p + A::dim_of(u * 4, g) * 4);
-    } else {
-#pragma unroll
-      for (int u = 0; u < kProducts; ++u) q[u] = *(const u32x4*)(p + A::dim_of(u, g) * 2);
-    }
-    const int sees = drafted + i;                      // the last row that the query sees
+  static constexpr int kSteps = kWeighEach / A::kStep, kProducts = A::kF32 ? D / 4 : D / 32, kEach = A::kEach, kWords = A::kF32 ? kProducts / 4 : kProducts;
+  struct Rows { typename A::KRegs k[kSteps]; float had[kSteps]; };      // had: what the rows have so far; lane rq of 16 has its row rq of every step
+  struct Query { u32x4 w[kWords]; float lse; int sees; };               // sees: the last row that it sees
+
+  static __device__ __forceinline__ void load(Rows& r, const AcceptArgs& a, int64_t start, int j0, int end) {
+    const int lane = threadIdx.x % kWave, rq = lane & 15, g = lane >> 4;
+    typename A::Rows rows;
+    rows.k = A::buffer(a.k, start + j0, end - j0, A::kRowBytes);
+    if constexpr (KIND == SLKV_BF16_KV_MXFP4) rows.ks = A::buffer(a.k_scale, start + j0, end - j0, A::kScales);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      f32x4 x[A::kTiles];
-      if constexpr (A::kF32) {
-        // several sums side by side: one chain of D/4 additions is what the result's error comes from
-        f32x4 y[4];
+      const typename A::Place place = A::place_of(s, lane);
+      A::load_k(r.k[s], rows, place);
+    }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) y[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < kSteps; ++s) {
+      const int row = j0 + s * A::kStep + g * kEach + rq;
+      r.had[s] = a.weight && rq < kEach && row < end ? a.weight[start + row] : 0.f;
+    }
+  }
+
+  static __device__ __forceinline__ void add(const Rows& rows, const AcceptArgs& a, int seg, int64_t start, int j0, int end, int drafted, int count, const int* tokens) {
+    const int lane = threadIdx.x % kWave, rq = lane & 15, g = lane >> 4, R = count * a.G;
+    float w[kSteps][kEach];
 #pragma unroll
-        for (int u = 0; u < kProducts; ++u) y[u % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[s].w[0][u]), qf[u], y[u % 4], 0, 0, 0);
-        x[0] = (y[0] + y[1]) + (y[2] + y[3]);
-      } else {
+    for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int t = 0; t < A::kTiles; ++t) {
-          x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < kEach; ++j) w[s][j] = 0.f;
+    const bool tail = j0 + kWeighEach > drafted;
+    Query ahead;
+    auto load_queries = [&](int r0) __attribute__((always_inline)) {
+      const int r = min(r0 + rq, R - 1), i = divide(r, a.G);
+      const int64_t query = ((int64_t)seg * a.G + (r - i * a.G)) * a.T + tokens[i];
+      const unsigned char* p = a.q + query * (D * (int)sizeof(typename A::wide));
 #pragma unroll
-          for (int u = 0; u < kProducts; ++u) x[t] = A::mfma(A::k_operand(kr[s], t, u), q[u], x[t]);
+      for (int u = 0; u < kWords; ++u) ahead.w[u] = *(const u32x4*)(p + (A::kF32 ? A::dim_of(u * 4, g) * 4 : A::dim_of(u, g) * 2));
+      ahead.lse = a.lse[query];
+      ahead.sees = drafted + i;
+    };
+    if (R > 0) load_queries(0);
+    for (int r0 = 0; r0 < R; r0 += 16) {
+      const Query now = ahead;
+      if (r0 + 16 < R) load_queries(r0 + 16);
+      // (a query that saw nothing has no weights; nor has one that is not there)
+      const float l2 = now.lse == -INFINITY || r0 + rq >= R ? INFINITY : now.lse * kLog2e;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        f32x4 x[A::kTiles];
+        if constexpr (A::kF32) {
+          // several sums side by side: one chain of D/4 additions is what the result's error comes from
+          f32x4 y[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) y[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int u = 0; u < kProducts; ++u)
+            y[u % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(rows.k[s].w[0][u]), __uint_as_float(now.w[u / 4][u % 4]), y[u % 4], 0, 0, 0);
+          x[0] = (y[0] + y[1]) + (y[2] + y[3]);
+        } else {
+#pragma unroll
+          for (int t = 0; t < A::kTiles; ++t) {
+            x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < kProducts; ++u) x[t] = A::mfma(A::k_operand(rows.k[s], t, u), now.w[u], x[t]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          const float e = exp2_fast(fmaf(x[j / 4][j % 4], a.c_log2, -l2));
+          w[s][j] += !tail || j0 + s * A::kStep + g * kEach + j <= now.sees ? e : 0.f;
         }
       }
+    }
+    // over the 16 queries of a row of lanes; lane rq of it gets its row rq
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      float mine = 0.f;
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
-        const float e = exp2_fast(fmaf(x[j / 4][j % 4], a.c_log2, -l2));
-        w[s][j] += !tail || j0 + s * A::kStep + g * kEach + j <= sees ? e : 0.f;
+        const float sum = reduce_lanes(w[s][j], 16, [](float x, float y) { return x + y; });
+        if (j == rq) mine = sum;
       }
+      const int row = j0 + s * A::kStep + g * kEach + rq;
+      if (rq < kEach && row < end) a.w_out[start + row] = rows.had[s] + mine;
     }
   }
-  // over the 16 queries of a row of lanes; lane rq of it gets its row rq
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    float mine = 0.f;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const float sum = reduce_lanes(w[s][j], 16, [](float x, float y) { return x + y; });
-      if (j == rq) mine = sum;
-    }
-    const int row = j0 + s * A::kStep + g * kEach + rq;
-    if (rq < kEach && row < end) a.w_out[start + row] = (a.weight ? a.weight[start + row] : 0.f) + mine;
+
+  static __device__ __forceinline__ void run(const AcceptArgs& a, int seg, int64_t start, int j0, int end, int drafted, int count, const int* tokens) {
+    if (j0 >= end) return;
+    Rows rows;
+    load(rows, a, start, j0, end);
+    add(rows, a, seg, start, j0, end, drafted, count, tokens);
   }
-}
+};
 
 template <int KIND, int D, class TAB>
 __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(const AcceptArgs a, const TAB tab) {
   constexpr int kRow = D * Kind<KIND>::kBits / 8, kUnits = kRow / 16, kScales = D / kScaleBlock;
   constexpr int kMoves = (kMostDraft * kUnits + kAcceptThreads - 1) / kAcceptThreads;   // 16-byte units of K a thread moves
   __shared__ int sh_token[kMostDraft], sh_base, sh_count;
-  const int s = find_segment_wave(tab.nseg, (int)blockIdx.x, [&](int i) { return tab.first[i]; });
-  const int seg = tab.seg0 + s, block = (int)blockIdx.x - tab.first[s], start = tab.start[s], room = tab.start[s + 1] - start;
+  const typename TAB::Place place = tab.find((int)blockIdx.x);
+  const int seg = place.seg, block = place.block, start = place.start, room = place.room;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   if (tid < kWave) {
     const Accepted r = accepted_of(a, seg, room, lane);
@@ -156,7 +190,7 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(const AcceptArgs
   const int base = __builtin_amdgcn_readfirstlane(sh_base), count = __builtin_amdgcn_readfirstlane(sh_count), to = max(base, 0);
   if (block > 0) {                                     // rows before the draft
     const int j0 = (block - 1) * kWeighRows + wave * kWeighEach;
-    weigh_rows<KIND, D>(a, seg, start, j0, min(to, j0 + kWeighEach), to, count, sh_token);
+    Weigh<KIND, D>::run(a, seg, start, j0, min(to, j0 + kWeighEach), to, count, sh_token);
     return;
   }
   // All rows are read before one is written: the path may go through the rows in any order, and more than once through one.
@@ -202,13 +236,11 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(const AcceptArgs
     if (a.pos) a.pos[row] = pos;
     if (a.weight) a.weight[row] = weight;
   }
-  if (!a.lse) {
-    if (tid == 0) a.lengths[seg] = to + count;
-    return;
-  }
+  if (!a.lengths_later && tid == 0) a.lengths[seg] = to + count;
+  if (!a.lse) return;
   __threadfence_block();
   __syncthreads();
-  if (wave == 0) weigh_rows<KIND, D>(a, seg, start, to, to + count, to, count, sh_token);
+  if (wave == 0) Weigh<KIND, D>::run(a, seg, start, to, to + count, to, count, sh_token);
 }
 
 template <class TAB>
@@ -250,14 +282,15 @@ extern "C" slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv
   a.c_log2 = kLog2e / std::sqrt((float)desc->d);
   hipStream_t const stream = (hipStream_t)hip_stream;
   const int64_t S = (int64_t)desc->B * desc->Hkv;
+  a.lengths_later = d_q && (!d_at || d_at == cache->d_lengths);
   auto launch = [&](auto tab, int64_t s0, int64_t ns) {
     using TAB = decltype(tab);
-    tab.nseg = (int32_t)ns, tab.seg0 = (int32_t)s0;
+    tab.nseg = (int32_t)ns, tab.seg0 = (int32_t)s0, tab.weights = d_q != nullptr;
     int64_t blocks = 0;
-    for (int64_t i = 0; i <= ns; ++i) {
-      tab.start[i] = (int32_t)desc->h_offsets[s0 + i];
-      tab.first[i] = (int32_t)blocks;
-      if (i < ns) blocks += 1 + (d_q ? (desc->h_offsets[s0 + i + 1] - desc->h_offsets[s0 + i] + kWeighRows - 1) / kWeighRows : 0);
+    for (int64_t i = 0; i <= ns; ++i) tab.start[i] = (int32_t)desc->h_offsets[s0 + i];
+    for (int64_t i = 0; i < ns; ++i) {
+      if (i % TAB::kGroup == 0) tab.before[i / TAB::kGroup] = (int32_t)blocks;
+      blocks += tab.blocks_of(tab.start[i + 1] - tab.start[i]);
     }
     with_kind(desc->dtype, [&](auto kind) {
       auto with_dim = [&](auto dim) {
@@ -267,7 +300,7 @@ extern "C" slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv
       if (desc->d == 64) with_dim(std::integral_constant<int, 64>{});
       else with_dim(std::integral_constant<int, 128>{});
     });
-    if (d_q) {
+    if (a.lengths_later) {
       ScopedKernelTimer timer(SLKV_K_ACCEPT);
       SLKV_LAUNCH((lengths_kernel<TAB>), dim3((unsigned)((ns + kAcceptWaves - 1) / kAcceptWaves)), dim3(kAcceptThreads), 0, stream, a, tab);
     }

@@ -595,7 +595,7 @@ TileChoice choose_tiles(int dtype, int d, int64_t rows, int64_t segments, double
     for (int parts = 1; parts <= 256; parts += parts < 4 ? 1 : parts / 2) {
       const double each = std::ceil(std::ceil(l.longest / parts) / kKeys[s]) * kKeys[s];
       const double groups = l.tiles * (parts == 1 ? 1 : even ? std::ceil(l.longest / each) : std::max(1.0, l.keys / l.tiles / each + 0.4));
-      const double steps = l.keys / kKeys[s] + 0.5 * groups, mean = std::min(1.0, steps / groups / (each / kKeys[s]));
+      const double steps = l.keys / kKeys[s] + 1.2 * groups, mean = std::min(1.0, steps / groups / (each / kKeys[s]));
       const double one = each / kKeys[s] * (groups <= 256 ? alone : alone + (loaded - alone) * mean);
       // (more workgroups than places: the last ones begin late; parts are about equal, whole tiles the longest first)
       const double all = steps * loaded / places + (groups <= places ? 0 : parts > 1 ? 0.5 * one : 0.1 * one);
