@@ -316,12 +316,18 @@ __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) 
   const int first = wq * 32;                           // the wave's first row of the tile
   const bool busy = w.r0 + first < w.rows;             // (waves without queries only stage)
 
+  // the first rows are on their way before anything else is asked for
+  typename A::Fetched raw;
+  if (w.begin < w.end) {
+    if constexpr (A::kNarrow) A::fetch(raw, w, w.begin, w.end);
+    else A::stage(w, w.begin, w.end, lds);
+  }
   typename A::Queries q;
   const int r_of = max(min(first + l32, w.rows - 1 - w.r0), 0), dt_of = divide(rem0 + r_of, a.G), t_of = t0 + dt_of;   // the lane's row of the tile, its token
-  const uint64_t bits = bits_of(w, t_of, a.T);
   const unsigned char* const q_at = w.q + t_of * w.q_tok + (rem0 + r_of - dt_of * a.G) * w.q_head;
 #pragma unroll
   for (int u = 0; u < (A::kF32 ? D / 8 : D / 16); ++u) q.w[u] = *(const u32x4*)(q_at + u * 32 + g * 16);
+  const uint64_t bits = bits_of(w, t_of, a.T);
 
   float ref = -INFINITY, sum = 0.f;
   f32x16 acc[kDT];
@@ -408,14 +414,8 @@ __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) 
   uint32_t buf = lds, other = lds + 2 * A::kTileBytes;
   int key0 = w.begin;
   const int whole_end = w.begin + max(min(all, w.end) - w.begin, 0) / A::kKeys * A::kKeys;
-  typename A::Fetched raw;
-  if (w.begin < w.end) {
-    if constexpr (A::kNarrow) {
-      A::fetch(raw, w, w.begin, w.end);
-      A::put(raw, buf);
-    } else {
-      A::stage(w, w.begin, w.end, buf);
-    }
+  if constexpr (A::kNarrow) {
+    if (w.begin < w.end) A::put(raw, buf);
   }
   auto run = [&](auto tail_c, int until) __attribute__((always_inline)) {
     for (; key0 < until; key0 += A::kKeys) {
