@@ -16,15 +16,18 @@
  *   Decoding on the compacted cache (the paper's Section 3.4 generates on it; the operators are
  *     standard ones): rows enter it, narrowed to 8 or 4 bits if asked for -> slkv_fill_cache,
  *     slkv_append_cache; the next tokens attend to it                -> slkv_attend_cache
+ *     a tree of drafted tokens attends to it                         -> slkv_attend_tree
+ *     those of them that turn out to be right stay                   -> slkv_accept_cache
  *     rows with the least accumulated attention weight leave it      -> slkv_evict_cache
  *     rows come back as 16-bit values                                -> slkv_cache_rows
+ *   The attention of the prompt itself, whose keys and values Stage 2b chooses from -> slkv_attend_prompt
  *
  * Conventions
  *   - Pointers named d_* are DEVICE pointers, h_* are HOST pointers.  The caller owns every
  *     buffer; the library allocates no device memory.  What it keeps between calls: per device,
  *     that its one-time set-up has been done (slkv_init), and the optional kernel-timing
  *     recorder at the end of this header.
- *   - slkv_score_heads, slkv_compress_layer, slkv_recompress_layer and the calls on a cache only enqueue work on `hip_stream` (a
+ *   - slkv_score_heads, slkv_compress_layer, slkv_recompress_layer, slkv_attend_prompt and the calls on a cache only enqueue work on `hip_stream` (a
  *     hipStream_t passed as void*, NULL = the default stream) and return without
  *     synchronising.  Host-side descriptors are consumed before the call returns.
  *   - Every argument is validated before the first GPU call; on any error nothing is
@@ -68,7 +71,7 @@ const char* slkv_status_str(slkv_status s);
 /* Detail of the last error on the calling thread; valid until its next slkv call. */
 const char* slkv_last_error(void);
 /* ABI version: major * 1000 + minor.  slkv_score_heads_first and slkv_score_heads_qk_first joined 1.5 without a
- * number of their own, and so did the calls on a cache (slkv_fill_cache to slkv_evict_cache): a program that loads the library at run time looks
+ * number of their own, and so did the calls on a cache (slkv_fill_cache to slkv_evict_cache, slkv_attend_tree, slkv_accept_cache) and slkv_attend_prompt: a program that loads the library at run time looks
  * these symbols up. */
 int32_t slkv_version(void);
 /* One-time set-up on the CURRENT device (host pointer arguments: none): raises the LDS limit of
@@ -453,7 +456,7 @@ typedef struct {
   int32_t B, Hq, Hkv, d;       /* d in {64, 128}; Hq % Hkv == 0 */
   int32_t reserved[2];         /* 0 */
   const int64_t* h_cu_q;       /* [B+1] host: queries, non-decreasing, >= 0, last < 2^31 */
-  const int64_t* h_cu_k;       /* [B+1] host: tokens of K and V; NULL: h_cu_q (whole prompts) */
+  const int64_t* h_cu_k;       /* [B+1] host: tokens of K and V, of a sequence 2^30 at most; NULL: h_cu_q (whole prompts) */
   /* element (head, token, :) of an array at head*stride_head + token*stride_tok; rows of d elements contiguous; strides >= 0 and multiples of 16
    * bytes, 0 among them (out: rows may not overlap); token strides of k and v below 2^24 bytes */
   int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head, out_stride_tok, out_stride_head;
@@ -477,7 +480,8 @@ slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const void* d_q, co
  * (two passes, long histories: 1 + 1 + 6 + 1; one pass: 1 + 4 + 3 + 1; histories up to 32768: 1 + 1 + 1 + 1, both passes in
  * one launch 0 + 1 + 1 + 1, one pass 1 + 4 + 1 + 1, in each of these without the last one where the selection copies all rows; ragged
  * caches and batches of many short histories: one SLKV_K_SCORE_ACCUM record in all, where the scoring launch selects and copies too).
- * Fill, append, rows and evict make one each (more beyond 240 segments; 560 and more share a launch whose rooms and rows outside are below 65536); attend one or two for every 600 segments.
+ * Fill, append, rows and evict make one each (more beyond 240 segments; 560 and more share a launch whose rooms and rows outside are below 65536); attend and attend_tree one or two for
+ * every 600 segments, accept for every 880, attend_prompt for every 64 sequences.
  * Process-wide; not meant for production.
  */
 typedef enum {

@@ -172,7 +172,7 @@ class PromptCall(_OnDevice):
         self._lse_like = None
 
     def _rows(self, t, heads, tokens, tdt, name):
-        if self._tensor(t, (heads, tokens, self.d), tdt, name, contiguous=False).stride(2) != 1:
+        if self._tensor(t, (heads, tokens, self.d), tdt, name, contiguous=False).stride(2) != 1 and tokens:
             raise ValueError("%s: rows are not contiguous" % name)
         return t
 

@@ -6,6 +6,7 @@ Usage: python -m paper_2508_15806_amd.build
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -31,16 +32,17 @@ def build(verbose=True):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
-    objs = []
+    cmds = []
     for src in HIP_SOURCES:
-        obj = os.path.join(objdir, src + ".o")
-        run([hipcc] + COMMON + DEVICE + ["-c", os.path.join(CSRC, src), "-o", obj])
-        objs.append(obj)
+        cmds.append([hipcc] + COMMON + DEVICE + ["-c", os.path.join(CSRC, src), "-o", os.path.join(objdir, src + ".o")])
     for src in HOST_SOURCES:
-        obj = os.path.join(objdir, src + ".o")
         # plain C++ (no device pass); host arithmetic (budget allocation) must not be contracted into FMAs
-        run([hipcc] + COMMON + ["-ffp-contract=off", "-x", "c++", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INCLUDE, "-c", os.path.join(CSRC, src), "-o", obj])
-        objs.append(obj)
+        cmds.append([hipcc] + COMMON + ["-ffp-contract=off", "-x", "c++", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INCLUDE, "-c", os.path.join(CSRC, src),
+                                        "-o", os.path.join(objdir, src + ".o")])
+    # the sources side by side: the longest takes as long as all others together
+    with ThreadPoolExecutor(max_workers=min(4, os.cpu_count() or 1)) as pool:
+        list(pool.map(run, cmds))
+    objs = [c[-1] for c in cmds]
     run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs)
     return LIB
 

@@ -127,6 +127,8 @@ static slkv_status prompt_checks(const slkv_prompt_desc* d, PromptPlan& plan) {
   if (n && !by_head && !by_token) return fail(SLKV_ERR_BAD_ARG, "out: rows overlap");
   const int64_t G = d->Hq / d->Hkv;
   for (int64_t b = 0; b < d->B; ++b)
+    if (cu_k_of(d)[b + 1] - cu_k_of(d)[b] > (int64_t(1) << 30)) return fail(SLKV_ERR_UNSUPPORTED, "sequence %lld: more than 2^30 tokens", (long long)b);
+  for (int64_t b = 0; b < d->B; ++b)
     if ((d->h_cu_q[b + 1] - d->h_cu_q[b]) * G >= (int64_t(1) << 31) - 512) return fail(SLKV_ERR_UNSUPPORTED, "sequence %lld: 2^31 - 512 query rows of a KV head and more", (long long)b);
   plan = plan_prompt(d);
   if (plan.slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");

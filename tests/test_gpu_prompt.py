@@ -119,6 +119,15 @@ def test_many_sequences():
     run_and_check(rng, "bf16_kv8", 4, 2, 64, [1] * 150, (n + 1).tolist())
 
 
+def test_no_tokens():
+    for n, m in (([0, 0], None), ([0, 0], [5, 0]), ([3, 0], [0, 0])):
+        cu_q, cu_k = offsets(n), offsets(n if m is None else m)
+        q, k, v = inputs(np.random.default_rng(1), "bf16", 4, 2, 64, cu_q, cu_k)
+        out, lse = api.PromptCall("bf16", 2, 4, 2, 64, cu_q, cu_k).run(q, k, v)
+        torch.cuda.synchronize()
+        assert out.shape == q.shape and bool((out == 0).all()) and bool((lse == -float("inf")).all())
+
+
 def test_rows_outside_the_sequences_stay():
     rng = np.random.default_rng(4)
     cu = offsets([30, 20], 10)
