@@ -44,6 +44,7 @@ struct TileWork {
 
 struct TileArgs {
   int32_t G, T;                           // heads of a segment; tokens (tree)
+  int32_t blocks;                         // tiles and their parts
   float c_log2;                           // log2(e) / sqrt(d)
   float* part_o;                          // [slot][tile row][D], relative to the part's reference
   float* part_ml;                         // [slot][tile row][2]: reference (log2), sum
@@ -78,8 +79,12 @@ struct Tiles {
   // Narrow rows of four subtiles a step: one tile in LDS, the next one in registers, so that two workgroups share a CU.
   static constexpr bool kSingle = kNarrow && WK == 4 && WQ == 1;
   static constexpr int kTilesBytes = (kSingle ? 2 : 4) * kTileBytes;
-  static constexpr int kLds = kTilesBytes > kWaves * 32 * kOutRow * 4 ? kTilesBytes : kWaves * 32 * kOutRow * 4;
-  static constexpr int kPerSimd = KIND == SLKV_F32 || (WQ == 1 && WK == 4 && !kSingle) ? 1 : 2;   // waves of a SIMD, at least
+  // Whether a workgroup takes tiles in turn: not where queries are few and keys many, whose workgroups have enough to do, and no registers to spare for it.
+  static constexpr bool kTurns = WK < 4;
+  static constexpr int kOutBytes = WK == 1 ? 0 : kWaves * 32 * kOutRow * 4;
+  static constexpr int kLds = kTilesBytes > kOutBytes ? kTilesBytes : kOutBytes;
+  // waves of a SIMD, at least: what LDS and registers allow
+  static constexpr int kPerSimd = D == 64 ? (kWaves == 4 && WK < 4 && !kF32 ? 3 : 2) : kF32 || (WQ == 1 && WK == 4 && !kSingle) ? 1 : 2;
   // Reference of fp16 weights: they reach 2^15, so that those down to 2^-26 of the largest keep all their bits.
   static constexpr float kBelow = KIND == SLKV_F16 ? 12.f : 0.f, kBelowPower = KIND == SLKV_F16 ? 0x1p-12f : 1.f;
   static constexpr float kAbove = KIND == SLKV_F16 ? 15.f : 8.f;   // a product this far above the reference moves it
@@ -294,205 +299,301 @@ template <class A>
 __device__ __forceinline__ float tile_lse(float top, float total, bool none) {
   return none ? -INFINITY : total > 0.f ? ((top + A::kBelow) + __builtin_amdgcn_logf(total * A::kBelowPower)) * kLn2 : NAN;
 }
-__device__ __forceinline__ f32x4 tile_output(f32x4 o, float total, bool none) {
-  const float inv = 1.f / total;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = none ? 0.f : total > 0.f ? o[e] * inv : NAN;
-  return o;
-}
+__device__ __forceinline__ float total_scale(float total) { return total > 0.f ? 1.f / total : NAN; }
 
+// Workgroups take tiles in turn: as many workgroups as the chip has places go through them back and forth, so that tiles that get smaller come out even.  The next tile's first rows and queries
+// are on their way while the outputs are written.  (A workgroup for every tile: 17 us beside its steps, of which 6 between two workgroups of a CU, 5 for the first rows, 7 for outputs through LDS; 16 prompts
+// of 1024 tokens 270 us.)
 template <int KIND, int D, int WQ, int WK, class TAB>
 __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) void attend_tiles_kernel(const TileArgs a, const TAB tab) {
   using A = Tiles<KIND, D, WQ, WK>;
   constexpr int kSub = A::kSub, kDT = A::kDT;
   __shared__ __align__(1024) unsigned char sh[A::kLds];
-  __shared__ float sh_m[WK][32 * WQ], sh_l[WK][32 * WQ];
-  const TileWork w = tab.template find<A::kQueries, A::kKeys, D, KIND>(a, (int)blockIdx.x);
-  if (w.part >= w.parts) return;
+  constexpr int kRowsOut = WK > 1 ? 32 * WQ : 1;
+  __shared__ float sh_m[WK][kRowsOut], sh_l[WK][kRowsOut], sh_scale[kRowsOut];
+  __shared__ int64_t sh_at[kRowsOut];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int l32 = lane & 31, g = lane >> 5, wq = wave % WQ, wk = wave / WQ;
-  const int t0 = w.r0 / a.G, rem0 = w.r0 % a.G;        // token and head of the tile's first row
-  const int first = wq * 32;                           // the wave's first row of the tile
-  const bool busy = w.r0 + first < w.rows;             // (waves without queries only stage)
+  const int first = wq * 32;                           // the wave's first row of a tile
 
-  // the first rows are on their way before anything else is asked for
-  typename A::Fetched raw;
-  if (w.begin < w.end) {
-    if constexpr (A::kNarrow) A::fetch(raw, w, w.begin, w.end);
-    else A::stage(w, w.begin, w.end, lds);
+  // The table goes through LDS: one round trip to the arguments, and none for the tiles after the first.
+  __shared__ typename TAB::Words table;
+  {
+    constexpr int kWords = sizeof(typename TAB::Words) / 4;
+    const uint32_t* const from = (const uint32_t*)&tab.words;
+    for (int i = threadIdx.x; i < kWords; i += A::kThreads) ((uint32_t*)&table)[i] = from[i];
+    __syncthreads();
   }
-  typename A::Queries q;
-  const int r_of = max(min(first + l32, w.rows - 1 - w.r0), 0), dt_of = divide(rem0 + r_of, a.G), t_of = t0 + dt_of;   // the lane's row of the tile, its token
-  const unsigned char* const q_at = w.q + t_of * w.q_tok + (rem0 + r_of - dt_of * a.G) * w.q_head;
-#pragma unroll
-  for (int u = 0; u < (A::kF32 ? D / 8 : D / 16); ++u) q.w[u] = *(const u32x4*)(q_at + u * 32 + g * 16);
-  const uint64_t bits = bits_of(w, t_of, a.T);
-
-  float ref = -INFINITY, sum = 0.f;
-  f32x16 acc[kDT];
-#pragma unroll
-  for (int dt = 0; dt < kDT; ++dt) acc[dt] = f32x16{};
-  // keys that every query of the tile sees
-  const int all = w.sees ? w.hist : w.hist + t0 + 1;
-  // bit j: the lane's query sees the key key0 + j, which is there
-  auto seen = [&](int key0) __attribute__((always_inline)) {
-    uint32_t m = first_bits((w.sees ? w.hist : w.hist + t_of + 1) - key0);
-    if (w.sees) {
-      const int u = key0 - w.hist;                     // the draft's first row is bit -u
-      m |= u >= 64 || u <= -32 ? 0u : u >= 0 ? (uint32_t)(bits >> u) : (uint32_t)bits << -u;
+  int turn = 0;
+  // the number of the workgroup's next tile, -1: there is none
+  auto next_block = [&]() __attribute__((always_inline)) {
+    while (A::kTurns || turn == 0) {
+      if (turn * (int64_t)gridDim.x >= a.blocks) break;
+      const int block = turn * (int)gridDim.x + (turn & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+      ++turn;
+      if (block < a.blocks) return block;
     }
-    return m & first_bits(w.end - key0);
+    return -1;
   };
+  // the next tile whose part has keys, or outputs to write; false: there is none
+  auto next_tile = [&](TileWork& w) __attribute__((always_inline)) {
+    while (true) {
+      const int block = next_block();
+      if (block < 0) return false;
+      w = tab.template describe<A::kQueries, A::kKeys, D, KIND>(a, table, tab.template locate<A::kQueries>(a, table, block));
+      if (w.part < w.parts) return true;
+    }
+  };
+  TileWork w;
+  if (!next_tile(w)) return;
 
-  auto step = [&](auto tail_c, int key0, uint32_t buf) __attribute__((always_inline)) {
-    constexpr bool tail = decltype(tail_c)::value;
-    const uint32_t kt = buf + wk * 32 * kSub * A::kRow, vt = kt + A::kTileBytes;
-    const int mine = key0 + wk * 32 * kSub;
-    f32x16 x[kSub];
-    A::logits(x, q, kt, l32, g);
-    if constexpr (tail) {
+  typename A::Fetched raw;
+  typename A::Queries q;
+  int t_of, head_of;                                   // the lane's row: token and head
+  uint64_t bits;
+  auto load_rows = [&]() __attribute__((always_inline)) {
+    if (w.begin < w.end) {
+      if constexpr (A::kNarrow) A::fetch(raw, w, w.begin, w.end);
+      else A::stage(w, w.begin, w.end, lds);
+    }
+  };
+  auto load_queries = [&]() __attribute__((always_inline)) {
+    const int t0 = w.r0 / a.G, rem0 = w.r0 - t0 * a.G;  // token and head of the tile's first row
+    const int r = rem0 + max(min(first + l32, w.rows - 1 - w.r0), 0), dt = divide(r, a.G);
+    t_of = t0 + dt;
+    head_of = r - dt * a.G;
+    const unsigned char* const at = w.q + t_of * w.q_tok + head_of * w.q_head;
+#pragma unroll
+    for (int u = 0; u < (A::kF32 ? D / 8 : D / 16); ++u) q.w[u] = *(const u32x4*)(at + u * 32 + g * 16);
+    bits = bits_of(w, t_of, a.T);
+  };
+  load_rows();
+  load_queries();
+
+  while (true) {
+    const bool busy = w.r0 + first < w.rows;           // (waves without queries only stage)
+    float ref = -INFINITY, sum = 0.f;
+    f32x16 acc[kDT];
+#pragma unroll
+    for (int dt = 0; dt < kDT; ++dt) acc[dt] = f32x16{};
+    // keys that every query of the tile sees
+    const int all = w.sees ? w.hist : w.hist + w.r0 / a.G + 1;
+    // bit j: the lane's query sees the key key0 + j, which is there
+    auto seen = [&](int key0) __attribute__((always_inline)) {
+      uint32_t m = first_bits((w.sees ? w.hist : w.hist + t_of + 1) - key0);
+      if (w.sees) {
+        const int u = key0 - w.hist;                   // the draft's first row is bit -u
+        m |= u >= 64 || u <= -32 ? 0u : u >= 0 ? (uint32_t)(bits >> u) : (uint32_t)bits << -u;
+      }
+      return m & first_bits(w.end - key0);
+    };
+
+    auto step = [&](auto tail_c, int key0, uint32_t buf) __attribute__((always_inline)) {
+      constexpr bool tail = decltype(tail_c)::value;
+      const uint32_t kt = buf + wk * 32 * kSub * A::kRow, vt = kt + A::kTileBytes;
+      const int mine = key0 + wk * 32 * kSub;
+      f32x16 x[kSub];
+      A::logits(x, q, kt, l32, g);
+      if constexpr (tail) {
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) {
+          const uint32_t m = seen(mine + s * 32) >> (4 * g);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[s][i] = m & 1u << (i / 4 * 8 + i % 4) ? x[s][i] : -INFINITY;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < kSub; ++s)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[s][i]);
+      top *= a.c_log2;
+      if (__ballot(top > ref + A::kAbove)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(ref, top - A::kBelow);
+        const float f = ref == -INFINITY ? 0.f : exp2_fast(ref - now);
+        // (sums of a NaN stay one)
+        sum *= f;
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) acc[dt] *= f;
+        ref = now;
+      }
+      // (one rounding, of the difference: a large product's own would be an error of the weight)
+      const float from = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+      for (int s = 0; s < kSub; ++s)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          x[s][i] = exp2_fast(fmaf(x[s][i], a.c_log2, -from));
+          sum += x[s][i];
+        }
 #pragma unroll
       for (int s = 0; s < kSub; ++s) {
-        const uint32_t m = seen(mine + s * 32) >> (4 * g);
+        const uint32_t vs = vt + s * 32 * A::kRow;
+        if (tail && A::any_not_finite(vs, lane)) {
+          // a row at a time, to the queries that see it: an infinity or NaN reaches no other through a weight of 0
+          const uint32_t m = seen(mine + s * 32);
+          for (int row = 0; row < 32; ++row) {
+            float p = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[s][i] = m & 1u << (i / 4 * 8 + i % 4) ? x[s][i] : -INFINITY;
-      }
-    }
-    float top = -INFINITY;
+            for (int i = 0; i < 16; ++i)
+              if (i == row / 8 * 4 + row % 4) p = x[s][i];
+            p = __shfl(p, (row / 4 & 1) * 32 + l32);
+            if (m >> row & 1) {
 #pragma unroll
-    for (int s = 0; s < kSub; ++s)
+              for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[s][i]);
-    top *= a.c_log2;
-    if (__ballot(top > ref + A::kAbove)) {
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float now = fmaxf(ref, top - A::kBelow);
-      const float f = ref == -INFINITY ? 0.f : exp2_fast(ref - now);
-      // (sums of a NaN stay one)
-      sum *= f;
-#pragma unroll
-      for (int dt = 0; dt < kDT; ++dt) acc[dt] *= f;
-      ref = now;
-    }
-    // (one rounding, of the difference: a large product's own would be an error of the weight)
-    const float from = ref == -INFINITY ? 0.f : ref;
-#pragma unroll
-    for (int s = 0; s < kSub; ++s)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[s][i] = exp2_fast(fmaf(x[s][i], a.c_log2, -from));
-        sum += x[s][i];
-      }
-#pragma unroll
-    for (int s = 0; s < kSub; ++s) {
-      const uint32_t vs = vt + s * 32 * A::kRow;
-      if (tail && A::any_not_finite(vs, lane)) {
-        // a row at a time, to the queries that see it: an infinity or NaN reaches no other through a weight of 0
-        const uint32_t m = seen(mine + s * 32);
-        for (int row = 0; row < 32; ++row) {
-          float p = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (i == row / 8 * 4 + row % 4) p = x[s][i];
-          p = __shfl(p, (row / 4 & 1) * 32 + l32);
-          if (m >> row & 1) {
-#pragma unroll
-            for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) acc[dt][i] += p * A::value(vs, row, dt * 32 + i / 4 * 8 + 4 * g + i % 4);
+                for (int i = 0; i < 16; ++i) acc[dt][i] += p * A::value(vs, row, dt * 32 + i / 4 * 8 + 4 * g + i % 4);
+            }
           }
+        } else {
+          A::add_values(acc, x[s], vs, lane);
         }
-      } else {
-        A::add_values(acc, x[s], vs, lane);
       }
-    }
-  };
+    };
 
-  // Tiles that every query sees whole, then the others: the steps are two programs, so that the first has no branches for what the second has to look after (in one, with copies of
-  // the sums where its ways met, 32768 tokens took 8.90 ms).
-  uint32_t buf = lds, other = lds + 2 * A::kTileBytes;
-  int key0 = w.begin;
-  const int whole_end = w.begin + max(min(all, w.end) - w.begin, 0) / A::kKeys * A::kKeys;
-  if constexpr (A::kNarrow) {
-    if (w.begin < w.end) A::put(raw, buf);
-  }
-  auto run = [&](auto tail_c, int until) __attribute__((always_inline)) {
-    for (; key0 < until; key0 += A::kKeys) {
-      const bool more = key0 + A::kKeys < w.end;
-      if constexpr (A::kNarrow) {
-        if (more) A::fetch(raw, w, key0 + A::kKeys, w.end);
-        __syncthreads();
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (more) A::stage(w, key0 + A::kKeys, w.end, other);
-      }
-      if (busy) step(tail_c, key0, buf);
-      if constexpr (A::kSingle) {
-        __syncthreads();
-        if (more) A::put(raw, buf);
-        continue;
-      }
-      if constexpr (A::kNarrow) {
-        if (more) A::put(raw, other);
-      }
-      const uint32_t t = buf;
-      buf = other;
-      other = t;
+    // Tiles of keys that every query sees whole, then the others: the steps are two programs, so that the first has no branches for what the second has to look after (in one, with copies of
+    // the sums where its ways met, 32768 tokens took 8.90 ms).
+    uint32_t buf = lds, other = lds + 2 * A::kTileBytes;
+    int key0 = w.begin;
+    const int whole_end = w.begin + max(min(all, w.end) - w.begin, 0) / A::kKeys * A::kKeys;
+    if constexpr (A::kNarrow) {
+      if (w.begin < w.end) A::put(raw, buf);
     }
-  };
-  run(std::integral_constant<bool, false>{}, whole_end);
-  run(std::integral_constant<bool, true>{}, w.end);
+    auto run = [&](auto tail_c, int until) __attribute__((always_inline)) {
+      for (; key0 < until; key0 += A::kKeys) {
+        const bool more = key0 + A::kKeys < w.end;
+        if constexpr (A::kNarrow) {
+          if (more) A::fetch(raw, w, key0 + A::kKeys, w.end);
+          __syncthreads();
+        } else {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          __syncthreads();
+          if (more) A::stage(w, key0 + A::kKeys, w.end, other);
+        }
+        if (busy) step(tail_c, key0, buf);
+        if constexpr (A::kSingle) {
+          __syncthreads();
+          if (more) A::put(raw, buf);
+        } else {
+          if constexpr (A::kNarrow) {
+            if (more) A::put(raw, other);
+          }
+          const uint32_t t = buf;
+          buf = other;
+          other = t;
+        }
+      }
+    };
+    run(std::integral_constant<bool, false>{}, whole_end);
+    run(std::integral_constant<bool, true>{}, w.end);
 
-  // The waves that share queries are put together, and the outputs turned round, through LDS.
-  const bool whole = w.parts == 1;
-  const int slot = w.slot0 + w.part * w.slot_step;
-  float* const sh_o = (float*)sh;
-  const float total = sum + __shfl_xor(sum, 32);
-  __syncthreads();                                   // (the last tile has been read)
-  if (g == 0) {
-    sh_m[wk][wq * 32 + l32] = ref;
-    sh_l[wk][wq * 32 + l32] = total;
-  }
-  if constexpr (WK > 1) __syncthreads();
-  float f = 1.f;
-  if constexpr (WK > 1) {
-    float top = -INFINITY;
+    const TileWork now = w;
+    const int t_now = t_of, head_now = head_of;
+    const uint64_t bits_now = bits;
+    bool more = false;
+    if constexpr (A::kTurns) more = next_tile(w);
+    const bool whole = now.parts == 1;
+    const int64_t row0 = (int64_t)(now.slot0 + now.part * now.slot_step) * A::kQueries;
+    const float total = sum + __shfl_xor(sum, 32);
+    __syncthreads();                                   // the last rows have been read
+    if constexpr (WK == 1) {
+      if (more) {
+        load_rows();
+        load_queries();
+      }
+      if (now.r0 + first + l32 < now.rows) {
+        if (whole) {
+          const bool none = sees_none(now, t_now, bits_now);
+          const float scale = total_scale(total);
+          unsigned char* const at = now.out + t_now * now.o_tok + head_now * now.o_head;
 #pragma unroll
-    for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_m[i][wq * 32 + l32]);
-    // (a wave that saw nothing has a sum of 0, or NaN where a product was NaN)
-    f = ref == -INFINITY ? 1.f : exp2_fast(ref - top);
-  }
+          for (int dt = 0; dt < kDT; ++dt) {
 #pragma unroll
-  for (int dt = 0; dt < kDT; ++dt)
+            for (int i = 0; i < 16; ++i) acc[dt][i] = none ? 0.f : acc[dt][i] * scale;
+            if constexpr (A::kF32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *(f32x4*)&sh_o[((wk * WQ + wq) * 32 + l32) * A::kOutRow + dt * 32 + i * 8 + 4 * g] =
-          f32x4{acc[dt][i * 4], acc[dt][i * 4 + 1], acc[dt][i * 4 + 2], acc[dt][i * 4 + 3]} * f;
-  __syncthreads();
-  constexpr int kLanes = D / 4;                      // threads of a row of outputs
-  for (int idx = threadIdx.x; idx < 32 * WQ * kLanes; idx += A::kThreads) {
-    const int r = idx / kLanes, d0 = idx % kLanes * 4;    // row of the tile, dims
-    if (w.r0 + r >= w.rows) continue;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    float top = -INFINITY, l = 0.f;
+              for (int i = 0; i < 4; ++i)
+                *(f32x4*)(at + (dt * 32 + i * 8 + 4 * g) * 4) = f32x4{acc[dt][i * 4], acc[dt][i * 4 + 1], acc[dt][i * 4 + 2], acc[dt][i * 4 + 3]};
+            } else {
+              // dims 8 i .. 8 i + 3 are in lane l, the next four in lane l + 32: of two neighbouring i each gets one whole
 #pragma unroll
-    for (int i = 0; i < WK; ++i) {
-      o += *(const f32x4*)&sh_o[(i * WQ * 32 + r) * A::kOutRow + d0];
-      top = fmaxf(top, sh_m[i][r]);
-    }
+              for (int i = 0; i < 4; i += 2) {
+                u32x4 o;
 #pragma unroll
-    for (int i = 0; i < WK; ++i) l += sh_l[i][r] * (WK == 1 || sh_m[i][r] == -INFINITY ? 1.f : exp2_fast(sh_m[i][r] - top));
-    if (whole) {
-      const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
-      const bool none = sees_none(w, t, bits_of(w, t, a.T));
-      store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
-      if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
+                for (int e = 0; e < 2; ++e) {
+                  const uint32_t x = A::pair(acc[dt][i * 4 + 2 * e], acc[dt][i * 4 + 2 * e + 1]), y = A::pair(acc[dt][i * 4 + 4 + 2 * e], acc[dt][i * 4 + 5 + 2 * e]);
+                  const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, y, false, false));
+                  o[e] = t[0];
+                  o[2 + e] = t[1];
+                }
+                *(u32x4*)(at + (dt * 32 + (i + g) * 8) * 2) = o;
+              }
+            }
+          }
+          if (now.lse && g == 0) now.lse[head_now * now.lse_head + t_now] = tile_lse<A>(ref, total, none);
+        } else {
+          const int64_t row = row0 + first + l32;
+#pragma unroll
+          for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *(f32x4*)(a.part_o + row * D + dt * 32 + i * 8 + 4 * g) = f32x4{acc[dt][i * 4], acc[dt][i * 4 + 1], acc[dt][i * 4 + 2], acc[dt][i * 4 + 3]};
+          if (g == 0) *(f32x2*)(a.part_ml + row * 2) = f32x2{ref, total};
+        }
+      }
     } else {
-      *(f32x4*)(a.part_o + ((int64_t)slot * A::kQueries + r) * D + d0) = o;
-      if (d0 == 0) *(f32x2*)(a.part_ml + ((int64_t)slot * A::kQueries + r) * 2) = f32x2{top, l};
+      // the waves that share queries are put together through LDS
+      float* const sh_o = (float*)sh;
+      if (g == 0) {
+        sh_m[wk][first + l32] = ref;
+        sh_l[wk][first + l32] = total;
+      }
+      __syncthreads();
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_m[i][first + l32]);
+      // (a wave that saw nothing has a sum of 0, or NaN where a product was NaN)
+      const float mine = ref == -INFINITY ? 1.f : exp2_fast(ref - top);
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(f32x4*)&sh_o[((wk * WQ + wq) * 32 + l32) * A::kOutRow + dt * 32 + i * 8 + 4 * g] =
+              f32x4{acc[dt][i * 4], acc[dt][i * 4 + 1], acc[dt][i * 4 + 2], acc[dt][i * 4 + 3]} * mine;
+      if (wk == 0 && g == 0 && now.r0 + first + l32 < now.rows) {
+        const int r = first + l32;
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < WK; ++i) l += sh_l[i][r] * (sh_m[i][r] == -INFINITY ? 1.f : exp2_fast(sh_m[i][r] - top));
+        if (whole) {
+          const bool none = sees_none(now, t_now, bits_now);
+          sh_scale[r] = none ? 0.f : total_scale(l);
+          sh_at[r] = t_now * now.o_tok + head_now * now.o_head;
+          if (now.lse) now.lse[head_now * now.lse_head + t_now] = tile_lse<A>(top, l, none);
+        } else {
+          *(f32x2*)(a.part_ml + (row0 + r) * 2) = f32x2{top, l};
+        }
+      }
+      __syncthreads();
+      constexpr int kLanes = D / 4;                    // threads of a row of outputs
+      for (int idx = threadIdx.x; idx < 32 * WQ * kLanes; idx += A::kThreads) {
+        const int r = idx / kLanes, d0 = idx % kLanes * 4;   // row of the tile, dims
+        if (now.r0 + r >= now.rows) break;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < WK; ++i) o += *(const f32x4*)&sh_o[(i * WQ * 32 + r) * A::kOutRow + d0];
+        if (whole) store_out<KIND>(now.out + sh_at[r] + d0 * (int)sizeof(typename A::wide), o * sh_scale[r]);
+        else *(f32x4*)(a.part_o + (row0 + r) * D + d0) = o;
+      }
+      if (more) {
+        __syncthreads();
+        load_rows();
+        load_queries();
+      }
     }
+    if (!more) return;
   }
 }
 
@@ -501,7 +602,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) 
 template <int KIND, int D, int WQ, int WK, class TAB>
 __global__ __launch_bounds__(256) void join_tiles_kernel(const TileArgs a, const TAB tab) {
   using A = Tiles<KIND, D, WQ, WK>;
-  const TileWork w = tab.template find<A::kQueries, A::kKeys, D, KIND>(a, (int)blockIdx.x);
+  const TileWork w = tab.template describe<A::kQueries, A::kKeys, D, KIND>(a, tab.words, tab.template locate<A::kQueries>(a, tab.words, (int)blockIdx.x));
   if (w.parts == 1 || w.part >= w.parts) return;
   constexpr int kLanes = D / 4, kRows = 256 / kLanes, kAtOnce = 8;
   const int t0 = w.r0 / a.G, rem0 = w.r0 % a.G, lane = threadIdx.x % kLanes, d0 = lane * 4;
@@ -538,7 +639,7 @@ __global__ __launch_bounds__(256) void join_tiles_kernel(const TileArgs a, const
     l = reduce_lanes(l, kLanes, [](float u, float v) { return u + v; });
     const int dt = divide(rem0 + r, a.G), head = rem0 + r - dt * a.G, t = t0 + dt;
     const bool none = sees_none(w, t, bits_of(w, t, a.T));
-    store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), tile_output(o, l, none));
+    store_out<KIND>(w.out + t * w.o_tok + head * w.o_head + d0 * (int)sizeof(typename A::wide), none ? f32x4{0.f, 0.f, 0.f, 0.f} : o * total_scale(l));
     if (w.lse && d0 == 0) w.lse[head * w.lse_head + t] = tile_lse<A>(top, l, none);
   }
 }
@@ -550,6 +651,14 @@ struct TileShape { int wq, wk; };
 constexpr TileShape kTileShapes[] = {{1, 4}, {2, 2}, {4, 1}, {4, 2}, {8, 1}};
 constexpr int kTileShapeCount = 5;
 inline int tile_queries(int shape) { return 32 * kTileShapes[shape].wq; }
+
+// Workgroups of a launch, at most: as many as the registers and LDS of the chip have places for.
+template <class A>
+constexpr unsigned tile_places() {
+  if (!A::kTurns) return ~0u;
+  const int waves = 4 * A::kPerSimd / A::kWaves, lds = 160 * 1024 / (A::kLds + 4096);
+  return 256 * (unsigned)std::max(1, std::min(waves, lds));
+}
 
 // f with the waves of a shape as compile-time constants.  fp32 has two shapes: others do not fit LDS or registers.
 template <int KIND, class F>

@@ -5,22 +5,61 @@
 
 namespace slkv {
 
-// Sequences of a launch, those with the most keys first.  Workgroups: sequence, then tiles of queries from the last one (which has the most keys) down, then parts of
-// the keys, then KV heads, so that with 8 of them a head stays on an XCD and its L2.
+// Sequences of a launch, those with the most keys first.  Tiles of queries come in the order of their keys, the most first, whatever sequence they are of, and for each of them the KV heads, so
+// that with 8 of these a head stays on an XCD and its L2.  In order (where there are parts, and for sequences of one length, whose keys and values stay in the caches this way: 64 of 256 tokens 116 us, else
+// 128): sequence, tiles from the last one down, parts of the keys, KV heads.  (8 sequences of 110 to 4000 tokens: 436 us in order, else 412.)
 struct PromptTab {
   static constexpr int kSeqs = 64;
   const unsigned char *k, *v, *q;
   unsigned char* out;
   float* lse;
   int64_t q_tok, q_head, o_tok, o_head, k_row, v_row, k_head, v_head, lse_head;   // bytes; lse_head: elements
-  int32_t nseq, hkv;
-  int32_t first[kSeqs + 1], q0[kSeqs], nq[kSeqs], k0[kSeqs], nk[kSeqs], parts[kSeqs];
+  int32_t nseq, hkv, in_order, shift;                  // 2^shift: tokens of a tile, about
+  struct Words { int32_t first[kSeqs + 1], q0[kSeqs], nq[kSeqs], k0[kSeqs], nk[kSeqs], parts[kSeqs]; } words;
+
+  // sequence; of it, tiles from the last one down and their parts; KV head
+  struct Place { int s, rest, h; };
+  template <int QUERIES>
+  __device__ __forceinline__ Place locate(const TileArgs& a, const Words& t, int block) const {
+    int s = 0, rest, h;
+    if (in_order) {
+      if (nseq > 1) s = find_segment_wave(nseq, block, [&](int i) { return t.first[i]; });
+      const int i = block - __builtin_amdgcn_readfirstlane(t.first[s]);
+      rest = i / hkv;
+      h = i - rest * hkv;
+    } else {
+      // The i-th tile from the end of sequence b has the level nk[b] / 2^shift - i; lane b counts its tiles of a level and above.  Of the tiles down to the level wanted `rank`
+      // come before.
+      const int rank = block / hkv, lane = threadIdx.x % kWave;
+      h = block - rank * hkv;
+      const int mine = lane < nseq ? (a.G * t.nq[min(lane, nseq - 1)] + QUERIES - 1) / QUERIES : 0, top = lane < nseq ? t.nk[min(lane, nseq - 1)] >> shift : 0;
+      auto count = [&](int level) __attribute__((always_inline)) {
+        const uint32_t all = wave_incl_scan((uint32_t)min(max(top - level + 1, 0), mine));
+        return (int)__builtin_amdgcn_readlane((int)all, kWave - 1);
+      };
+      int lo = -(1 << 30), hi = __builtin_amdgcn_readfirstlane(top) + 1;     // count(lo) > rank >= count(hi)
+      // (the levels end where the last tiles of all sequences do)
+      const uint32_t least = wave_reduce_to_last((uint32_t)(mine ? top - mine + 1 : hi) ^ 0x80000000u, [](uint32_t x, uint32_t y) { return min(x, y); });
+      lo = (int)((uint32_t)__builtin_amdgcn_readlane((int)least, kWave - 1) ^ 0x80000000u);
+      while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (count(mid) > rank) lo = mid;
+        else hi = mid;
+      }
+      uint64_t there = __ballot(mine && top >= lo && top - lo < mine);
+      for (int skip = rank - count(lo + 1); skip > 0; --skip) there &= there - 1;
+      s = __builtin_ctzll(there);
+      rest = __builtin_amdgcn_readlane(top, s) - lo;
+    }
+    return Place{s, rest, h};
+  }
 
   template <int QUERIES, int KEYS, int D, int KIND>
-  __device__ __forceinline__ TileWork find(const TileArgs& a, int block) const {
-    const int s = find_segment_wave(nseq, block, [&](int i) { return first[i]; });
-    const int i = block - first[s], h = i % hkv, rest = i / hkv;
-    const int parts_here = parts[s], new_tokens = nq[s], keys = nk[s], rows = a.G * new_tokens;
+  __device__ __forceinline__ TileWork describe(const TileArgs& a, const Words& t, const Place& at) const {
+    auto uniform = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+    const int s = at.s, h = at.h, rest = at.rest;
+    const int parts_here = in_order ? uniform(t.parts[s]) : 1, new_tokens = uniform(t.nq[s]), keys = uniform(t.nk[s]), rows = a.G * new_tokens;
+    const int64_t key0 = uniform(t.k0[s]), query0 = uniform(t.q0[s]);
     const int tiles = (rows + QUERIES - 1) / QUERIES, tile = tiles - 1 - rest / parts_here;
     TileWork w;
     w.part = rest % parts_here;
@@ -33,16 +72,16 @@ struct PromptTab {
     w.parts = each ? (end + each - 1) / each : 1;
     w.begin = w.part * each;
     w.end = min(end, w.begin + each);
-    w.k = k + h * k_head + k0[s] * k_row;
-    w.v = v + h * v_head + k0[s] * v_row;
+    w.k = k + h * k_head + key0 * k_row;
+    w.v = v + h * v_head + key0 * v_row;
     w.ks = w.vs = nullptr;
-    w.q = q + (int64_t)h * a.G * q_head + q0[s] * q_tok;
-    w.out = out + (int64_t)h * a.G * o_head + q0[s] * o_tok;
-    w.lse = lse ? lse + (int64_t)h * a.G * lse_head + q0[s] : nullptr;
+    w.q = q + (int64_t)h * a.G * q_head + query0 * q_tok;
+    w.out = out + (int64_t)h * a.G * o_head + query0 * o_tok;
+    w.lse = lse ? lse + (int64_t)h * a.G * lse_head + query0 : nullptr;
     w.sees = nullptr;
     w.q_tok = q_tok, w.q_head = q_head, w.o_tok = o_tok, w.o_head = o_head, w.lse_head = lse_head;
     w.k_row = k_row, w.v_row = v_row;
-    w.slot0 = first[s] + rest / parts_here * parts_here * hkv + h;
+    w.slot0 = in_order ? uniform(t.first[s]) + rest / parts_here * parts_here * hkv + h : 0;
     w.slot_step = hkv;
     return w;
   }
@@ -181,31 +220,39 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
     t.v_row = desc->v_stride_tok * narrow, t.v_head = desc->v_stride_head * narrow;
     t.lse_head = desc->h_cu_q[desc->B];
     t.hkv = desc->Hkv;
+    t.shift = 0;
+    while (2 << t.shift <= p.queries / a.G) ++t.shift;
     t.nseq = (int32_t)std::min<int64_t>(PromptTab::kSeqs, desc->B - b0);
+    auto length = [&](int i, const int64_t* cu) { return cu[b0 + i + 1] - cu[b0 + i]; };
     int order[PromptTab::kSeqs];
     for (int i = 0; i < t.nseq; ++i) order[i] = i;
     std::sort(order, order + t.nseq, [&](int x, int y) {
-      const int64_t kx = ck[b0 + x + 1] - ck[b0 + x], ky = ck[b0 + y + 1] - ck[b0 + y];
+      const int64_t kx = length(x, ck), ky = length(y, ck);
       return kx != ky ? kx > ky : x < y;
     });
+    bool even = true;
+    for (int i = 1; i < t.nseq; ++i) even &= length(i, desc->h_cu_q) == length(0, desc->h_cu_q) && length(i, ck) == length(0, ck);
+    t.in_order = p.split || even;
     int64_t blocks = 0;
     for (int i = 0; i < t.nseq; ++i) {
       const int64_t b = b0 + order[i];
-      t.first[i] = (int32_t)blocks;
-      t.q0[i] = (int32_t)desc->h_cu_q[b], t.nq[i] = (int32_t)(desc->h_cu_q[b + 1] - desc->h_cu_q[b]);
-      t.k0[i] = (int32_t)ck[b], t.nk[i] = (int32_t)(ck[b + 1] - ck[b]);
-      t.parts[i] = (int32_t)seq_parts(desc, b, p.each);
-      blocks += seq_tiles(desc, b, p.queries) * desc->Hkv * t.parts[i];
+      PromptTab::Words& x = t.words;
+      x.first[i] = (int32_t)blocks;
+      x.q0[i] = (int32_t)desc->h_cu_q[b], x.nq[i] = (int32_t)(desc->h_cu_q[b + 1] - desc->h_cu_q[b]);
+      x.k0[i] = (int32_t)ck[b], x.nk[i] = (int32_t)(ck[b + 1] - ck[b]);
+      x.parts[i] = (int32_t)seq_parts(desc, b, p.each);
+      blocks += seq_tiles(desc, b, p.queries) * desc->Hkv * x.parts[i];
     }
-    t.first[t.nseq] = (int32_t)blocks;
+    t.words.first[t.nseq] = (int32_t)blocks;
     if (!blocks) continue;
+    a.blocks = (int32_t)blocks;
     auto launch = [&](auto kind, auto dim) {
       constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
       with_shape<kKind>(p.shape, [&](auto wq, auto wk) {
         constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
         {
           ScopedKernelTimer timer(SLKV_K_PROMPT);
-          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTab>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTab>), dim3(std::min((unsigned)blocks, tile_places<Tiles<kKind, kDim, kWQ, kWK>>())), dim3(kWQ * kWK * kWave), 0, stream, a, t);
         }
         if (p.split) {
           ScopedKernelTimer timer(SLKV_K_TILES_JOIN);

@@ -20,29 +20,39 @@ struct TreeTab {
   const uint64_t* sees;
   const int32_t* lengths;
   int32_t nseg, seg0, hkv, each;
-  int32_t start[N + 1], before[kGroups];
-  uint16_t order[N];
+  struct Words {
+    int32_t start[N + 1], before[kGroups];
+    uint16_t order[N];
+  } words;
 
-  template <int QUERIES, int KEYS, int D, int KIND>
-  __device__ __forceinline__ TileWork find(const TileArgs& a, int block) const {
+  // segment, tile of queries, part; of the segment: first row and room, parts, parts of others before its own
+  struct Place { int s, tile, part, at, room, parts, first; };
+  template <int QUERIES>
+  __device__ __forceinline__ Place locate(const TileArgs& a, const Words& t, int block) const {
     const int tiles = (a.G * a.T + QUERIES - 1) / QUERIES, part_id = block / tiles, lane = threadIdx.x % kWave;
     const int groups = (nseg + kGroup - 1) / kGroup;
-    const int b0 = before[min(lane, groups - 1)];
+    const int b0 = t.before[min(lane, groups - 1)];
     const int grp = __popcll(__ballot(lane < groups && b0 <= part_id)) - 1;
-    const int in_group = order[min(grp * kGroup + min(lane, kGroup - 1), nseg - 1)];
-    const int at_lane = start[in_group], room_lane = start[in_group + 1] - at_lane;
+    const int in_group = t.order[min(grp * kGroup + min(lane, kGroup - 1), nseg - 1)];
+    const int at_lane = t.start[in_group], room_lane = t.start[in_group + 1] - at_lane;
     const bool in = lane < kGroup && grp * kGroup + lane < nseg;
     const int parts_lane = in ? max(1, (room_lane + each - 1) / each) : 0;
     const int first_lane = __builtin_amdgcn_readlane(b0, grp) + (int)wave_incl_scan((uint32_t)parts_lane) - parts_lane;
     const int which = __popcll(__ballot(in && first_lane <= part_id)) - 1;
-    const int s = __builtin_amdgcn_readlane(in_group, which), at = __builtin_amdgcn_readlane(at_lane, which), room = __builtin_amdgcn_readlane(room_lane, which);
-    const int parts = __builtin_amdgcn_readlane(parts_lane, which), first = __builtin_amdgcn_readlane(first_lane, which);
-    const int seg = seg0 + s, b = seg / hkv, h = seg % hkv, tile = block - part_id * tiles;
+    const int first = __builtin_amdgcn_readlane(first_lane, which);
+    return Place{__builtin_amdgcn_readlane(in_group, which), block - part_id * tiles, part_id - first, __builtin_amdgcn_readlane(at_lane, which),
+                 __builtin_amdgcn_readlane(room_lane, which), __builtin_amdgcn_readlane(parts_lane, which), first};
+  }
+
+  template <int QUERIES, int KEYS, int D, int KIND>
+  __device__ __forceinline__ TileWork describe(const TileArgs& a, const Words&, const Place& p) const {
+    const int seg = seg0 + p.s, b = seg / hkv, h = seg % hkv, at = p.at, room = p.room, parts = p.parts;
+    const int tiles = (a.G * a.T + QUERIES - 1) / QUERIES;
     constexpr int kRow = D * Kind<KIND>::kBits / 8, kWide = D * (int)sizeof(typename Kind<KIND>::wide), kScales = D / kScaleBlock;
     TileWork w;
-    w.part = part_id - first;
+    w.part = p.part;
     w.rows = a.G * a.T;
-    w.r0 = tile * QUERIES;
+    w.r0 = p.tile * QUERIES;
     w.n = __builtin_amdgcn_readfirstlane(rows_in_use(lengths, seg, room));
     w.hist = w.n - a.T;
     // the rows in use are spread over the parts of the room
@@ -63,7 +73,7 @@ struct TreeTab {
     w.q_head = w.o_head = (int64_t)a.T * kWide;
     w.lse_head = a.T;
     w.k_row = w.v_row = kRow;
-    w.slot0 = first * tiles + tile;
+    w.slot0 = p.first * tiles + p.tile;
     w.slot_step = tiles;
     return w;
   }
@@ -115,14 +125,14 @@ static void order_segments(TAB& t) {
   int from[kSteps + 1] = {};
   uint8_t key[TAB::kSegs];
   auto length = [&](int i) {
-    const int64_t room = t.start[i + 1] - t.start[i], parts = std::max<int64_t>(1, (room + t.each - 1) / t.each);
+    const int64_t room = t.words.start[i + 1] - t.words.start[i], parts = std::max<int64_t>(1, (room + t.each - 1) / t.each);
     return (room + parts - 1) / parts;
   };
   int64_t most = 1;
   for (int i = 0; i < t.nseg; ++i) most = std::max(most, length(i));
   for (int i = 0; i < t.nseg; ++i) ++from[(key[i] = (uint8_t)(kSteps - 1 - length(i) * (kSteps - 1) / most)) + 1];
   for (int k = 0; k < kSteps; ++k) from[k + 1] += from[k];
-  for (int i = 0; i < t.nseg; ++i) t.order[from[key[i]]++] = (uint16_t)i;
+  for (int i = 0; i < t.nseg; ++i) t.words.order[from[key[i]]++] = (uint16_t)i;
 }
 
 static slkv_status tree_checks(const slkv_cache_desc* desc, int32_t T, TreePlan& plan) {
@@ -179,20 +189,21 @@ extern "C" slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_
     t.nseg = (int32_t)ns, t.seg0 = (int32_t)s0, t.hkv = desc->Hkv;
     int64_t blocks = 0;
     t.each = (int32_t)p.each;
-    for (int64_t i = 0; i <= ns; ++i) t.start[i] = (int32_t)desc->h_offsets[s0 + i];
+    for (int64_t i = 0; i <= ns; ++i) t.words.start[i] = (int32_t)desc->h_offsets[s0 + i];
     order_segments(t);
     for (int64_t i = 0; i < ns; ++i) {
-      if (i % TAB::kGroup == 0) t.before[i / TAB::kGroup] = (int32_t)blocks;
-      blocks += tree_parts(desc, s0 + t.order[i], p.each);
+      if (i % TAB::kGroup == 0) t.words.before[i / TAB::kGroup] = (int32_t)blocks;
+      blocks += tree_parts(desc, s0 + t.words.order[i], p.each);
     }
     blocks *= tiles;
+    a.blocks = (int32_t)blocks;
     auto launch = [&](auto kind, auto dim) {
       constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
       with_shape<kKind>(p.shape, [&](auto wq, auto wk) {
         constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
         {
           ScopedKernelTimer timer(SLKV_K_TREE);
-          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, TAB>), dim3((unsigned)blocks), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, TAB>), dim3(std::min((unsigned)blocks, tile_places<Tiles<kKind, kDim, kWQ, kWK>>())), dim3(kWQ * kWK * kWave), 0, stream, a, t);
         }
         if (p.split) {
           ScopedKernelTimer timer(SLKV_K_TILES_JOIN);
