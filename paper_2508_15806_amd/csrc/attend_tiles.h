@@ -79,12 +79,13 @@ struct Tiles {
   // Narrow rows of four subtiles a step: one tile in LDS, the next one in registers, so that two workgroups share a CU.
   static constexpr bool kSingle = kNarrow && WK == 4 && WQ == 1;
   static constexpr int kTilesBytes = (kSingle ? 2 : 4) * kTileBytes;
-  // Whether a workgroup takes tiles in turn: not where queries are few and keys many, whose workgroups have enough to do, and no registers to spare for it.
-  static constexpr bool kTurns = WK < 4;
+  // Whether a workgroup takes tiles in turn: the ones that have a CU to themselves.  Where workgroups share one they fill each other's beginnings and ends, and the chip deals tiles out
+  // more evenly (3 prompts of 1111 tokens in fp16, 512 places: 34 us, in turn on 768: 27, dealt out: 25).
+  static constexpr bool kTurns = kWaves == 8;
   static constexpr int kOutBytes = WK == 1 ? 0 : kWaves * 32 * kOutRow * 4;
   static constexpr int kLds = kTilesBytes > kOutBytes ? kTilesBytes : kOutBytes;
   // waves of a SIMD, at least: what LDS and registers allow
-  static constexpr int kPerSimd = D == 64 ? (kWaves == 4 && WK < 4 && !kF32 ? 3 : 2) : kF32 || (WQ == 1 && WK == 4 && !kSingle) ? 1 : 2;
+  static constexpr int kPerSimd = D == 64 ? 2 : kF32 || (WQ == 1 && WK == 4 && !kSingle) ? 1 : 2;
   // Reference of fp16 weights: they reach 2^15, so that those down to 2^-26 of the largest keep all their bits.
   static constexpr float kBelow = KIND == SLKV_F16 ? 12.f : 0.f, kBelowPower = KIND == SLKV_F16 ? 0x1p-12f : 1.f;
   static constexpr float kAbove = KIND == SLKV_F16 ? 15.f : 8.f;   // a product this far above the reference moves it
@@ -301,9 +302,11 @@ __device__ __forceinline__ float tile_lse(float top, float total, bool none) {
 }
 __device__ __forceinline__ float total_scale(float total) { return total > 0.f ? 1.f / total : NAN; }
 
-// Workgroups take tiles in turn: as many workgroups as the chip has places go through them back and forth, so that tiles that get smaller come out even.  The next tile's first rows and queries
-// are on their way while the outputs are written.  (A workgroup for every tile: 17 us beside its steps, of which 6 between two workgroups of a CU, 5 for the first rows, 7 for outputs through LDS; 16 prompts
-// of 1024 tokens 270 us.)
+// A tile of queries, or a part of one's keys, a workgroup; workgroups of 8 waves take tiles in turn: as many of them as the chip has places go through the tiles back and forth, so that tiles that
+// get smaller come out even, and the next tile's first rows and queries are on their way while the outputs are written.  (Without turns, and with outputs through LDS, a workgroup took 17 us beside
+// its steps, of which 6 between two workgroups of a CU, 4 for the first rows, 6 for the outputs: 16 prompts of 1024 tokens 270 us, now 218; 4096 tokens 147, now 137.)
+// Bound by the matrix units' clock under load in long prompts (32768 tokens, 32 heads of 128: 7.8 ms, 1128 TFLOP/s, what the library's large product reaches), by a workgroup's
+// beginning and end in short ones, by memory and the join where queries are few.
 template <int KIND, int D, int WQ, int WK, class TAB>
 __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) void attend_tiles_kernel(const TileArgs a, const TAB tab) {
   using A = Tiles<KIND, D, WQ, WK>;

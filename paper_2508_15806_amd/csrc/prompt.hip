@@ -232,7 +232,6 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
     });
     bool even = true;
     for (int i = 1; i < t.nseq; ++i) even &= length(i, desc->h_cu_q) == length(0, desc->h_cu_q) && length(i, ck) == length(0, ck);
-    t.in_order = p.split || even;
     int64_t blocks = 0;
     for (int i = 0; i < t.nseq; ++i) {
       const int64_t b = b0 + order[i];
@@ -244,6 +243,7 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
       blocks += seq_tiles(desc, b, p.queries) * desc->Hkv * x.parts[i];
     }
     t.words.first[t.nseq] = (int32_t)blocks;
+    t.in_order = p.split || even || blocks <= 512;     // (looking a tile up in the other order takes 1.5 us)
     if (!blocks) continue;
     a.blocks = (int32_t)blocks;
     auto launch = [&](auto kind, auto dim) {
