@@ -130,7 +130,7 @@ def accept_segment(path, T, base, room):
             break
         if 0 <= base + p < room:
             rows.append(base + int(p))
-    return rows, max(base, 0)
+    return rows[:room - max(base, 0)], max(base, 0)
 
 
 def evict_segment(weight, w, cap):

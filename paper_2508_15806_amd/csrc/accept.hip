@@ -61,10 +61,11 @@ __device__ __forceinline__ Accepted accepted_of(const AcceptArgs& a, int seg, in
   const int length = ends ? __builtin_ctzll(ends) : kWave;             // the path ends at the first number that is none
   const bool there = lane < length && r.base + p >= 0 && r.base + p < room;
   const uint64_t all = __ballot(there);
-  r.count = __popcll(all);
+  const int found = __popcll(all);
+  r.count = min(found, room - max(r.base, 0));                         // (a number that comes twice is a row twice: there may not be room for all)
   // (nearly always all of the path)
   int from = lane;
-  if (r.count != length) {
+  if (found != length) {
     uint64_t left = all;
     for (int i = 0; i < lane && left; ++i) left &= left - 1;
     from = left ? __builtin_ctzll(left) : 0;

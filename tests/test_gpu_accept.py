@@ -116,6 +116,14 @@ def test_rows_behind_a_number_of_them(weights, own_lengths):
 
 
 @pytest.mark.parametrize("weights", [False, True])
+def test_rows_twice_stay_in_the_room(weights):
+    """The same token several times, in rooms that do not hold it as often; the next segment's rows and weights stay."""
+    rng = np.random.default_rng(12)
+    cache = random_cache(rng, "bf16", 2, 2, 2, 64, [20, 30, 25, 40], rooms=[20, 31, 25, 60])
+    check(cache, [[3, 3, 3, 3, 3, 3], [0, 0, 1, 1, 0, 0]], 4, weights=weights, rng=rng)
+
+
+@pytest.mark.parametrize("weights", [False, True])
 def test_fewer_rows_than_drafted_tokens(weights):
     rng = np.random.default_rng(4)
     cache = random_cache(rng, "bf16_kv8", 2, 2, 2, 64, [3, 0, 8, 7], rooms=[5, 0, 9, 7])

@@ -117,3 +117,4 @@ def test_oracle_accept():
     assert decode.accept_segment([0, 2, 6, 1], 6, 10, 40) == ([10, 12], 10)
     assert decode.accept_segment([0, 2, 5, 1], 6, -2, 40) == ([0, 3], 0)
     assert decode.accept_segment([0, 2, 1], 6, 38, 40) == ([38, 39], 38)
+    assert decode.accept_segment([0, 0, 1, 0], 6, 38, 40) == ([38, 38], 38)
