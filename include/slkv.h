@@ -428,7 +428,7 @@ slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_cache* cach
 
 /* What a verification leaves of a draft of T tokens whose rows stand behind the rows before it: the accepted ones move together and the others leave.
  * d_path [B][A] int32: the accepted tokens of every sequence in their new order, up to the first number outside 0 .. T-1 (or all A); the same number twice is a row twice, as far as the room holds it.  Drafted
- *   token u's row of segment s is base_s + u, with base_s = d_at[s] if d_at is given (it may be d_lengths itself), otherwise n_s - T.  Tokens whose row is not there (below 0, or
+ *   token u's row of segment s is base_s + u, with base_s = d_at[s] if d_at is given (it may be d_lengths itself, but not overlap it otherwise), otherwise n_s - T.  Tokens whose row is not there (below 0, or
  *   beyond the room) are left out in that segment.
  * The i-th accepted token's row (K, V, scales, position, weight) goes to row max(base_s, 0) + i, and d_lengths[s] becomes max(base_s, 0) + their number.  Rows behind these stay as they are.
  * d_q [B][Hq][T][d], d_lse [B][Hq][T]: the drafted tokens' queries and what slkv_attend_tree gave for them; with them, for the new rows in use j,

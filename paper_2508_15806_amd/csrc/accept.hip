@@ -283,6 +283,9 @@ extern "C" slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv
   a.c_log2 = kLog2e / std::sqrt((float)desc->d);
   hipStream_t const stream = (hipStream_t)hip_stream;
   const int64_t S = (int64_t)desc->B * desc->Hkv;
+  // (a workgroup reads its own segment's number alone before it sets the length)
+  if (d_at && d_at != cache->d_lengths && d_at < cache->d_lengths + S && cache->d_lengths < d_at + S)
+    return fail(SLKV_ERR_BAD_ARG, "d_at overlaps d_lengths and is not d_lengths itself");
   a.lengths_later = d_q && (!d_at || d_at == cache->d_lengths);
   auto launch = [&](auto tab, int64_t s0, int64_t ns) {
     using TAB = decltype(tab);

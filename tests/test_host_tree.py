@@ -49,6 +49,15 @@ def test_refused_acceptances():
     assert accept(lay=layout(d=32)) == 4 and accept(lay=layout(dtype=9)) == 2
 
 
+def test_rows_of_the_draft_do_not_overlap_the_lengths():
+    """d_at may be d_lengths itself, not a part of it: a segment's length would be set while another reads it."""
+    lay, lengths = layout(B=4, offsets=[0, 10, 20, 30, 40, 50, 60, 70, 80]), 1 << 20
+    for w in (NULL, FAKE):
+        for at in (lengths - 16, lengths + 16):
+            assert accept(lay=lay, arr=arrays(d_lengths=lengths), at=at, q=w, lse=w, w=w) == 2
+            assert b"overlaps" in B.lib().slkv_last_error()
+
+
 def bare_cache(monkeypatch):
     cache = api.Cache.__new__(api.Cache)
     cache.__dict__.update(layout=layout(), B=2, Hq=8, Hkv=2, d=128, query_dtype=torch.bfloat16, device=torch.device("cpu"), weight=torch.zeros(190), rows_in_all=190, _arrays=None,
