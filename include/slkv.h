@@ -458,7 +458,7 @@ typedef struct {
   const int64_t* h_cu_q;       /* [B+1] host: queries, non-decreasing, >= 0, last < 2^31 */
   const int64_t* h_cu_k;       /* [B+1] host: tokens of K and V, of a sequence 2^30 at most; NULL: h_cu_q (whole prompts) */
   /* element (head, token, :) of an array at head*stride_head + token*stride_tok; rows of d elements contiguous; strides >= 0 and multiples of 16
-   * bytes, 0 among them (out: rows may not overlap); token strides of k and v below 2^24 bytes */
+   * bytes, 0 among them (out: rows may not overlap); token strides of k and v below 2^24 bytes; element numbers below 2^40 */
   int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head, out_stride_tok, out_stride_head;
 } slkv_prompt_desc;
 

@@ -66,7 +66,6 @@ struct PromptTab {
     w.rows = rows;
     w.r0 = tile * QUERIES;
     w.hist = keys - new_tokens;
-    w.n = keys;
     const int last = (min(w.r0 + QUERIES, rows) - 1) / a.G, end = min(max(w.hist + last + 1, 0), keys);
     const int steps = (end + KEYS - 1) / KEYS, each = (steps + parts_here - 1) / parts_here * KEYS;
     w.parts = each ? (end + each - 1) / each : 1;
@@ -160,15 +159,20 @@ static slkv_status prompt_checks(const slkv_prompt_desc* d, PromptPlan& plan) {
     if (strides[i] < 0 || strides[i] > (int64_t(1) << 40) || strides[i] * elt % 16) return fail(SLKV_ERR_BAD_ARG, "stride %lld not a non-negative multiple of 16 bytes", (long long)strides[i]);
     if ((i == 4 || i == 6) && strides[i] * elt >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "token stride %lld of keys or values: 2^24 bytes and more", (long long)strides[i]);
   }
-  const int64_t n = d->h_cu_q[d->B] - d->h_cu_q[0];
-  const bool by_head = (n < 2 || d->out_stride_tok >= d->d) && (d->Hq < 2 || d->out_stride_head >= (n - 1) * d->out_stride_tok + d->d);
-  const bool by_token = (d->Hq < 2 || d->out_stride_head >= d->d) && (n < 2 || d->out_stride_tok >= (d->Hq - 1) * d->out_stride_head + d->d);
-  if (n && !by_head && !by_token) return fail(SLKV_ERR_BAD_ARG, "out: rows overlap");
   const int64_t G = d->Hq / d->Hkv;
   for (int64_t b = 0; b < d->B; ++b)
     if (cu_k_of(d)[b + 1] - cu_k_of(d)[b] > (int64_t(1) << 30)) return fail(SLKV_ERR_UNSUPPORTED, "sequence %lld: more than 2^30 tokens", (long long)b);
   for (int64_t b = 0; b < d->B; ++b)
     if ((d->h_cu_q[b + 1] - d->h_cu_q[b]) * G >= (int64_t(1) << 31) - 512) return fail(SLKV_ERR_UNSUPPORTED, "sequence %lld: 2^31 - 512 query rows of a KV head and more", (long long)b);
+  const int64_t n = d->h_cu_q[d->B] - d->h_cu_q[0];
+  // (element numbers stay below 2^40)
+  const int64_t tokens = cu_k_of(d)[d->B];
+  for (int i = 0; i < 8; i += 2)
+    if ((double)(i < 4 ? d->h_cu_q[d->B] : tokens) * strides[i] + (double)(i < 4 ? d->Hq : d->Hkv) * strides[i + 1] > 0x1p40)
+      return fail(SLKV_ERR_BAD_ARG, "strides %lld, %lld reach beyond 2^40 elements", (long long)strides[i], (long long)strides[i + 1]);
+  const bool by_head = (n < 2 || d->out_stride_tok >= d->d) && (d->Hq < 2 || d->out_stride_head >= (n - 1) * d->out_stride_tok + d->d);
+  const bool by_token = (d->Hq < 2 || d->out_stride_head >= d->d) && (n < 2 || d->out_stride_tok >= (d->Hq - 1) * d->out_stride_head + d->d);
+  if (n && !by_head && !by_token) return fail(SLKV_ERR_BAD_ARG, "out: rows overlap");
   plan = plan_prompt(d);
   if (plan.slots >= (1 << 24)) return fail(SLKV_ERR_UNSUPPORTED, "more than 2^24 workgroups");
   return SLKV_OK;

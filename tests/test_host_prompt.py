@@ -38,7 +38,7 @@ def test_struct_size_matches_the_header():
     (dict(d=96), 4), (dict(Hq=7), 2), (dict(dtype=5), 2), (dict(dtype=-1), 2), (dict(dtype=B.SLKV_BF16_KV_MXFP4), 4), (dict(B=0, cu_q=[0], cu_k=None), 2),
     (dict(cu_q=[0, 30, 20]), 2), (dict(cu_q=[-1, 30, 50]), 2), (dict(cu_k=[0, 100, 90]), 2), (dict(cu_k=[-2, 100, 130]), 2), (dict(cu_q=[0, 1, 2 ** 31]), 2),
     (dict(cu_k=[0, 1, 2 ** 31]), 2), (dict(Hkv=0, Hq=0), 2), (dict(Hq=1 << 17, Hkv=1), 2), (dict(cu_q=[0, 0, 2 ** 30], cu_k=None), 4), (dict(cu_k=[0, 1, 2 ** 30 + 2]), 4),
-    (dict(strides={0: 4}), 2), (dict(strides={3: -128}), 2), (dict(strides={2: 1 << 23}), 4), (dict(strides={4: 1 << 23}), 4), (dict(strides={5: 1 << 41}), 2),
+    (dict(strides={0: 4}), 2), (dict(strides={3: -128}), 2), (dict(strides={2: 1 << 23}), 4), (dict(strides={4: 1 << 23}), 4), (dict(strides={5: 1 << 41}), 2), (dict(strides={0: 1 << 38}), 2), (dict(strides={3: 1 << 39}), 2),
     (dict(strides={6: 0}), 2), (dict(strides={7: 128}), 2), (dict(strides={6: 64}), 2), (dict(strides={7: 49 * 128}), 2), (dict(strides={6: 7 * 128, 7: 128}), 2),
 ])
 def test_refused_descriptors(over, status):
