@@ -24,7 +24,6 @@ namespace slkv {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-
 // Segment and tile of a workgroup; the same in all its lanes.
 struct TileWork {
   const unsigned char *k, *v, *ks, *vs;   // first row of the segment
@@ -36,7 +35,6 @@ struct TileWork {
   int64_t k_row, v_row;                   // bytes
   int rows, r0;                           // query rows of the segment; first one of the tile
   int hist;                               // token t sees the keys j <= hist + t, or j < hist and those of its bits
-  int n;                                  // keys of the segment
   int begin, end;                         // keys of this part of the tile's
   int part, parts;                        // parts that have keys, 1 at least
   int slot0, slot_step;                   // where the parts' results are
@@ -66,7 +64,7 @@ struct Tiles {
   static constexpr bool kF32 = KIND == SLKV_F32;
   static constexpr bool kNarrow = Kind<KIND>::kBits < 16;
   static constexpr int kWaves = WQ * WK, kThreads = kWaves * kWave;
-  static constexpr int kQueries = 32 * WQ;        // query rows of a workgroup
+  static constexpr int kQueries = 32 * WQ;             // query rows of a workgroup
   static constexpr int kSub = WK == 1 ? 2 : 1;         // subtiles of 32 keys that a wave takes of a staged tile
   static constexpr int kKeys = 32 * kSub * WK;         // rows of a staged tile
   static constexpr int kRow = D * (int)sizeof(wide);   // bytes of a row in LDS

@@ -53,13 +53,13 @@ struct TreeTab {
     w.part = p.part;
     w.rows = a.G * a.T;
     w.r0 = p.tile * QUERIES;
-    w.n = __builtin_amdgcn_readfirstlane(rows_in_use(lengths, seg, room));
-    w.hist = w.n - a.T;
+    const int n = __builtin_amdgcn_readfirstlane(rows_in_use(lengths, seg, room));
+    w.hist = n - a.T;
     // the rows in use are spread over the parts of the room
-    const int steps = (w.n + KEYS - 1) / KEYS, each = (steps + parts - 1) / parts * KEYS;
-    w.parts = each ? (w.n + each - 1) / each : 1;
+    const int steps = (n + KEYS - 1) / KEYS, each = (steps + parts - 1) / parts * KEYS;
+    w.parts = each ? (n + each - 1) / each : 1;
     w.begin = w.part * each;
-    w.end = min(w.n, w.begin + each);
+    w.end = min(n, w.begin + each);
     w.k = k + (int64_t)at * kRow;
     w.v = v + (int64_t)at * kRow;
     w.ks = KIND == SLKV_BF16_KV_MXFP4 ? k_scale + (int64_t)at * kScales : nullptr;

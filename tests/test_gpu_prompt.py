@@ -110,6 +110,22 @@ def test_enough_queries_for_every_split_of_a_workgroup(dtype, Hq, Hkv, n):
         check(dtype, 3, 1, 128, cu, cu, q[heads], k[h:h + 1], v[h:h + 1], out[heads], lse[heads])
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,d", [("bf16", 64, 8, 128), ("bf16_kv8", 24, 8, 64), ("f16", 40, 8, 128)])
+def test_many_tiles_of_unequal_sequences(dtype, Hq, Hkv, d):
+    """So many tiles that they are taken in the order of their keys, whatever sequence they are of; sequences without queries, without keys, with fewer keys than queries."""
+    rng = np.random.default_rng(Hq)
+    n = [300, 0, 650, 17, 411, 128, 40, 5, 1, 222, 333, 700, 260, 0, 90]
+    m = [x + y for x, y in zip(n, [0, 30, 0, 400, 90, 0, -10, 0, 0, -222, 1, 64, 0, 0, 1000])]
+    cu_q, cu_k = offsets(n, 3), offsets(m, 1)
+    q, k, v = inputs(rng, dtype, Hq, Hkv, d, cu_q, cu_k)
+    out, lse = api.PromptCall(dtype, len(n), Hq, Hkv, d, cu_q, cu_k).run(q, k, v)
+    torch.cuda.synchronize()
+    G = Hq // Hkv
+    for h in (0, 3, Hkv - 1):
+        heads = [h * G, h * G + G - 1]
+        check(dtype, 2, 1, d, cu_q, cu_k, q[heads], k[h:h + 1], v[h:h + 1], out[heads], lse[heads])
+
+
 def test_many_sequences():
     # more than one launch holds
     rng = np.random.default_rng(3)
