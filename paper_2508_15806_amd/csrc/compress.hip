@@ -1175,9 +1175,10 @@ struct OneScan {
 };
 
 // 16 bytes per lane from base + off into LDS at lds (the same for the whole wave) + 16 * lane.  The caller waits for it (vmcnt);
-// the compiler does not know of it.
+// the compiler does not know of it.  (s_nop 4: a load into LDS needs a wait state behind a scalar write of m0, and its scalar address five behind a
+// vector instruction that wrote it; inside a statement nobody else sees to either.)
 __device__ __forceinline__ void load_to_lds16(const unsigned char* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 // v of this lane and of the lane 32 away, added up, in both.
