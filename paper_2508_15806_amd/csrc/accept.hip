@@ -123,8 +123,9 @@ struct Weigh {
     for (int r0 = 0; r0 < R; r0 += 16) {
       const Query now = ahead;
       if (r0 + 16 < R) load_queries(r0 + 16);
-      // (a query that saw nothing has no weights; nor has one that is not there)
-      const float l2 = now.lse == -INFINITY || r0 + rq >= R ? INFINITY : now.lse * kLog2e;
+      // a query that saw nothing has no weights, whatever its products are; nor has one that is not there
+      const float l2 = now.lse * kLog2e;
+      const int sees = now.lse == -INFINITY || r0 + rq >= R ? -1 : tail ? now.sees : INT32_MAX;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         f32x4 x[A::kTiles];
@@ -148,7 +149,7 @@ struct Weigh {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
           const float e = exp2_fast(fmaf(x[j / 4][j % 4], a.c_log2, -l2));
-          w[s][j] += !tail || j0 + s * A::kStep + g * kEach + j <= now.sees ? e : 0.f;
+          w[s][j] += j0 + s * A::kStep + g * kEach + j <= sees ? e : 0.f;
         }
       }
     }

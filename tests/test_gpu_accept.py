@@ -160,6 +160,36 @@ def test_a_token_that_saw_nothing_adds_nothing():
     assert torch.equal(cache.weight, before) and cache.lengths.tolist() == [47]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_token_that_saw_nothing_adds_nothing_where_keys_are_not_finite(dtype, bad):
+    """Products that are infinities or NaN, before the draft and in it."""
+    rng = np.random.default_rng(13)
+    cache = random_cache(rng, dtype, 1, 1, 2, 64, [300], rooms=[310])
+    cache.k[[7, 200, 297]] = bad
+    before = cache.weight.clone()
+    q = normal(rng, (1, 2, 4, 64), dtype).abs() + 1
+    lse = torch.full((1, 2, 4), -float("inf"), device="cuda")
+    cache.accept(torch.tensor([[0, 1]], dtype=torch.int32).cuda(), 4, q=q, lse=lse)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.weight, before) and cache.lengths.tolist() == [298]
+
+
+@pytest.mark.parametrize("G,count", [(1, 1), (3, 2), (4, 4), (3, 7)])
+def test_infinite_products_make_infinite_weights(G, count):
+    """exp of an infinite product, for any number of accepted queries: what is beside them in their tile has no part in it."""
+    rng = np.random.default_rng(14)
+    cache = random_cache(rng, "bf16", 1, 1, G, 64, [150], rooms=[160])
+    cache.k[20] = float("inf")
+    q = normal(rng, (1, G, 8, 64), "bf16").abs() + 1
+    lse = torch.full((1, G, 8), 5.0, device="cuda")
+    path = torch.tensor([list(range(count))], dtype=torch.int32).cuda()
+    cache.accept(path, 8, q=q, lse=lse)
+    torch.cuda.synchronize()
+    assert cache.weight[20].item() == float("inf")
+    assert torch.isfinite(cache.weight[:cache.lengths.item()]).nonzero().flatten().tolist() == [j for j in range(142 + count) if j != 20]
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_weights_are_those_of_one_token_after_the_other(dtype):
     """A draft that is accepted leaves the cache that attending to its tokens one at a time leaves."""
