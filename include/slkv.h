@@ -434,7 +434,7 @@ slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_cache* cach
  * d_q [B][Hq][T][d], d_lse [B][Hq][T]: the drafted tokens' queries and what slkv_attend_tree gave for them; with them, for the new rows in use j,
  *   weight_out[j] = weight[j] + sum over the segment's query heads and the accepted tokens i that see j (j <= max(base_s, 0) + i) of exp(q_i . k_j / sqrt(d) - lse_i)
  *   (a token whose lse is -infinity adds nothing): the weights that slkv_attend_cache would have added, for slkv_evict_cache to rank by.
- * d_weight_out [rows] fp32; may be cache->d_weight itself.  d_q, d_lse and d_weight_out are given together, or all NULL.  cache->d_weight NULL: sums begin at 0.
+ * d_weight_out [rows] fp32; may be cache->d_weight itself, but not overlap it otherwise.  d_q, d_lse and d_weight_out are given together, or all NULL.  cache->d_weight NULL: sums begin at 0.
  * 1 <= T, A <= 64.  cache->d_lengths is required.  The result has the same bits every time.
  * Errors: NULL, BAD_ARG, UNSUPPORTED (T, A, Hq/Hkv > 2^14), HIP. */
 slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv_cache* cache, int32_t T, int32_t A, const int32_t* d_path, const int32_t* d_at,

@@ -287,6 +287,10 @@ extern "C" slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv
   // (a workgroup reads its own segment's number alone before it sets the length)
   if (d_at && d_at != cache->d_lengths && d_at < cache->d_lengths + S && cache->d_lengths < d_at + S)
     return fail(SLKV_ERR_BAD_ARG, "d_at overlaps d_lengths and is not d_lengths itself");
+  // (a row's weight is read and written by the same thread; rows of a segment in no order)
+  const int64_t rows = desc->h_offsets[S] - desc->h_offsets[0];
+  if (d_weight_out && cache->d_weight && d_weight_out != cache->d_weight && d_weight_out < cache->d_weight + rows && cache->d_weight < d_weight_out + rows)
+    return fail(SLKV_ERR_BAD_ARG, "d_weight_out overlaps the cache's weights and is not these themselves");
   a.lengths_later = d_q && (!d_at || d_at == cache->d_lengths);
   auto launch = [&](auto tab, int64_t s0, int64_t ns) {
     using TAB = decltype(tab);

@@ -58,6 +58,14 @@ def test_rows_of_the_draft_do_not_overlap_the_lengths():
             assert b"overlaps" in B.lib().slkv_last_error()
 
 
+def test_weights_do_not_overlap_those_of_the_cache():
+    """d_weight_out may be the cache's weights, not a part of them: a row's weight would be written while another workgroup reads it."""
+    lay, weight = layout(offsets=[40, 140, 170, 170, 230]), 1 << 20
+    for w in (weight - 189 * 4 // 16 * 16, weight - 16, weight + 16, weight + 189 * 4 // 16 * 16):
+        assert accept(lay=lay, arr=arrays(d_weight=weight), q=FAKE, lse=FAKE, w=w) == 2
+        assert b"d_weight_out overlaps" in B.lib().slkv_last_error()
+
+
 def bare_cache(monkeypatch):
     cache = api.Cache.__new__(api.Cache)
     cache.__dict__.update(layout=layout(), B=2, Hq=8, Hkv=2, d=128, query_dtype=torch.bfloat16, device=torch.device("cpu"), weight=torch.zeros(190), rows_in_all=190, _arrays=None,
