@@ -459,8 +459,9 @@ class PromptBatch:
         if desc is None:
             if len(self._strided) >= 64:
                 self._strided.clear()
-            desc = self._strided[strides] = PromptDesc.from_buffer_copy(self.desc)
+            desc = PromptDesc.from_buffer_copy(self.desc)
             desc.strides[:] = [t.stride(i) if t.shape[i] > 1 else 0 for t in tensors for i in (1, 0)]    # (torch leaves anything as the stride of one)
+            self._strided[strides] = desc                          # whole: another host thread may find it from here on
         return C.addressof(desc), desc
 
 
