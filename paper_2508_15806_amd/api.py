@@ -2,6 +2,7 @@
 workspace with torch, calls the library.  No arithmetic of the method lives here."""
 
 import contextlib
+import threading
 
 import numpy as np
 import torch
@@ -54,13 +55,17 @@ class _Buffers:
 
 
 class _OnDevice:
-    """What Cache and PromptCall share: the checks of a call's tensors and its stream."""
+    """What Cache and PromptCall share: the checks of a call's tensors, its stream, its scratch."""
+
+    # Held while a call with scratch is enqueued: the launches of calls of two host threads on one stream, and so in one workspace, follow each other call by call.
+    # (Of every object its own; this one is for objects that no constructor has seen.)
+    _enqueuing = threading.Lock()
 
     def _set_device(self, device):
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        self._here, self._workspaces = contextlib.nullcontext(), {}
+        self._here, self._workspaces, self._enqueuing = contextlib.nullcontext(), {}, threading.Lock()
 
     def _tensor(self, t, shape, tdt, name, contiguous=True):
         if t.dtype != tdt or t.shape != shape:
@@ -80,7 +85,7 @@ class _OnDevice:
         return self._here if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
 
     def _workspace(self, nbytes, stream):
-        """Scratch for a call on the stream of this handle, which is the current one.  Calls that follow each other on a stream share it, and it grows with
+        """Scratch for a call on the stream of this handle, which is the current one; taken and used with self._enqueuing held.  Calls that follow each other on a stream share it, and it grows with
         the largest of them; a captured call has its own, which stays with its graph: the graph may be replayed anywhere.  (0.2 to 0.4 us of the host; a tensor for every call 0.9.)"""
         ws = None if torch.cuda.is_current_stream_capturing() else self._workspaces.get(stream, _NOTHING)
         if ws is None:
@@ -159,7 +164,8 @@ class PromptCall(_OnDevice):
     """Causal attention of a batch of packed prompts, or of their next pieces behind a history: what comes before LayerCall in a layer.
 
     cu_seqlens [B + 1]: the queries of every sequence; cu_k [B + 1]: its keys, of which the queries are the latest; None: the same.  Calls run on `stream`, or the
-    current stream of the device, and have scratch of their own on every stream and in every graph that torch captures; the object outlives these graphs."""
+    current stream of the device, and have scratch of their own on every stream and in every graph that torch captures; the object outlives these graphs.  Several host threads may
+    call one object."""
 
     def __init__(self, dtype, B_, Hq, Hkv, d, cu_seqlens, cu_k=None, device="cuda"):
         code, self.query_dtype, self.row_dtype = DTYPES[dtype]
@@ -191,7 +197,8 @@ class PromptCall(_OnDevice):
                 lse = self._lse_like = torch.empty((self.Hq, self.queries), dtype=torch.float32, device=self.device)
             else:
                 lse = torch.empty_like(self._lse_like)
-            B.slkv_attend_prompt(self.batch, q, k, v, out, self._workspace(self.workspace_bytes, handle), lse, handle)
+            with self._enqueuing:
+                B.slkv_attend_prompt(self.batch, q, k, v, out, self._workspace(self.workspace_bytes, handle), lse, handle)
         return out, lse
 
 
@@ -255,7 +262,7 @@ class Cache(_OnDevice):
     k_scale, v_scale [rows, d / 32] uint8; lengths [B * Hkv], pos [rows] int32; weight [rows] fp32); given keys without lengths fill their
     rooms.  positions, weights = False: a cache without these arrays.  Calls run on `stream`, or the current stream of the cache's device; the caller orders those that
     read or write the same arrays on several streams (attend() writes the weights where it has to add to them), and the object outlives the graphs that
-    captured them.  attend() has scratch of its own on every stream and in every graph that torch captures."""
+    captured them.  attend() and attend_tree() have scratch of their own on every stream and in every graph that torch captures; several host threads may call one object."""
 
     def __init__(self, dtype, B_, Hq, Hkv, d, offsets, k=None, v=None, k_scale=None, v_scale=None, lengths=None, pos=None, weight=None,
                  device="cuda", positions=True, weights=True):
@@ -290,13 +297,13 @@ class Cache(_OnDevice):
         self._arrays = B.CacheTensors(self.k, self.v, self.k_scale, self.v_scale, self.lengths, self.pos, self.weight)
         self._attend_like, self._tree_bytes = {}, {}
 
-    def _attend_buffers(self, T, weights, stream):
-        """A workspace for a call on the stream of this handle, and a tensor in the shape of its lse."""
+    def _attend_shape(self, T, weights):
+        """How large a call's workspace is, and a tensor in the shape of its lse."""
         like = self._attend_like.get((T, weights))
         if like is None:
             like = B.slkv_attend_workspace_bytes(self.layout, T, weights), torch.empty((self.B, self.Hq, T), dtype=torch.float32, device=self.device)
             self._attend_like[T, weights] = like
-        return self._workspace(like[0], stream), like[1]
+        return like
 
     def fill(self, k_rows, v_rows, src_offsets, pos=None, stream=None):
         """The rows that a prefill kept (LayerCall's k_out, v_out, offsets, kept_idx) become the cache."""
@@ -340,10 +347,11 @@ class Cache(_OnDevice):
             self._tensor(weight, (self.rows_in_all,), torch.float32, "weight")
         with self._on(stream):
             handle = B._stream(None)
-            ws, lse_like = self._attend_buffers(T, weight is not None, handle)
+            need, lse_like = self._attend_shape(T, weight is not None)
             out = torch.empty_like(q) if out is None else self._tensor(out, shape, self.query_dtype, "out")
             lse = torch.empty_like(lse_like) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
-            B.slkv_attend_cache(self.layout, self._arrays, q, out, ws, lse, weight, handle)
+            with self._enqueuing:
+                B.slkv_attend_cache(self.layout, self._arrays, q, out, self._workspace(need, handle), lse, weight, handle)
         return out, lse
 
     def attend_tree(self, q, sees, out=None, lse=None, stream=None):
@@ -362,7 +370,8 @@ class Cache(_OnDevice):
                 need = self._tree_bytes[T] = B.slkv_tree_workspace_bytes(self.layout, T)
             out = torch.empty_like(q) if out is None else self._tensor(out, shape, self.query_dtype, "out")
             lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device) if lse is None else self._tensor(lse, shape[:3], torch.float32, "lse")
-            B.slkv_attend_tree(self.layout, self._arrays, q, sees, out, self._workspace(need, handle), lse, handle)
+            with self._enqueuing:
+                B.slkv_attend_tree(self.layout, self._arrays, q, sees, out, self._workspace(need, handle), lse, handle)
         return out, lse
 
     def accept(self, path, T, at=None, q=None, lse=None, weight=None, stream=None):
