@@ -175,7 +175,7 @@ class PromptCall(_OnDevice):
         self.keys = self.queries if cu_k is None else int(self.batch.cu_k[-1])
         self.workspace_bytes = B.slkv_prompt_workspace_bytes(self.batch)
         self._set_device(device)
-        self._lse_like = None
+        self._no_lse = None
 
     def _rows(self, t, heads, tokens, tdt, name):
         if self._tensor(t, (heads, tokens, self.d), tdt, name, contiguous=False).stride(2) != 1 and tokens:
@@ -193,10 +193,10 @@ class PromptCall(_OnDevice):
             out = torch.empty_like(q) if out is None else self._rows(out, self.Hq, self.queries, self.query_dtype, "out")
             if lse is not None:
                 self._tensor(lse, (self.Hq, self.queries), torch.float32, "lse")
-            elif self._lse_like is None:
-                lse = self._lse_like = torch.empty((self.Hq, self.queries), dtype=torch.float32, device=self.device)
             else:
-                lse = torch.empty_like(self._lse_like)
+                if self._no_lse is None:                # (holds no memory; naming type and device anew takes half a us)
+                    self._no_lse = torch.empty((0,), dtype=torch.float32, device=self.device)
+                lse = self._no_lse.new_empty((self.Hq, self.queries))
             with self._enqueuing:
                 B.slkv_attend_prompt(self.batch, q, k, v, out, self._workspace(self.workspace_bytes, handle), lse, handle)
         return out, lse

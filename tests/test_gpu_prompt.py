@@ -253,3 +253,25 @@ def test_streams_and_graphs():
         for i in range(2):
             assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i])), turn
             assert all(torch.equal(a, b) for a, b in zip(got[i], want[2 + i])), turn
+
+
+def test_first_call_inside_a_capture():
+    """An object whose first call is captured: replays with other work between them, calls outside the graph, and its outputs after the graph is gone."""
+    rng = np.random.default_rng(15)
+    cu_q, cu_k = offsets([4, 30]), offsets([5000, 3001])
+    q, k, v = inputs(rng, "bf16", 8, 2, 128, cu_q, cu_k)
+    call, other = (api.PromptCall("bf16", 2, 8, 2, 128, cu_q, cu_k) for _ in range(2))
+    want = [x.clone() for x in other.run(q, k, v)]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = call.run(q, k, v)
+    for turn in range(3):
+        for x in got:
+            x.zero_()
+        g.replay()
+        again = call.run(q, k, v)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) and torch.equal(c, b) for a, b, c in zip(got, want, again)), turn
+    del g, got
+    assert all(torch.equal(a, b) for a, b in zip(call.run(q, k, v), want))

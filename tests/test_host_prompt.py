@@ -1,7 +1,10 @@
 """CPU-only tests of slkv_attend_prompt: descriptors, refusals before any GPU call, workspace sizes, the checks of api.PromptCall."""
 
+import contextlib
 import ctypes as C
+import gc
 import types
+import weakref
 
 import numpy as np
 import pytest
@@ -94,6 +97,21 @@ def test_prompt_call_checks_its_tensors(monkeypatch):
         api.PromptCall("bf16", 2, 8, 2, 128, [0, 30], device="cpu:0")
     with pytest.raises(ValueError, match="stream"):
         api.PromptCall("bf16", 1, 8, 2, 128, [0, 30], device="cuda:0")._on(types.SimpleNamespace(device=torch.device("cuda", 1)))
+
+
+def test_prompt_call_keeps_no_outputs(monkeypatch):
+    """An output is the caller's alone: its memory, or that of the graph whose capture made it, is free when the caller lets it go."""
+    call = api.PromptCall("bf16", 2, 8, 2, 128, [0, 30, 50], device="cpu:0")
+    call.device = torch.device("cpu")
+    monkeypatch.setattr(call, "_on", lambda stream: contextlib.nullcontext(), raising=False)
+    monkeypatch.setattr(B, "_stream", lambda stream: 0)
+    monkeypatch.setattr(B, "slkv_attend_prompt", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    q, k = torch.zeros((8, 50, 128), dtype=torch.bfloat16), torch.zeros((2, 50, 128), dtype=torch.bfloat16)
+    for _ in range(2):
+        kept = [weakref.ref(x) for x in call.run(q, k, k)]
+        gc.collect()
+        assert all(x() is None for x in kept)
 
 
 def test_oracle_against_a_loop():
