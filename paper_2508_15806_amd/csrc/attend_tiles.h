@@ -231,13 +231,17 @@ struct Tiles {
     if constexpr (kF32) {
       const int g = lane >> 5, l32 = lane & 31;
       const uint32_t at = vt + 4 * g * kRow + (uint32_t)((l32 / 4) ^ (g << 3)) * 16 + l32 % 4 * 4;
+      // The 32 keys are summed on their own, in two chains, and then added: a product adds two keys, and a sum that takes 16384 of these loses what the weights' sum keeps.
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
+      for (int dt = 0; dt < kDT; ++dt) {
+        f32x16 y[2] = {f32x16{}, f32x16{}};
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) {
+        for (int i = 0; i < 16; ++i) {
           const float v = lds_at<float>((at ^ (uint32_t)((i & 3 | (i >> 2 & 1) << 2 | dt << 3) * 16)) + (i / 4 * 8 + i % 4) * kRow);
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], acc[dt], 0, 0, 0);
+          y[i % 2] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], y[i % 2], 0, 0, 0);
         }
+        acc[dt] += y[0] + y[1];
+      }
     } else {
       // lane i of 16 reads the piece i % 4, of 8 bytes, of row i / 4: of the rows 4 g .. 4 g + 3 and, with j2, 8 rows on; 16 dims to 16 lanes
       const int g = lane >> 5, h = lane >> 4 & 1, i4 = lane >> 2 & 3, i1 = lane >> 1 & 1;
@@ -423,13 +427,17 @@ __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) 
       }
       // (one rounding, of the difference: a large product's own would be an error of the weight)
       const float from = ref == -INFINITY ? 0.f : ref;
+      // A step's weights are added to each other first, in four chains: the sum takes one addition for every 64 keys (WK = 4: 128).  (Added one by one, thousands of weights of 2^-24 of
+      // it leave no trace: a lane's half of 32767 of them behind one large key was lost, 8.7e-4 of the log-sum-exp.)
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           x[s][i] = exp2_fast(fmaf(x[s][i], a.c_log2, -from));
-          sum += x[s][i];
+          part[i % 4] += x[s][i];
         }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
       for (int s = 0; s < kSub; ++s) {
         const uint32_t vs = vt + s * 32 * A::kRow;

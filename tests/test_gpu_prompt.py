@@ -7,7 +7,7 @@ import torch
 from oracle import decode
 from oracle.prompt import attend_prompt
 from paper_2508_15806_amd import api
-from decode_parity import f64, normal
+from decode_parity import HALF_STEP, f64, normal
 from tile_parity import check_outputs
 
 pytestmark = pytest.mark.gpu
@@ -211,6 +211,43 @@ def test_large_logits(dtype):
     out, lse = api.PromptCall(dtype, 1, 2, 1, 64, cu).run(q, k, v)
     torch.cuda.synchronize()
     check(dtype, 2, 1, 64, cu, cu, q, k, v, out, lse)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", [(8, 2, 32768), (1, 1, 3), (1, 1, 100)])
+def test_a_long_flat_tail_behind_one_large_key(dtype, d, Hq, Hkv, n):
+    """The first key has a logit x of 16.75 or 16.8, all others 0: each of them has less than 2^-24 of the first one's weight, half an ulp of it, all together 2e-3 of it.  Whole prompts whose
+    tiles go through all keys, and few queries behind 32765.
+
+    Query i, of the keys 0 .. i: with w = exp(-x), lse = x + ln(1 + i w), out = (v_0 + w sum_j v_j) / (1 + i w).  Products are exact; a logit of 24.2 in base 2 and what the
+    log-sum-exp is made of are rounded five times (2^-18 in all); a sum over m keys takes at most one addition for every 32 keys, and 64 more inside steps, between lanes, waves and parts."""
+    if dtype == "f32" and n == 32768:
+        Hq, Hkv = 4, 4
+    m, u, rng = 32768, 2.0 ** -24, np.random.default_rng(d)
+    q, k = torch.zeros((Hq, n, d), device="cuda"), torch.zeros((Hkv, m, d), device="cuda")
+    of_q, of_k = ((8.0, 8.0), (16.0, 0.75)) if d == 64 else ((16.0, 8.0), (12.0, -0.25))      # products of 134 and 190
+    q[:, :, 1], q[:, :, 5] = of_q
+    k[:, 0, 1], k[:, 0, 5] = of_k
+    x = (of_q[0] * of_k[0] + of_q[1] * of_k[1]) / d ** 0.5
+    tdt = api.DTYPES[dtype][1]
+    q, k = q.to(tdt), narrow(k.to(tdt), dtype)
+    v = narrow(normal(rng, (Hkv, m, d), dtype).abs(), dtype)
+    cu_q, cu_k = offsets([n]), offsets([m])
+    out, lse = api.PromptCall(dtype, 1, Hq, Hkv, d, cu_q, cu_k).run(q, k, v)
+    torch.cuda.synchronize()
+    rows = np.unique(np.concatenate([[0, n - 1], rng.integers(0, n, 200)]))
+    i = m - n + rows
+    w = np.exp(-x)
+    assert 0.5 * u < w < u
+    sums = (m / 32 + 64) * u
+    np.testing.assert_allclose(f64(lse[:, rows]), np.broadcast_to(x + np.log1p(i * w), (Hq, len(rows))), rtol=0, atol=2.0 ** -18 + sums)
+    for h in range(Hq):
+        vv = values(v[h // (Hq // Hkv)])
+        o = (vv[0] + w * (np.cumsum(vv, 0)[i] - vv[0])) / (1 + i * w)[:, None]
+        # weights in the queries' type: half a step of each; outputs rounded once; v >= 0, so the sum of p |v| is out itself
+        half = HALF_STEP[dtype]
+        np.testing.assert_allclose(f64(out[h, rows]), o, rtol=2 * (2.0 ** -18 + sums) + (0 if dtype == "f32" else 2 * half + half ** 2), atol=0)
 
 
 def test_same_bits_every_time():
