@@ -417,8 +417,8 @@ slkv_status slkv_evict_cache(const slkv_cache_desc* desc, const slkv_cache* cach
 
 /* Attention of T drafted tokens, the nodes of a tree (or several), over the rows in use, the last T of which are theirs: row n_s - T + u is drafted token u's.  Drafted
  * token t of sequence b sees all rows before the draft, and drafted token u's row exactly if bit u of d_sees[b][t] is set (bits from T on mean nothing); rows that are not there
- * (n_s < T) are seen by none.  lse and out as in slkv_attend_cache, of the rows that the token sees; the rest of what is said there holds, but for weights: they enter the
- * product with v rounded to the type of the queries as in slkv_attend_prompt, and none are added up (slkv_accept_cache does that for the tokens that turn out to be right).
+ * (n_s < T) are seen by none.  lse and out as in slkv_attend_cache, of the rows that the token sees; the rest of what is said there holds, weights enter the
+ * product with v as in slkv_attend_prompt, and none are added up (slkv_accept_cache does that for the tokens that turn out to be right).
  * d_q, d_out [B][Hq][T][d];  d_sees [B][T] 64-bit numbers;  1 <= T <= 64, any Hq/Hkv;  d_lse [B][Hq][T] fp32, may be NULL
  * Workspace: as for slkv_attend_cache, of slkv_tree_workspace_bytes.
  * Errors: NULL, BAD_ARG, UNSUPPORTED (T), WORKSPACE, HIP. */
@@ -447,8 +447,8 @@ slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv_cache* cac
  *   lse = ln sum_j exp(x_j),  out = sum_j exp(x_j - lse) v_j.
  * A query that sees no key (n_b > m_b): out 0, lse -infinity.  Infinities and NaN in keys and values that a query does not see do not reach it.  The result does
  * not depend on what else runs, and has the same bits every time.
- * Products q . k are exact (fp32 elements: rounded), their sums, the softmax and lse fp32; a weight enters the product with v as it is for SLKV_F32, otherwise rounded to
- * the type of the queries relative to a power of two near the largest one; out is rounded once.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
+ * Products q . k are exact (fp32 elements: rounded), their sums, the softmax and lse fp32; a weight enters the product with v as it is for SLKV_F32, and as two 16-bit numbers otherwise, which hold it to
+ * 2^-16 of itself (SLKV_F16: to 2^-21 of itself or 2^-36 of the query's largest weight, whichever is more); out is rounded once.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
  */
 typedef struct {
   uint32_t struct_size;        /* sizeof(slkv_prompt_desc) */

@@ -226,7 +226,29 @@ struct Tiles {
     }
   }
 
-  // acc += p V of one subtile; vt: V in LDS, at the subtile
+  // Two weights >= 0 as a pair of 16-bit numbers, rounded towards 0, and the pair of what is left, which is above 0 wherever the first number is: an infinite value times the one and times the other
+  // makes no NaN.  bf16: 2^-20 of the weight more than what is left; fp16: 2^-24 at least, 2^-36 of the query's largest weight.  (With what is left as it is, and NaN looked for in the outputs and mended
+  // by a second turn, 2 to 40 % slower: registers.)
+  static __device__ __forceinline__ void halves(float x, float y, uint32_t& hi, uint32_t& lo) {
+    if constexpr (KIND == SLKV_F16) {
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x, y));
+      const u16x2 rest = __builtin_bit_cast(u16x2, __builtin_amdgcn_cvt_pkrtz(x - (float)h[0], y - (float)h[1]));
+      uint32_t one = 0x00010001u;
+      asm("" : "+s"(one));                             // (a minimum with a known 1 becomes four comparisons and selections)
+      hi = __builtin_bit_cast(uint32_t, h);
+      lo = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(rest, __builtin_elementwise_min(__builtin_bit_cast(u16x2, h), __builtin_bit_cast(u16x2, one))));
+    } else {
+      constexpr float kMore = 1.f + 0x1p-20f;
+      const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+      hi = __builtin_amdgcn_perm(yb, xb, 0x07060302u);
+      lo = pair(fmaf(x, kMore, -__uint_as_float(xb & 0xffff0000u)), fmaf(y, kMore, -__uint_as_float(yb & 0xffff0000u)));
+    }
+  }
+
+  // acc += p V of one subtile; vt: V in LDS, at the subtile.  16-bit types: a weight enters as two numbers, which hold it to 2^-16 (fp16: 2^-21) of itself, as in slkv_attend_cache: one
+  // would add as much error as the output's own rounding.  The second product is half of the call's matrix work more: a third of the time where that is what a call takes its time with (32 heads of
+  // 128 in bf16: 32768 tokens 7.9 ms with one number, 10.6 with two; 512 queries behind 65024 keys 555, 715 us), 6 % where it is not (32 drafted tokens on 128 segments of 1024 rows 38.5, 40.8 us).
   static __device__ __forceinline__ void add_values(f32x16 (&acc)[kDT], const f32x16& p, uint32_t vt, int lane) {
     if constexpr (kF32) {
       const int g = lane >> 5, l32 = lane & 31;
@@ -249,21 +271,27 @@ struct Tiles {
       const uint32_t at = vt + row * kRow + (uint32_t)((2 * h + i1) ^ swizzle(row)) * 16 + (lane & 1) * 8;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        u32x4 po;
+        u32x4 hi, lo, vo[kDT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) po[j] = pair(p[c * 8 + j * 2], p[c * 8 + j * 2 + 1]);
+        for (int j = 0; j < 4; ++j) {
+          uint32_t h2, l2;
+          halves(p[c * 8 + j * 2], p[c * 8 + j * 2 + 1], h2, l2);
+          hi[j] = h2;
+          lo[j] = l2;
+        }
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) {
-          u32x4 vo;
+        for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
           for (int j2 = 0; j2 < 2; ++j2) {
             // 8 rows on: swizzle changes bit 1
             const u32x2 t = read_turned((at ^ (uint32_t)(dt * 64 ^ j2 * 32)) + (c * 16 + j2 * 8) * kRow);
-            vo[j2 * 2] = t[0];
-            vo[j2 * 2 + 1] = t[1];
+            vo[dt][j2 * 2] = t[0];
+            vo[dt][j2 * 2 + 1] = t[1];
           }
-          acc[dt] = mfma(vo, po, acc[dt]);
-        }
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) acc[dt] = mfma(vo[dt], hi, acc[dt]);
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) acc[dt] = mfma(vo[dt], lo, acc[dt]);
       }
     }
   }
