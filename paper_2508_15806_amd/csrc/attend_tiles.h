@@ -15,9 +15,9 @@
 
 #include "attend_rows.h"
 #include "launch.h"
+#include "tile_plan.h"
 
 #include <algorithm>
-#include <cmath>
 
 namespace slkv {
 
@@ -684,12 +684,6 @@ __global__ __launch_bounds__(256) void join_tiles_kernel(const TileArgs a, const
 
 // ------------------------------------------------------------------ host
 
-// Waves of a workgroup: along the queries, along the keys of a staged tile.
-struct TileShape { int wq, wk; };
-constexpr TileShape kTileShapes[] = {{1, 4}, {2, 2}, {4, 1}, {4, 2}, {8, 1}};
-constexpr int kTileShapeCount = 5;
-inline int tile_queries(int shape) { return 32 * kTileShapes[shape].wq; }
-
 // Workgroups of a launch, at most: as many as the registers and LDS of the chip have places for.
 template <class A>
 constexpr unsigned tile_places() {
@@ -698,65 +692,16 @@ constexpr unsigned tile_places() {
   return 256 * (unsigned)std::max(1, std::min(waves, lds));
 }
 
-// f with the waves of a shape as compile-time constants.  fp32 has two shapes: others do not fit LDS or registers.
-template <int KIND, class F>
+// f with the waves of a shape as compile-time constants.
+template <int KIND, int D, int S = 0, class F>
 void with_shape(int shape, F f) {
-  using std::integral_constant;
-  integral_constant<int, 1> one;
-  integral_constant<int, 2> two;
-  integral_constant<int, 4> four;
-  if constexpr (KIND != SLKV_F32) {
-    if (shape == 0) return f(one, four);
-    if (shape == 3) return f(four, two);
-    if (shape == 4) return f(integral_constant<int, 8>{}, one);
-  }
-  if (shape == 1) return f(two, two);
-  f(four, one);
-}
-
-// What a call consists of in a shape: workgroups without parts, keys of all and of the longest.
-struct TileLoad { double tiles, keys, longest; };
-struct TileChoice { int shape; int64_t each; };        // each: keys of a part, at most
-
-// The shape and the parts that should be done first.  A workgroup takes kBegin us and, for every 64 keys (128: shape 0), alone[shape] us on a CU that it has to itself, loaded[shape] where all places are
-// taken; longer where nobody else reads the same rows.  The keys and values of all segments (bytes) come at 4.8 TB/s at best; parts cost a second launch, and their sums are written and read.
-// (us, bf16, d = 128, 32 heads, 8 KV heads: 32768 tokens in shape 4 7800, in 2 7900; 4096: 143, 152, in shape 1 169; 1024: 28 in shape 2, 22 in shape 1, 44 in shape 0; 130: 11.6, 9.2, 8.0;
-// 128 queries a segment on 128 segments of 1024 rows: 35 in shape 3 with parts of 900, 40 in shape 2, 38 in it with parts of 600, 53 of 200; 64 on 512 segments of 1024 MXFP4 rows: 55 in shape 1 whole, 102 with parts of 200.)
-template <class LOAD>
-TileChoice choose_tiles(int dtype, int d, int64_t rows, int64_t segments, double bytes, LOAD load) {
-  constexpr double kBegin = 5.5, kJoin = 6;
-  constexpr double kShared[] = {1.45, 0.85, 1.25, 1.2, 1.9}, kStreaming[] = {1.8, 1.5, 1.9, 1.4, 2.1}, kLoaded[] = {1.45, 1.24, 1.94, 1.2, 1.9};
-  constexpr int kKeys[] = {128, 64, 64, 64, 64}, kPlaces[] = {1, 2, 2, 1, 1};
-  const bool f32 = dtype == SLKV_F32, narrow = kind_bits(dtype) < 16;
-  TileChoice best{2, 1};
-  double least = 1e300;
-  for (int s = 0; s < kTileShapeCount; ++s) {
-    if (f32 && s != 1 && s != 2) continue;
-    if (s > 0 && rows <= tile_queries(s) / 2 && !(f32 && s == 1)) continue;   // (no more waves than queries)
-    if (d == 64 && s == 4) continue;                             // (8192 tokens in fp16: 354 us, 320 in shape 2)
-    const TileLoad l = load(tile_queries(s));
-    const double scale = (f32 ? (d == 64 ? 4 : 8) * (s == 1 ? 0.78 : 1) : d == 64 ? 0.55 : 1) * (narrow ? 1.2 : 1);
-    const double alone = (l.tiles < 4.0 * segments && !f32 ? kStreaming[s] : kShared[s]) * scale, loaded = f32 ? alone : std::max(kLoaded[s] * scale, alone) * (narrow && s == 0 ? 2 : 1);
-    const double places = 256.0 * (f32 ? 1 : narrow && s == 0 ? 2 : kPlaces[s]);
-    const bool even = l.keys > 0.95 * l.longest * l.tiles;
-    for (int parts = 1; parts <= 256; parts += parts < 4 ? 1 : parts / 2) {
-      const double each = std::ceil(std::ceil(l.longest / parts) / kKeys[s]) * kKeys[s];
-      const double groups = l.tiles * (parts == 1 ? 1 : even ? std::ceil(l.longest / each) : std::max(1.0, l.keys / l.tiles / each + 0.4));
-      const double steps = l.keys / kKeys[s] + 1.2 * groups, mean = std::min(1.0, steps / groups / (each / kKeys[s]));
-      const double one = each / kKeys[s] * (groups <= 256 ? alone : alone + (loaded - alone) * mean);
-      // (more workgroups than places: the last ones begin late; parts are about equal, whole tiles the longest first)
-      const double all = steps * loaded / places + (groups <= places ? 0 : parts > 1 ? 0.5 * one : 0.1 * one);
-      double us = kBegin + std::max(std::max(one, all), bytes / 4.8e6 + (parts > 1 || l.tiles < places ? 0.2 * one : 0));
-      if (parts > 1) us += kJoin + groups * tile_queries(s) * d * 8 / 6e6;
-      if (us < least) least = us, best = TileChoice{s, (int64_t)std::max(each, 1.0)};
-      if (each <= kKeys[s]) break;
+  if constexpr (S < kTileShapeCount) {
+    if constexpr (has_shape(KIND, D, S)) {
+      if (shape == S) return f(std::integral_constant<int, kTileShapes[S].wq>{}, std::integral_constant<int, kTileShapes[S].wk>{});
     }
+    with_shape<KIND, D, S + 1>(shape, f);
   }
-  return best;
 }
-
-// Workgroups of a part that join tiles.
-inline unsigned join_slices(int queries) { return (unsigned)std::max(1, queries / 32); }
 
 }  // namespace slkv
 #endif

@@ -50,9 +50,6 @@ struct Kind<SLKV_BF16_KV_FP8> { typedef __bf16 wide; static constexpr int kBits 
 template <>
 struct Kind<SLKV_BF16_KV_MXFP4> { typedef __bf16 wide; static constexpr int kBits = 4; };
 
-inline int kind_bits(int dtype) { return dtype == SLKV_F32 ? 32 : dtype == SLKV_BF16_KV_FP8 ? 8 : dtype == SLKV_BF16_KV_MXFP4 ? 4 : 16; }
-inline int wide_bytes(int dtype) { return dtype == SLKV_F32 ? 4 : 2; }
-
 // 2^(e - 127) as the operand of the converters, which read its exponent field: 0 stands for 2^-127, 255 for NaN.
 __device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
 

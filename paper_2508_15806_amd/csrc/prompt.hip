@@ -9,7 +9,7 @@ namespace slkv {
 // that with 8 of these a head stays on an XCD and its L2.  In order (where there are parts, and for sequences of one length, whose keys and values stay in the caches this way: 64 of 256 tokens 116 us, else
 // 128): sequence, tiles from the last one down, parts of the keys, KV heads.  (8 sequences of 110 to 4000 tokens: 436 us in order, else 412.)
 struct PromptTab {
-  static constexpr int kSeqs = 64;
+  static constexpr int kSeqs = kPromptSeqs;
   const unsigned char *k, *v, *q;
   unsigned char* out;
   float* lse;
@@ -85,58 +85,6 @@ struct PromptTab {
     return w;
   }
 };
-
-struct PromptPlan {
-  int shape;                         // waves and tiles of a workgroup
-  int queries;                       // rows of a workgroup's tile
-  int64_t each;                      // keys of a part, about
-  int64_t slots;                     // workgroups of a launch, the most
-  bool split;
-  size_t off_ml, bytes;
-};
-
-static int64_t seq_tiles(const slkv_prompt_desc* d, int64_t b, int queries) {
-  return ((d->h_cu_q[b + 1] - d->h_cu_q[b]) * (d->Hq / d->Hkv) + queries - 1) / queries;
-}
-static const int64_t* cu_k_of(const slkv_prompt_desc* d) { return d->h_cu_k ? d->h_cu_k : d->h_cu_q; }
-static int64_t seq_parts(const slkv_prompt_desc* d, int64_t b, int64_t each) {
-  return std::max<int64_t>(1, (cu_k_of(d)[b + 1] - cu_k_of(d)[b] + each - 1) / each);
-}
-
-static PromptPlan plan_prompt(const slkv_prompt_desc* d) {
-  PromptPlan p;
-  const int64_t G = d->Hq / d->Hkv;
-  const int64_t* ck = cu_k_of(d);
-  int64_t rows = 0, kv = 0;
-  for (int64_t b = 0; b < d->B; ++b) rows = std::max(rows, (d->h_cu_q[b + 1] - d->h_cu_q[b]) * G), kv += ck[b + 1] - ck[b];
-  const TileChoice c = choose_tiles(d->dtype, d->d, rows, (int64_t)d->B * d->Hkv, (double)kv * d->Hkv * d->d * kind_bits(d->dtype) / 4, [&](int queries) {
-    TileLoad l{0, 0, 1};
-    for (int64_t b = 0; b < d->B; ++b) {
-      const int64_t t = seq_tiles(d, b, queries) * d->Hkv, n = d->h_cu_q[b + 1] - d->h_cu_q[b], m = ck[b + 1] - ck[b];
-      if (!t) continue;
-      l.tiles += t;
-      l.keys += (double)t * std::max<int64_t>(1, m - n / 2);
-      l.longest = std::max(l.longest, (double)m);
-    }
-    l.tiles = std::max(l.tiles, 1.0);
-    return l;
-  });
-  p.shape = c.shape;
-  p.each = c.each;
-  p.queries = tile_queries(p.shape);
-  p.split = false;
-  for (int64_t b = 0; b < d->B; ++b) p.split |= seq_tiles(d, b, p.queries) && seq_parts(d, b, p.each) > 1;
-  p.slots = 0;
-  for (int64_t b0 = 0; b0 < d->B; b0 += PromptTab::kSeqs) {
-    int64_t here = 0;
-    for (int64_t b = b0; b < std::min<int64_t>(d->B, b0 + PromptTab::kSeqs); ++b) here += seq_tiles(d, b, p.queries) * d->Hkv * seq_parts(d, b, p.each);
-    p.slots = std::max(p.slots, here);
-  }
-  const size_t o = p.split ? (size_t)p.slots * p.queries * d->d * sizeof(float) : 0;
-  p.off_ml = o;
-  p.bytes = std::max<size_t>(16, o + (p.split ? (size_t)p.slots * p.queries * 2 * sizeof(float) : 0));
-  return p;
-}
 
 // Everything that can be checked without the arrays; the plan of a descriptor that passes.
 static slkv_status prompt_checks(const slkv_prompt_desc* d, PromptPlan& plan) {
@@ -234,8 +182,6 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
       const int64_t kx = length(x, ck), ky = length(y, ck);
       return kx != ky ? kx > ky : x < y;
     });
-    bool even = true;
-    for (int i = 1; i < t.nseq; ++i) even &= length(i, desc->h_cu_q) == length(0, desc->h_cu_q) && length(i, ck) == length(0, ck);
     int64_t blocks = 0;
     for (int i = 0; i < t.nseq; ++i) {
       const int64_t b = b0 + order[i];
@@ -247,12 +193,12 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
       blocks += seq_tiles(desc, b, p.queries) * desc->Hkv * x.parts[i];
     }
     t.words.first[t.nseq] = (int32_t)blocks;
-    t.in_order = p.split || even || blocks <= 512;     // (looking a tile up in the other order takes 1.5 us)
+    t.in_order = prompt_in_order(desc, p, b0);
     if (!blocks) continue;
     a.blocks = (int32_t)blocks;
     auto launch = [&](auto kind, auto dim) {
       constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
-      with_shape<kKind>(p.shape, [&](auto wq, auto wk) {
+      with_shape<kKind, kDim>(p.shape, [&](auto wq, auto wk) {
         constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
         {
           ScopedKernelTimer timer(SLKV_K_PROMPT);

@@ -16,6 +16,10 @@ constexpr int kMaxSegPerLaunch = 64;  // (sequence, KV head) segments whose ever
 slkv_status fail(slkv_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 void clear_error();
 
+// Bits of an element of K and V, bytes of one of the queries.
+inline int kind_bits(int dtype) { return dtype == SLKV_F32 ? 32 : dtype == SLKV_BF16_KV_FP8 ? 8 : dtype == SLKV_BF16_KV_MXFP4 ? 4 : 16; }
+inline int wide_bytes(int dtype) { return dtype == SLKV_F32 ? 4 : 2; }
+
 // Rows kept for a segment of n tokens, window w and capacity cap (Algorithm 3).
 int64_t kept_rows(int64_t n, int64_t w, int64_t cap);
 

@@ -78,46 +78,6 @@ struct TreeTab {
     return w;
   }
 };
-constexpr int kTreeSegs = 600;
-
-struct TreePlan {
-  int shape, queries;
-  int64_t each;                      // room rows of a part, at most
-  int64_t slots;
-  bool split;
-  size_t off_ml, bytes;
-};
-
-static int64_t tree_parts(const slkv_cache_desc* d, int64_t s, int64_t each) {
-  return std::max<int64_t>(1, (d->h_offsets[s + 1] - d->h_offsets[s] + each - 1) / each);
-}
-
-static TreePlan plan_tree(const slkv_cache_desc* d, int T) {
-  TreePlan p;
-  const int64_t S = (int64_t)d->B * d->Hkv, R = (int64_t)(d->Hq / d->Hkv) * T, rows = d->h_offsets[S] - d->h_offsets[0];
-  int64_t most = 1;
-  for (int64_t s = 0; s < S; ++s) most = std::max(most, d->h_offsets[s + 1] - d->h_offsets[s]);
-  const TileChoice c = choose_tiles(d->dtype, d->d, R, S, (double)rows * d->d * kind_bits(d->dtype) / 4, [&](int queries) {
-    const double tiles = (double)((R + queries - 1) / queries);
-    return TileLoad{S * tiles, std::max<double>(1, (double)rows) * tiles, (double)most};
-  });
-  p.shape = c.shape;
-  p.each = std::min(most, c.each);
-  p.queries = tile_queries(p.shape);
-  const int64_t tiles = (R + p.queries - 1) / p.queries;
-  p.split = most > p.each;
-  p.slots = 0;
-  for (int64_t s0 = 0; s0 < S; s0 += kTreeSegs) {
-    int64_t here = 0;
-    for (int64_t s = s0; s < std::min<int64_t>(S, s0 + kTreeSegs); ++s) here += tree_parts(d, s, p.each) * tiles;
-    p.slots = std::max(p.slots, here);
-  }
-  const size_t o = p.split ? (size_t)p.slots * p.queries * d->d * sizeof(float) : 0;
-  p.off_ml = o;
-  p.bytes = std::max<size_t>(16, o + (p.split ? (size_t)p.slots * p.queries * 2 * sizeof(float) : 0));
-  return p;
-}
-
 // The segments with the longest parts first, by sixteenths of the longest.
 template <class TAB>
 static void order_segments(TAB& t) {
@@ -199,7 +159,7 @@ extern "C" slkv_status slkv_attend_tree(const slkv_cache_desc* desc, const slkv_
     a.blocks = (int32_t)blocks;
     auto launch = [&](auto kind, auto dim) {
       constexpr int kKind = decltype(kind)::value, kDim = decltype(dim)::value;
-      with_shape<kKind>(p.shape, [&](auto wq, auto wk) {
+      with_shape<kKind, kDim>(p.shape, [&](auto wq, auto wk) {
         constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
         {
           ScopedKernelTimer timer(SLKV_K_TREE);
