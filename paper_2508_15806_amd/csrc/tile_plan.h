@@ -24,8 +24,9 @@ struct TileChoice { int shape; int64_t each; };        // each: keys of a part, 
 
 // The shape and the parts that should be done first.  A workgroup takes kBegin us and, for every 64 keys (128: shape 0), alone[shape] us on a CU that it has to itself, loaded[shape] where all places are
 // taken; longer where nobody else reads the same rows.  The keys and values of all segments (bytes) come at 4.8 TB/s at best; parts cost a second launch, and their sums are written and read.
-// (us, bf16, d = 128, 32 heads, 8 KV heads: 32768 tokens in shape 4 7800, in 2 7900; 4096: 143, 152, in shape 1 169; 1024: 28 in shape 2, 22 in shape 1, 44 in shape 0; 130: 11.6, 9.2, 8.0;
-// 128 queries a segment on 128 segments of 1024 rows: 35 in shape 3 with parts of 900, 40 in shape 2, 38 in it with parts of 600, 53 of 200; 64 on 512 segments of 1024 MXFP4 rows: 55 in shape 1 whole, 102 with parts of 200.)
+// (The figures are those of one 16-bit number a weight.  With two, full chips take 1.36 times as long in shapes 2 and 4, 1.2 in 1 and 3, 1.1 in 0, and with figures to match the rule chose worse: 4096 tokens in shape 2.
+// us, bf16, d = 128, 32 heads, 8 KV heads: 32768 tokens in shape 4 10600, in 2 10600, in 3 11920, in 1 12140; 4096: 180, 192, in shape 1 222; 1024: 30 in shape 2, 26 in shape 1, 47 in shape 0; 130: 9.0, 8.6, 8.1;
+// 128 queries a segment on 128 segments of 1056 rows: 34 in shape 3, 36 in shape 2, in two parts 33 and 35, in four 46 and 40; 64 on 512 segments of 1040 MXFP4 rows: 39 in shape 1 whole, 58 in two parts.)
 template <class LOAD>
 TileChoice choose_tiles(int dtype, int d, int64_t rows, int64_t segments, double bytes, LOAD load) {
   constexpr double kBegin = 5.5, kJoin = 6;
