@@ -10,6 +10,7 @@ import pytest
 
 import tile_plan
 from paper_2508_15806_amd import binding as B
+from tile_cases import PROMPTS, TREES
 
 ALL = {(dtype, d, waves) for dtype in range(5) for d in (64, 128) for i, waves in enumerate(tile_plan.shapes()) if tile_plan.has_shape(dtype, d, i)}
 
@@ -58,3 +59,31 @@ def test_the_plan_is_the_librarys():
 def test_order_of_tiles(n, m, in_order):
     plan = tile_plan.prompt(B.PromptBatch(B.SLKV_BF16, len(n), 32, 8, 128, cu(n), None if m is None else cu(m)))
     assert plan.in_order == in_order and not plan.split
+
+
+CODES = {"f32": B.SLKV_F32, "bf16": B.SLKV_BF16, "f16": B.SLKV_F16, "bf16_kv8": B.SLKV_BF16_KV_FP8, "bf16_kv4": B.SLKV_BF16_KV_MXFP4}
+
+
+@pytest.mark.parametrize("dtype,d,waves,kind,Hq,Hkv,n,m", PROMPTS)
+def test_programs_of_the_prompt_cases(dtype, d, waves, kind, Hq, Hkv, n, m):
+    plan = tile_plan.prompt(B.PromptBatch(CODES[dtype], len(n), Hq, Hkv, d, cu(n), None if m is None else cu(m)))
+    assert plan.waves == waves and plan.split == (kind == "split") and plan.in_order == (kind != "by keys")
+    assert plan.blocks > 256 or plan.split or waves[0] * waves[1] == 4
+
+
+@pytest.mark.parametrize("dtype,d,waves,kind,Hq,Hkv,seqs,T,room", TREES)
+def test_programs_of_the_tree_cases(dtype, d, waves, kind, Hq, Hkv, seqs, T, room):
+    plan = tile_plan.tree(B.CacheLayout(CODES[dtype], seqs, Hq, Hkv, d, np.arange(seqs * Hkv + 1) * room), T)
+    assert plan.waves == waves and plan.split == (kind == "split")
+    assert plan.blocks > 256 or plan.split or waves[0] * waves[1] == 4
+
+
+def test_the_cases_are_all_programs():
+    kinds = {(c[0], c[1], c[2], c[3]) for c in PROMPTS}
+    for dtype in ("f32", "bf16", "f16", "bf16_kv8"):
+        for d in (64, 128):
+            for i, waves in enumerate(tile_plan.shapes()):
+                if tile_plan.has_shape(CODES[dtype], d, i):
+                    # (few queries of E4M3 rows: no call has so many tiles of them, of unequal sequences)
+                    assert {k for k in ("split", "in order", "by keys") if (dtype, d, waves, k) in kinds} >= ({"split", "in order"} if (dtype, waves) == ("bf16_kv8", (1, 4)) else {"split", "in order", "by keys"})
+    assert {(CODES[c[0]], c[1], c[2], c[3]) for c in TREES} == {x + (k,) for x in ALL for k in ("split", "whole")}
