@@ -253,17 +253,19 @@ struct Tiles {
     if constexpr (kF32) {
       const int g = lane >> 5, l32 = lane & 31;
       const uint32_t at = vt + 4 * g * kRow + (uint32_t)((l32 / 4) ^ (g << 3)) * 16 + l32 % 4 * 4;
-      // The 32 keys are summed on their own, in two chains, and then added: a product adds two keys, and a sum that takes 16384 of these loses what the weights' sum keeps.
+      // The 32 keys are summed on their own and then added: a product adds two keys, and a sum that takes 16384 of these loses what the weights' sum keeps.
+      f32x16 y[kDT];
 #pragma unroll
-      for (int dt = 0; dt < kDT; ++dt) {
-        f32x16 y[2] = {f32x16{}, f32x16{}};
+      for (int dt = 0; dt < kDT; ++dt) y[dt] = f32x16{};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) {
           const float v = lds_at<float>((at ^ (uint32_t)((i & 3 | (i >> 2 & 1) << 2 | dt << 3) * 16)) + (i / 4 * 8 + i % 4) * kRow);
-          y[i % 2] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], y[i % 2], 0, 0, 0);
+          y[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], y[dt], 0, 0, 0);
         }
-        acc[dt] += y[0] + y[1];
-      }
+#pragma unroll
+      for (int dt = 0; dt < kDT; ++dt) acc[dt] += y[dt];
     } else {
       // lane i of 16 reads the piece i % 4, of 8 bytes, of row i / 4: of the rows 4 g .. 4 g + 3 and, with j2, 8 rows on; 16 dims to 16 lanes
       const int g = lane >> 5, h = lane >> 4 & 1, i4 = lane >> 2 & 3, i1 = lane >> 1 & 1;
