@@ -448,7 +448,7 @@ slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv_cache* cac
  * A query that sees no key (n_b > m_b): out 0, lse -infinity.  Infinities and NaN in keys and values that a query does not see do not reach it.  The result does
  * not depend on what else runs, and has the same bits every time.
  * Products q . k are exact (fp32 elements: rounded), their sums, the softmax and lse fp32; a weight enters the product with v as it is for SLKV_F32, and as two 16-bit numbers otherwise, which hold it to
- * 2^-16 of itself (SLKV_F16: to 2^-21 of itself or 2^-36 of the query's largest weight, whichever is more); out is rounded once.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
+ * 2^-16 of itself (SLKV_F16: to 2^-21 of itself or 2^-36 of the query's largest weight, whichever is more; an infinite v beside a weight that they cannot hold, below 2^-100 (SLKV_F16: 2^-36) of the largest, may give NaN); out is rounded once.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
  */
 typedef struct {
   uint32_t struct_size;        /* sizeof(slkv_prompt_desc) */

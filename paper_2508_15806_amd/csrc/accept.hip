@@ -75,8 +75,8 @@ __device__ __forceinline__ Accepted accepted_of(const AcceptArgs& a, int seg, in
 }
 
 // Weights of kWeighEach rows from row j0 of a segment on, up to `end`, one wave; those of the draft, from row `drafted` on, are seen by the tokens that were accepted with or
-// after them.  tokens: the accepted ones, in LDS.  Bound by latency and by memory: the rows' keys, what they have so far and the first queries are asked for at once, the next queries a tile
-// ahead.  (256 segments of 2048 E4M3 rows, 8 tokens: 27 us, 3.2 TB/s.  A wave that goes through several times as many rows, the next ones on their way in registers: 31 to 44.)
+// after them.  tokens: the accepted ones, in LDS.  Bound by latency and by memory: the rows' keys, what they have so far and the first queries are asked for at once, but only behind the path's
+// round trips (table, length, path) and a barrier; the next queries a tile ahead.  (256 segments of 2048 E4M3 rows, 8 tokens: 27 us, 3.2 TB/s.  A wave that goes through several times as many rows, the next ones on their way in registers: 31 to 44.)
 template <int KIND, int D>
 struct Weigh {
   using A = Attend<KIND, D>;

@@ -79,7 +79,7 @@ struct Tiles {
   static constexpr bool kSingle = kNarrow && WK == 4 && WQ == 1;
   static constexpr int kTilesBytes = (kSingle ? 2 : 4) * kTileBytes;
   // Whether a workgroup takes tiles in turn: the ones that have a CU to themselves.  Where workgroups share one they fill each other's beginnings and ends, and the chip deals tiles out
-  // more evenly (3 prompts of 1111 tokens in fp16, 512 places: 34 us, in turn on 768: 27, dealt out: 25).
+  // more evenly (3 prompts of 1111 tokens in fp16, with one number a weight: in turn on 512 places 34 us, on 768 27, dealt out 25; with two 31).
   static constexpr bool kTurns = kWaves == 8;
   static constexpr int kOutBytes = WK == 1 ? 0 : kWaves * 32 * kOutRow * 4;
   static constexpr int kLds = kTilesBytes > kOutBytes ? kTilesBytes : kOutBytes;
@@ -132,7 +132,8 @@ struct Tiles {
   static constexpr int kSrcChunks = kNarrow ? kSrcRow / 16 : 1;
   static constexpr int kUnits = kKeys * kSrcChunks, kFetch = (kUnits + kThreads - 1) / kThreads;
   struct Fetched { u32x4 k[kFetch], v[kFetch]; uint32_t ks[kFetch], vs[kFetch]; };
-  // a wave takes whole rows, its neighbouring lanes a piece of one after the other, so that what they write finds all banks
+  // A wave takes whole rows, neighbouring lanes the same piece of neighbouring rows: what 16 of them write lies in 64 different banks.  (All the same 30 % (MXFP4) and 39 % (E4M3) of the LDS cycles
+  // of narrow rows' kernels are conflicts, 10 and 13 % of all cycles; bf16 rows of 128 dims, which are read the same way and not written like this, have none.  The cause is not known.)
   static constexpr int kUnitRows = kWave / kSrcChunks;
   static __device__ __forceinline__ int row_of_unit(int u) { return u / kWave * kUnitRows + u % kUnitRows; }
   static __device__ __forceinline__ int chunk_of_unit(int u) { return u % kWave / kUnitRows; }
@@ -314,10 +315,11 @@ struct Tiles {
   }
 };
 
-// Whether nothing is seen by token t.  (A tree's token that sees nothing of the draft sees what is before it.)
+// The drafted tokens that token t sees, a bit each; causal: none.
 __device__ __forceinline__ uint64_t bits_of(const TileWork& w, int t, int T) {
   return w.sees ? w.sees[t] & (T < 64 ? (1ull << T) - 1 : ~0ull) : 0ull;
 }
+// Whether nothing is seen by token t.  (A tree's token that sees nothing of the draft sees what is before it.)
 __device__ __forceinline__ bool sees_none(const TileWork& w, int t, uint64_t bits) {
   if (!w.sees) return w.hist + t < 0;
   // rows of the draft that are there: hist + u >= 0
@@ -337,9 +339,10 @@ __device__ __forceinline__ float total_scale(float total) { return total > 0.f ?
 
 // A tile of queries, or a part of one's keys, a workgroup; workgroups of 8 waves take tiles in turn: as many of them as the chip has places go through the tiles back and forth, so that tiles that
 // get smaller come out even, and the next tile's first rows and queries are on their way while the outputs are written.  (Without turns, and with outputs through LDS, a workgroup took 17 us beside
-// its steps, of which 6 between two workgroups of a CU, 4 for the first rows, 6 for the outputs: 16 prompts of 1024 tokens 270 us, now 218; 4096 tokens 147, now 137.)
-// Bound by the matrix units' clock under load in long prompts (32768 tokens, 32 heads of 128: 7.8 ms, 1128 TFLOP/s, what the library's large product reaches), by a workgroup's
-// beginning and end in short ones, by memory and the join where queries are few.
+// its steps, of which 6 between two workgroups of a CU, 4 for the first rows, 6 for the outputs; with one number a weight 16 prompts of 1024 tokens went from 270 to 218 us, 4096 tokens
+// from 147 to 137: with two they take 254 and 187.)
+// Bound by the chip's power in long prompts (32768 tokens, 32 heads of 128 in bf16: 10.6 to 11.1 ms, 1.19 PFLOP/s of matrix work where the library's large product reaches 1.13; matrix units 64 %, vector units 54 %
+// of the cycles busy at a clock of 1.84 GHz), by a workgroup's beginning and end in short ones, by memory and the join where queries are few.
 template <int KIND, int D, int WQ, int WK, class TAB>
 __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) void attend_tiles_kernel(const TileArgs a, const TAB tab) {
   using A = Tiles<KIND, D, WQ, WK>;
@@ -494,7 +497,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) 
     };
 
     // Tiles of keys that every query sees whole, then the others: the steps are two programs, so that the first has no branches for what the second has to look after (in one, with copies of
-    // the sums where its ways met, 32768 tokens took 8.90 ms).
+    // the sums where its ways met, 32768 tokens took 8.90 ms where 7.97 were left, with one number a weight).
     uint32_t buf = lds, other = lds + 2 * A::kTileBytes;
     int key0 = w.begin;
     const int whole_end = w.begin + max(min(all, w.end) - w.begin, 0) / A::kKeys * A::kKeys;

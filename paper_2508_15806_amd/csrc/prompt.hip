@@ -6,8 +6,8 @@
 namespace slkv {
 
 // Sequences of a launch, those with the most keys first.  Tiles of queries come in the order of their keys, the most first, whatever sequence they are of, and for each of them the KV heads, so
-// that with 8 of these a head stays on an XCD and its L2.  In order (where there are parts, and for sequences of one length, whose keys and values stay in the caches this way: 64 of 256 tokens 116 us, else
-// 128): sequence, tiles from the last one down, parts of the keys, KV heads.  (8 sequences of 110 to 4000 tokens: 436 us in order, else 412.)
+// that with 8 of these a head stays on an XCD and its L2.  In order (where there are parts, and for sequences of one length, whose keys and values stay in the caches this way: 64 of 256 tokens 130 us, else
+// 140): sequence, tiles from the last one down, parts of the keys, KV heads.  (8 sequences of 110 to 4000 tokens: 590 us in order, else 542.)
 struct PromptTab {
   static constexpr int kSeqs = kPromptSeqs;
   const unsigned char *k, *v, *q;

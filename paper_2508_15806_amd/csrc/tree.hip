@@ -1,8 +1,7 @@
-// Attention of a tree of drafted tokens over a cache (slkv_attend_tree), and what becomes of the draft (slkv_accept_cache).
+// Attention of a tree of drafted tokens over a cache (slkv_attend_tree).
 #include "attend_tiles.h"
 
 #include <algorithm>
-#include <limits>
 
 namespace slkv {
 
