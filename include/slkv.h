@@ -448,13 +448,17 @@ slkv_status slkv_accept_cache(const slkv_cache_desc* desc, const slkv_cache* cac
  * A query that sees no key (n_b > m_b): out 0, lse -infinity.  Infinities and NaN in keys and values that a query does not see do not reach it.  The result does
  * not depend on what else runs, and has the same bits every time.
  * Products q . k are exact (fp32 elements: rounded), their sums, the softmax and lse fp32; a weight enters the product with v as it is for SLKV_F32, and as two 16-bit numbers otherwise, which hold it to
- * 2^-16 of itself (SLKV_F16: to 2^-21 of itself or 2^-36 of the query's largest weight, whichever is more; an infinite v beside a weight that they cannot hold, below 2^-100 (SLKV_F16: 2^-36) of the largest, may give NaN); out is rounded once.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
+ * 2^-16 of itself (SLKV_F16: to 2^-21 of itself or 2^-36 of the query's largest weight, whichever is more; an infinite v beside a weight that they cannot hold, below 2^-100 (SLKV_F16: 2^-36) of the largest, may give NaN); out is rounded once.
+ * With SLKV_PROMPT_SHORT_WEIGHTS a weight enters that product as one number, rounded to the type of the queries (2^-8 of itself, SLKV_F16: 2^-11; SLKV_F32: no difference): long prompts take a quarter less time, and outputs
+ * are up to 1.4 times as far from the exact ones.  Sums are divided at the end: results are finite for |x| up to 2^22 and |v| times the keys up to 2^118.
  */
+#define SLKV_PROMPT_SHORT_WEIGHTS 1
 typedef struct {
   uint32_t struct_size;        /* sizeof(slkv_prompt_desc) */
   int32_t dtype;               /* slkv_dtype, all but SLKV_BF16_KV_MXFP4 */
   int32_t B, Hq, Hkv, d;       /* d in {64, 128}; Hq % Hkv == 0 */
-  int32_t reserved[2];         /* 0 */
+  int32_t options;             /* 0 or SLKV_PROMPT_SHORT_WEIGHTS */
+  int32_t reserved;            /* 0 */
   const int64_t* h_cu_q;       /* [B+1] host: queries, non-decreasing, >= 0, last < 2^31 */
   const int64_t* h_cu_k;       /* [B+1] host: tokens of K and V, of a sequence 2^30 at most; NULL: h_cu_q (whole prompts) */
   /* element (head, token, :) of an array at head*stride_head + token*stride_tok; rows of d elements contiguous; strides >= 0 and multiples of 16

@@ -163,14 +163,15 @@ class RaggedCall(_Buffers):
 class PromptCall(_OnDevice):
     """Causal attention of a batch of packed prompts, or of their next pieces behind a history: what comes before LayerCall in a layer.
 
-    cu_seqlens [B + 1]: the queries of every sequence; cu_k [B + 1]: its keys, of which the queries are the latest; None: the same.  Calls run on `stream`, or the
+    cu_seqlens [B + 1]: the queries of every sequence; cu_k [B + 1]: its keys, of which the queries are the latest; None: the same.  short_weights: softmax weights enter the product with the
+    values as one number of the queries' type, not two: long prompts in a quarter less time, outputs up to 1.4 times as far from the exact ones.  Calls run on `stream`, or the
     current stream of the device, and have scratch of their own on every stream and in every graph that torch captures; the object outlives these graphs.  Several host threads may
     call one object."""
 
-    def __init__(self, dtype, B_, Hq, Hkv, d, cu_seqlens, cu_k=None, device="cuda"):
+    def __init__(self, dtype, B_, Hq, Hkv, d, cu_seqlens, cu_k=None, device="cuda", short_weights=False):
         code, self.query_dtype, self.row_dtype = DTYPES[dtype]
         self.dtype, self.B, self.Hq, self.Hkv, self.d = dtype, B_, Hq, Hkv, d
-        self.batch = B.PromptBatch(code, B_, Hq, Hkv, d, cu_seqlens, cu_k)
+        self.batch = B.PromptBatch(code, B_, Hq, Hkv, d, cu_seqlens, cu_k, B.SLKV_PROMPT_SHORT_WEIGHTS if short_weights else 0)
         self.queries = int(self.batch.cu_q[-1])
         self.keys = self.queries if cu_k is None else int(self.batch.cu_k[-1])
         self.workspace_bytes = B.slkv_prompt_workspace_bytes(self.batch)

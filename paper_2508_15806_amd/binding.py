@@ -18,6 +18,7 @@ SLKV_F32, SLKV_BF16, SLKV_F16, SLKV_BF16_KV_FP8, SLKV_BF16_KV_MXFP4 = 0, 1, 2, 3
 SLKV_POOL_NONE, SLKV_POOL_MAX, SLKV_POOL_AVG = 0, 1, 2
 SLKV_BUDGET_EXACT, SLKV_BUDGET_PAPER_LITERAL, SLKV_BUDGET_EXACT_PER_QUERY_HEAD = 0, 1, 2
 SLKV_AGG_MICRO, SLKV_AGG_MACRO = 0, 1
+SLKV_PROMPT_SHORT_WEIGHTS = 1
 
 STATUS_NAMES = {0: "SLKV_OK", 1: "SLKV_ERR_NULL", 2: "SLKV_ERR_BAD_ARG", 3: "SLKV_ERR_BAD_VALUE",
                 4: "SLKV_ERR_UNSUPPORTED", 5: "SLKV_ERR_WORKSPACE", 6: "SLKV_ERR_CAPACITY", 7: "SLKV_ERR_HIP"}
@@ -87,7 +88,7 @@ class CacheArrays(C.Structure):
 
 class PromptDesc(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32),
-                ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("reserved", C.c_int32 * 2),
+                ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("reserved", C.c_int32 * 2),      # options, reserved
                 ("h_cu_q", C.c_void_p), ("h_cu_k", C.c_void_p), ("strides", C.c_int64 * 8)]
 
 
@@ -440,13 +441,13 @@ def slkv_accept_cache(layout, cache, T, path, at=None, q=None, lse=None, weight_
 class PromptBatch:
     """Host-side descriptor of a batch of packed prompts; keeps the numpy arrays it points to alive.  Strides are those of the tensors of a call."""
 
-    def __init__(self, dtype, B, Hq, Hkv, d, cu_q, cu_k=None):
+    def __init__(self, dtype, B, Hq, Hkv, d, cu_q, cu_k=None, options=0):
         self.cu_q = np.array(cu_q, dtype=np.int64)                 # copies: the batch stays what it is
         self.cu_k = None if cu_k is None else np.array(cu_k, dtype=np.int64)
         for cu, name in ((self.cu_q, "cu_q"), (self.cu_k, "cu_k")):
             if cu is not None and cu.shape != (B + 1,):
                 raise ValueError("%s: %d entries wanted, got shape %s" % (name, B + 1, cu.shape))
-        self.desc = PromptDesc(C.sizeof(PromptDesc), int(dtype), B, Hq, Hkv, d, (C.c_int32 * 2)(0, 0), self.cu_q.ctypes.data,
+        self.desc = PromptDesc(C.sizeof(PromptDesc), int(dtype), B, Hq, Hkv, d, (C.c_int32 * 2)(options, 0), self.cu_q.ctypes.data,
                                None if cu_k is None else self.cu_k.ctypes.data, (C.c_int64 * 8)(0, 0, 0, 0, 0, 0, d, 0))
         self.desc.strides[7] = d * max(int(self.cu_q[-1]), 1)      # (of out: [Hq][tokens][d] until a call says otherwise)
         self.address = C.addressof(self.desc)

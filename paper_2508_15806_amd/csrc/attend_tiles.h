@@ -248,8 +248,9 @@ struct Tiles {
   }
 
   // acc += p V of one subtile; vt: V in LDS, at the subtile.  16-bit types: a weight enters as two numbers, which hold it to 2^-16 (fp16: 2^-21) of itself, as in slkv_attend_cache: one
-  // would add as much error as the output's own rounding.  The second product is half of the call's matrix work more: a third of the time where that is what a call takes its time with (32 heads of
+  // (ONE, where the caller asks for it) would add as much error as the output's own rounding.  The second product is half of the call's matrix work more: a third of the time where that is what a call takes its time with (32 heads of
   // 128 in bf16: 32768 tokens 7.9 ms with one number, 10.6 with two; 512 queries behind 65024 keys 555, 715 us), 6 % where it is not (32 drafted tokens on 128 segments of 1024 rows 38.5, 40.8 us).
+  template <bool ONE>
   static __device__ __forceinline__ void add_values(f32x16 (&acc)[kDT], const f32x16& p, uint32_t vt, int lane) {
     if constexpr (kF32) {
       const int g = lane >> 5, l32 = lane & 31;
@@ -277,10 +278,15 @@ struct Tiles {
         u32x4 hi, lo, vo[kDT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          uint32_t h2, l2;
-          halves(p[c * 8 + j * 2], p[c * 8 + j * 2 + 1], h2, l2);
-          hi[j] = h2;
-          lo[j] = l2;
+          const float x = p[c * 8 + j * 2], y = p[c * 8 + j * 2 + 1];
+          if constexpr (ONE) {
+            hi[j] = pair(x, y);
+          } else {
+            uint32_t h2, l2;
+            halves(x, y, h2, l2);
+            hi[j] = h2;
+            lo[j] = l2;
+          }
         }
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
@@ -293,8 +299,10 @@ struct Tiles {
           }
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt) acc[dt] = mfma(vo[dt], hi, acc[dt]);
+        if constexpr (!ONE) {
 #pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) acc[dt] = mfma(vo[dt], lo, acc[dt]);
+          for (int dt = 0; dt < kDT; ++dt) acc[dt] = mfma(vo[dt], lo, acc[dt]);
+        }
       }
     }
   }
@@ -491,7 +499,7 @@ __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) 
             }
           }
         } else {
-          A::add_values(acc, x[s], vs, lane);
+          A::template add_values<TAB::kOneNumber>(acc, x[s], vs, lane);
         }
       }
     };

@@ -10,6 +10,7 @@ namespace slkv {
 // 140): sequence, tiles from the last one down, parts of the keys, KV heads.  (8 sequences of 110 to 4000 tokens: 590 us in order, else 542.)
 struct PromptTab {
   static constexpr int kSeqs = kPromptSeqs;
+  static constexpr bool kOneNumber = false;            // of the queries' type a weight
   const unsigned char *k, *v, *q;
   unsigned char* out;
   float* lse;
@@ -86,6 +87,10 @@ struct PromptTab {
   }
 };
 
+struct PromptTabOne : PromptTab {
+  static constexpr bool kOneNumber = true;
+};
+
 // Everything that can be checked without the arrays; the plan of a descriptor that passes.
 static slkv_status prompt_checks(const slkv_prompt_desc* d, PromptPlan& plan) {
   if (!d) return fail(SLKV_ERR_NULL, "desc is NULL");
@@ -96,7 +101,8 @@ static slkv_status prompt_checks(const slkv_prompt_desc* d, PromptPlan& plan) {
   if (d->B > (1 << 20) || d->Hkv > (1 << 16) || d->Hq > (1 << 16)) return fail(SLKV_ERR_BAD_ARG, "B, Hq or Hkv too large");
   if (d->Hq % d->Hkv) return fail(SLKV_ERR_BAD_ARG, "Hq %% Hkv != 0");
   if (d->d != 64 && d->d != 128) return fail(SLKV_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", d->d);
-  if (d->reserved[0] || d->reserved[1]) return fail(SLKV_ERR_BAD_ARG, "desc.reserved must be 0");
+  if (d->options & ~SLKV_PROMPT_SHORT_WEIGHTS) return fail(SLKV_ERR_BAD_ARG, "desc.options: unknown bits %d", d->options);
+  if (d->reserved) return fail(SLKV_ERR_BAD_ARG, "desc.reserved must be 0");
   slkv_status st = validate_offsets(d->h_cu_q, d->B, "h_cu_q");
   if (st != SLKV_OK) return st;
   if (d->h_cu_k && (st = validate_offsets(d->h_cu_k, d->B, "h_cu_k")) != SLKV_OK) return st;
@@ -202,7 +208,12 @@ extern "C" slkv_status slkv_attend_prompt(const slkv_prompt_desc* desc, const vo
         constexpr int kWQ = decltype(wq)::value, kWK = decltype(wk)::value;
         {
           ScopedKernelTimer timer(SLKV_K_PROMPT);
-          SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTab>), dim3(std::min((unsigned)blocks, tile_places<Tiles<kKind, kDim, kWQ, kWK>>())), dim3(kWQ * kWK * kWave), 0, stream, a, t);
+          const dim3 grid(std::min((unsigned)blocks, tile_places<Tiles<kKind, kDim, kWQ, kWK>>())), block(kWQ * kWK * kWave);
+          if (kKind == SLKV_F32 || !(desc->options & SLKV_PROMPT_SHORT_WEIGHTS)) {
+            SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTab>), grid, block, 0, stream, a, t);
+          } else if constexpr (kKind != SLKV_F32) {
+            SLKV_LAUNCH((attend_tiles_kernel<kKind, kDim, kWQ, kWK, PromptTabOne>), grid, block, 0, stream, a, PromptTabOne{t});
+          }
         }
         if (p.split) {
           ScopedKernelTimer timer(SLKV_K_TILES_JOIN);

@@ -11,6 +11,7 @@ namespace slkv {
 // max(1, ceil(room / each)).  Workgroups: parts, in each of them the tiles of queries.
 template <int N>
 struct TreeTab {
+  static constexpr bool kOneNumber = false;            // of the queries' type a weight
   static constexpr int kSegs = N, kGroup = 16, kGroups = (N + kGroup - 1) / kGroup;
   static_assert(kGroups <= kWave, "a lane for every group");
   const unsigned char *k, *v, *k_scale, *v_scale, *q;

@@ -62,6 +62,18 @@ def test_descriptor_struct():
     assert L.slkv_prompt_workspace_bytes(None, C.addressof(n)) == 1 and L.slkv_prompt_workspace_bytes(batch().address, None) == 1
 
 
+def test_options():
+    lay = dict(dtype=B.SLKV_BF16, B=2, Hq=8, Hkv=2, d=128, cu_q=[0, 1, 2], cu_k=[0, 9000, 18000])
+    plain, short = B.PromptBatch(**lay), B.PromptBatch(options=B.SLKV_PROMPT_SHORT_WEIGHTS, **lay)
+    assert B.slkv_prompt_workspace_bytes(plain) == B.slkv_prompt_workspace_bytes(short)
+    assert api.PromptCall("bf16", 2, 8, 2, 128, [0, 1, 2], device="cpu:0").batch.desc.reserved[0] == 0
+    assert api.PromptCall("bf16", 2, 8, 2, 128, [0, 1, 2], device="cpu:0", short_weights=True).batch.desc.reserved[0] == B.SLKV_PROMPT_SHORT_WEIGHTS
+    for bad in (2, 3, -1, 1 << 30):
+        x = batch()
+        x.desc.reserved[0] = bad
+        assert attend(x) == 2
+
+
 def test_refused_calls():
     for name in ("q", "k", "v", "out", "ws"):
         assert attend(**{name: NULL}) == 1
