@@ -349,8 +349,8 @@ __device__ __forceinline__ float total_scale(float total) { return total > 0.f ?
 // get smaller come out even, and the next tile's first rows and queries are on their way while the outputs are written.  (Without turns, and with outputs through LDS, a workgroup took 17 us beside
 // its steps, of which 6 between two workgroups of a CU, 4 for the first rows, 6 for the outputs; with one number a weight 16 prompts of 1024 tokens went from 270 to 218 us, 4096 tokens
 // from 147 to 137: with two they take 254 and 187.)
-// Bound by the chip's power in long prompts (32768 tokens, 32 heads of 128 in bf16: 10.6 to 11.1 ms, 1.19 PFLOP/s of matrix work where the library's large product reaches 1.13; matrix units 64 %, vector units 54 %
-// of the cycles busy at a clock of 1.84 GHz), by a workgroup's beginning and end in short ones, by memory and the join where queries are few.
+// Bound by the chip's power in long prompts (32768 tokens, 32 heads of 128 in bf16: 10.6 to 11.8 ms by box, 1.1 to 1.24 PFLOP/s of matrix work where the library's large product reaches 1.13; matrix units 64 %, vector units 54 %
+// of the cycles busy at a clock of 1.82 GHz), by a workgroup's beginning and end in short ones, by memory and the join where queries are few.
 template <int KIND, int D, int WQ, int WK, class TAB>
 __global__ __launch_bounds__(WQ* WK* kWave, (Tiles<KIND, D, WQ, WK>::kPerSimd)) void attend_tiles_kernel(const TileArgs a, const TAB tab) {
   using A = Tiles<KIND, D, WQ, WK>;
