@@ -1,5 +1,7 @@
 """slkv_attend_prompt against the float64 oracle: types, head layouts, lengths from nothing to long, histories, strides, values that are not finite."""
 
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -312,3 +314,30 @@ def test_first_call_inside_a_capture():
         assert all(torch.equal(a, b) and torch.equal(c, b) for a, b, c in zip(got, want, again)), turn
     del g, got
     assert all(torch.equal(a, b) for a, b in zip(call.run(q, k, v), want))
+
+
+def test_two_host_threads_on_one_stream():
+    """Calls of one object whose keys are split, from two threads at once, each with inputs and strides of its own."""
+    rng = np.random.default_rng(16)
+    cu_q, cu_k = offsets([4, 30]), offsets([5000, 3001])
+    call = api.PromptCall("bf16", 2, 8, 2, 128, cu_q, cu_k)
+    sets = [inputs(rng, "bf16", 8, 2, 128, cu_q, cu_k) for _ in range(2)]
+    sets[1] = (sets[1][0].transpose(0, 1).contiguous().transpose(0, 1),) + sets[1][1:]
+    want = [[x.clone() for x in api.PromptCall("bf16", 2, 8, 2, 128, cu_q, cu_k).run(*s)] for s in sets]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def several(i):
+        try:
+            for _ in range(60):
+                got[i].append(call.run(*sets[i]))
+        except BaseException as e:
+            errors.append(e)
+
+    threads = [threading.Thread(target=several, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors and all(torch.equal(a, b) for i in range(2) for x in got[i] for a, b in zip(x, want[i]))
